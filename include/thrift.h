@@ -13,6 +13,8 @@
  *   thrift_attn_prefill_chunk  the same kernel for a chunk of queries against a longer key range
  *   thrift_attn_decode      the same algorithm for one query token over a dual 4-bit / 16-bit KV
  *                           cache (Sec. 4.1, last sentences; Sec. 5), evaluated split-K
+ * and, around them, rotary positions (thrift_rope) and a paged 16-bit cache (thrift_page_map, thrift_paged_append,
+ * thrift_paged_decode).
  *
  * Conventions shared by every call
  *   - Every pointer is a DEVICE pointer unless the comment says "host".  The caller owns every
@@ -23,7 +25,7 @@
  *   - No global state: calls on different streams are independent.
  *   - Tensors are contiguous, last index fastest.  16-bit tensors are IEEE fp16 (THRIFT_F16) or
  *     bfloat16 (THRIFT_BF16).
- *   - Shape limits of this version: D == 128, Bk == 64, Bq in {64, 128} (prefill), Hq a multiple of Hkv,
+ *   - Shape limits of this version (rotary positions and the paged cache state their own): D == 128, Bk == 64, Bq in {64, 128} (prefill), Hq a multiple of Hkv,
  *     at most 4096 key blocks per row (N <= 262144), a GQA group of at most 32 heads in decode, a decode
  *     cache capacity Nkv that is a multiple of Bk.  Sequence lengths need NOT be multiples of Bq or Bk (a
  *     short last block is handled as the entry points below describe).  Anything else returns
@@ -368,6 +370,124 @@ thrift_status thrift_kv_cache_append_advance(const void* k_new, const void* v_ne
                                              const int32_t* seqlens, const int32_t* new_lens, int32_t* seqlens_out,
                                              void* k16, void* v16, uint8_t* k4, uint8_t* ks, uint8_t* v4, uint8_t* vs, float* kmean,
                                              int B, int Hkv, int Nkv, int D, int Bk, void* stream);
+
+/*
+ * Around the attention: rotary positions, and a paged 16-bit cache with the attention that reads it.
+ *
+ * Rotary positions.  Channels 0 .. rot-1 of a head are rot/2 pairs; pair i of the token at position p is turned by the angle
+ * a = p * freqs[i] and both channels are multiplied by `gain`:
+ *   y0 = gain * (x0 cos a - x1 sin a),   y1 = gain * (x1 cos a + x0 sin a);     channels rot .. D-1 are copied.
+ * Angles are formed and reduced in fp64, cos and sin are good to 2e-7, the products are fp32 and are rounded once.
+ */
+typedef enum THRIFT_ENUM_INT { THRIFT_ROPE_HALF = 0,         /* pair i: channels i and i + rot/2 */
+                               THRIFT_ROPE_INTERLEAVED = 1   /* pair i: channels 2i and 2i + 1 */ } thrift_rope_layout;
+
+/* Host: freqs[i], i < rot/2 (radians per position) for rotary base `base`, and the gain of the scaling (nullable).
+ *   THRIFT_ROPE_PLAIN     theta_i = base^(-2i/rot), gain 1
+ *   THRIFT_ROPE_LINEAR    theta_i / factor: positions interpolated, gain 1
+ *   THRIFT_ROPE_NTK       theta_i of the base  base * factor^(rot/(rot-2)), gain 1: the slowest pair as THRIFT_ROPE_LINEAR, the
+ *                         fastest as it was (rot >= 4)
+ *   THRIFT_ROPE_BY_PARTS  theta_i * ((1-w) / factor + w), w = clamp((original * theta_i / (2 pi) - slow) / (fast - slow), 0, 1):
+ *                         pairs that turn less than `slow` times within `original` tokens are interpolated, those that turn more
+ *                         than `fast` times are left (arXiv 2309.00071, which uses 1 and 32); gain 0.1 ln(factor) + 1
+ * rot even, 2 .. 1024; base > 1; factor >= 1 (not used by PLAIN); original > 0 and fast > slow >= 0 (BY_PARTS only); all finite.
+ * Otherwise THRIFT_ERR_SHAPE. */
+typedef enum THRIFT_ENUM_INT { THRIFT_ROPE_PLAIN = 0, THRIFT_ROPE_LINEAR = 1, THRIFT_ROPE_NTK = 2, THRIFT_ROPE_BY_PARTS = 3 } thrift_rope_scaling;
+thrift_status thrift_rope_frequencies(int rot, double base, int scaling, double factor, double original, double slow, double fast,
+                                      double* freqs, float* gain);
+
+/*
+ * Rotation of the query heads, and in the same launch of the key heads, of a batch.
+ *   q, q_out [B,Hq,N,D], k, k_out (nullable, both or neither) [B,Hkv,N,D]  16-bit (dt)
+ *   *_strides (host, nullable): elements from one batch entry, head and token to the next; NULL = contiguous.  The channels of a
+ *     head are contiguous.  So q and k may lie in the output of one projection, and the results need not lie as the inputs do.
+ *     Any strides of an input are allowed (0 repeats it); the elements of an output must not coincide.  q_out may be q with the
+ *     same strides (in place), k_out likewise k; apart from that outputs overlap nothing.
+ *   positions (nullable) int32: token (b, n) is at positions[b * positions_stride + n]; NULL: n
+ *   freqs (device) [rot/2] fp64; rot even, 2 .. D; D <= 1024; layout: thrift_rope_layout
+ * Every size runs; 16-byte accesses are used where addresses and strides allow them (D, rot/2 resp. rot multiples of 8).
+ */
+thrift_status thrift_rope(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides, int Hq,
+                          const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides, int Hkv, thrift_dtype dt,
+                          const int32_t* positions, int64_t positions_stride, const double* freqs, int rot, int layout, float gain,
+                          int B, int N, int D, void* stream);
+
+/* Gradient of thrift_rope with respect to its inputs: the transposed rotation of the gradients of its outputs (the angle's sign
+ * turned, the same gain).  q, k: gradients of q_out, k_out; q_out, k_out: gradients of q, k.  Arguments as thrift_rope. */
+thrift_status thrift_rope_backward(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides, int Hq,
+                                   const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides, int Hkv, thrift_dtype dt,
+                                   const int32_t* positions, int64_t positions_stride, const double* freqs, int rot, int layout, float gain,
+                                   int B, int N, int D, void* stream);
+
+/*
+ * Pages of a paged cache.  A page holds page_size consecutive tokens of one sequence (page_size: 16, 32, 64, 128 or 256); the pages of
+ * sequence b are block_table[b][0 .. ceil(length / page_size) - 1].  Slot s is token s % page_size of page s / page_size.  Free
+ * pages lie on a stack: free_pages[0 .. free_count[0] - 1], the next one to be taken last.
+ *
+ * thrift_page_map gives the new tokens of a step their places, from the lengths on the device alone.  The new tokens of all sequences
+ * lie in rows one after the other, in sequence order: sequence b has rows starts[b] .. starts[b+1] - 1.
+ *   seqlens [B]: tokens cached before the call (clamped to 0 .. max_pages * page_size); new_lens [B]: new tokens (negative: 0)
+ *   block_table [B,max_pages]: entries of new pages are written, the others are left as they are
+ *   free_pages [free_capacity], free_count [1] (clamped to 0 .. free_capacity): read only
+ *   rows: length of slots and positions.  Rows past the end of these arrays are cut off (starts stops at `rows`)
+ *   slots [rows]: where the row's token goes, -1 for a row without a place: a row behind the last sequence, a token past the block
+ *     table's width, a token for which no free page was left (sequences are served in order), one whose page the table names
+ *     outside 0 .. n_pages - 1
+ *   positions [rows]: the token's position in its sequence; 0 behind the last sequence
+ *   starts [B+1]; seqlens_out [B]: tokens that have a place after the call; free_count_out [1]: free pages left
+ * Outputs are arrays of their own (seqlens_out is not seqlens, free_count_out not free_count).  B <= 4096;
+ * n_pages * page_size and max_pages * page_size + rows below 2^31.
+ */
+thrift_status thrift_page_map(const int32_t* seqlens, const int32_t* new_lens, int B, int page_size, int n_pages,
+                              int32_t* block_table, int max_pages, const int32_t* free_pages, int free_capacity, const int32_t* free_count,
+                              int rows, int32_t* slots, int32_t* positions, int32_t* starts, int32_t* seqlens_out, int32_t* free_count_out,
+                              void* stream);
+
+/*
+ * Returns the pages of finished sequences: for every b with drop[b] != 0 the ceil(seqlens[b] / page_size) pages of the sequence are put
+ * on the stack in order (sequence, page) and its length becomes 0.  Table entries outside 0 .. n_pages - 1 are not put back, nor is what would pass
+ * free_capacity.  block_table is read only.  seqlens_out [B], free_count_out [1]: arrays of their own.
+ */
+thrift_status thrift_page_release(const int32_t* seqlens, const int32_t* drop, int B, int page_size, int n_pages,
+                                  const int32_t* block_table, int max_pages, int32_t* free_pages, int free_capacity, const int32_t* free_count,
+                                  int32_t* seqlens_out, int32_t* free_count_out, void* stream);
+
+/*
+ * New tokens into a paged cache: row t's keys, rotated, and values go to slots[t]; its queries are rotated into q_out.
+ *   q (nullable, then q_out is unused) [T,Hq,D], k, v [T,Hkv,D] 16-bit (dt); *_strides (host, nullable): elements from one token and
+ *     one head to the next, NULL = contiguous: q, k and v may lie in the output of one projection.  q_out [T,Hq,D] contiguous; may
+ *     be q itself (contiguous then).
+ *   slots [T]: from thrift_page_map.  A row whose slot lies outside 0 .. n_pages * page_size - 1 is skipped: its keys and values go
+ *     nowhere and its q_out row is left as it was.  No slot may occur twice.
+ *   positions [T], freqs, rot, layout, gain as thrift_rope; rot == 0: nothing is rotated (positions and freqs unused, q copied)
+ *   k_pages, v_pages [n_pages,Hkv,page_size,D] 16-bit (dt)
+ * D even, <= 1024.
+ */
+thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
+                                  const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,
+                                  const int32_t* positions, const double* freqs, int rot, int layout, float gain,
+                                  void* k_pages, void* v_pages, int n_pages, int page_size, int D, void* stream);
+
+/* Host: bytes of workspace thrift_paged_decode needs (0 for sizes that it refuses). */
+size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D);
+
+/*
+ * Attention of one new token per sequence over a paged 16-bit cache; the new token's key and value are in the cache already.
+ *   o = sum_j p_j v_j,  p = softmax over j < seqlens[b] of softmax_scale * q . k_j; scores, probabilities and sums in fp32
+ *   q [B,Hq,D] 16-bit (dt); k_pages, v_pages [n_pages,Hkv,page_size,D]; block_table [B,max_pages]; D 64, 128 or 256; Hq a multiple
+ *     of Hkv, at most 32 heads per KV head
+ *   seqlens [B]: cached tokens, clamped to 0 .. max_pages * page_size.  What pages hold past the length reaches no result, whatever
+ *     it is.  A sequence of length 0 gives zeros.
+ *   block_table entries within the length must name pages; others give unspecified numbers but are never followed outside
+ *     k_pages and v_pages (clamped to 0 .. n_pages - 1).
+ *   softmax_scale <= 0 selects 1/sqrt(D)
+ *   out [B,Hq,D] in out_dt; lse (nullable) [B,Hq] fp32: log-sum-exp of the scaled scores, -inf for length 0
+ *   workspace: thrift_paged_decode_workspace(...) bytes, 16-byte aligned; the next call on the same stream may use it again
+ */
+thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,
+                                  const int32_t* block_table, int max_pages, const int32_t* seqlens, int B, int Hq, int Hkv, int D,
+                                  int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement helper (not a step of the method): one launch of a microbenchmark of a hardware rate that the

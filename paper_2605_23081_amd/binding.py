@@ -10,7 +10,7 @@ import ctypes as C
 import math
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -26,7 +26,9 @@ EXPORTS = (
     "thrift_attn_prefill_workspace", "thrift_attn_prefill", "thrift_attn_prefill_chunk", "thrift_attn_prefill_ordered",
     "thrift_attn_decode_workspace", "thrift_attn_decode_least_workspace", "thrift_attn_decode", "thrift_attn_decode_shared", "thrift_attn_decode_static",
     "thrift_kv_cache_append", "thrift_kv_cache_append_advance",
-    "thrift_attention_forward_workspace", "thrift_attention_forward", "thrift_peak_probe",
+    "thrift_attention_forward_workspace", "thrift_attention_forward",
+    "thrift_rope_frequencies", "thrift_rope", "thrift_rope_backward", "thrift_page_map", "thrift_page_release",
+    "thrift_paged_append", "thrift_paged_decode_workspace", "thrift_paged_decode", "thrift_peak_probe",
 )
 
 _lib = None
@@ -73,6 +75,16 @@ def lib() -> C.CDLL:
         L.thrift_attention_forward_workspace.argtypes = [i, i, i, i, i, i, i, i, d, i]
         L.thrift_attention_forward.argtypes = [p, p, p, i, i, i, i, i, i, i, i, i, d, i, i, f, p, i, p, p, sz, p]
         L.thrift_kv_cache_append_advance.argtypes = [p, p, i, i, p, p, p, p, p, p, p, p, p, p, i, i, i, i, i, p]
+        i64 = C.c_int64
+        L.thrift_rope_frequencies.argtypes = [i, d, i, d, d, d, d, C.POINTER(d), C.POINTER(f)]
+        L.thrift_rope.argtypes = [p, p, p, p, i, p, p, p, p, i, i, p, i64, p, i, i, f, i, i, i, p]
+        L.thrift_rope_backward.argtypes = L.thrift_rope.argtypes
+        L.thrift_page_map.argtypes = [p, p, i, i, i, p, i, p, i, p, i, p, p, p, p, p, p]
+        L.thrift_page_release.argtypes = [p, p, i, i, i, p, i, p, i, p, p, p, p]
+        L.thrift_paged_append.argtypes = [p, p, p, i, p, p, p, p, i, i, i, p, p, p, i, i, f, p, p, i, i, i, p]
+        L.thrift_paged_decode_workspace.restype = sz
+        L.thrift_paged_decode_workspace.argtypes = [i] * 6
+        L.thrift_paged_decode.argtypes = [p, i, p, p, i, p, i, p, i, i, i, i, i, f, p, i, p, p, sz, p]
         L.thrift_peak_probe.argtypes = [i, i, i, p, sz, C.POINTER(C.c_double), p]
         _lib = L
     return _lib
@@ -464,6 +476,247 @@ def thrift_peak_probe(kind: int, buffer: torch.Tensor, iters: int = 2000, dtype:
     _check(lib().thrift_peak_probe(int(kind), _DT[dtype], int(iters), _ptr(buffer), buffer.numel(), C.byref(work), _stream()),
            "thrift_peak_probe")
     return float(work.value)
+
+
+# ---- around the attention: rotary positions and the paged 16-bit cache ----
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "by_parts": 3}
+
+
+def rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original: float = 0.0,
+                     slow: float = 1.0, fast: float = 32.0, device=None) -> Tuple[torch.Tensor, float]:
+    """Radians per position of the rot/2 pairs (fp64, on `device`) and the gain, for the scalings of include/thrift.h."""
+    freqs, gain = (C.c_double * max(rot // 2, 1))(), C.c_float()
+    _check(lib().thrift_rope_frequencies(int(rot), float(base), ROPE_SCALINGS[scaling], float(factor), float(original), float(slow),
+                                         float(fast), freqs, C.byref(gain)), "thrift_rope_frequencies")
+    return torch.tensor(list(freqs), dtype=torch.float64, device=device), float(gain.value)
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """Device tensors, all on the current device: the calls run on its current stream."""
+    current = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None:
+            assert t.is_cuda and t.device.index == current, f"a tensor on {t.device}; the current device is {current}"
+
+
+def _apart(t: torch.Tensor) -> bool:
+    """No two elements of t share an address (sufficient: every stride passes what the smaller ones reach)."""
+    reach = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz > 1):
+        if stride < reach:
+            return False
+        reach = stride * (size - 1) + reach
+    return True
+
+
+def _strides(t: torch.Tensor, dims) -> C.Array:
+    return (C.c_int64 * len(dims))(*[t.stride(d) for d in dims])
+
+
+def _heads(t: torch.Tensor, shape, dtype) -> None:
+    assert tuple(t.shape) == tuple(shape) and t.dtype == dtype, (tuple(t.shape), tuple(shape), t.dtype, dtype)
+    assert t.stride(-1) == 1 or t.shape[-1] == 1, "the channels of a head are contiguous"
+
+
+def _rope(name: str, q, k, freqs, positions, layout: str, gain: float, q_out, k_out):
+    assert q.dtype in (torch.float16, torch.bfloat16), q.dtype
+    B, Hq, N, D = q.shape
+    _heads(q, q.shape, q.dtype)
+    if k is None:
+        assert k_out is None
+    else:
+        _heads(k, (B, k.shape[1], N, D), q.dtype)
+        if k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        _heads(k_out, k.shape, k.dtype)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _heads(q_out, q.shape, q.dtype)
+    assert _apart(q_out) and (k_out is None or _apart(k_out)), "elements of an output coincide"
+    assert freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous(), (freqs.dtype, tuple(freqs.shape))
+    step = 0
+    if positions is not None:
+        assert positions.dtype == torch.int32 and tuple(positions.shape) in ((N,), (B, N)) and (N == 1 or positions.stride(-1) == 1), tuple(positions.shape)
+        step = positions.stride(0) if positions.dim() == 2 else 0
+    _here(q, k, q_out, k_out, freqs, positions)
+    s = lambda t: None if t is None else _strides(t, (0, 1, 2))
+    _check(getattr(lib(), name)(_ptr(q), s(q), _ptr(q_out), s(q_out), Hq, _ptr(k), s(k), _ptr(k_out), s(k_out), 0 if k is None else k.shape[1],
+                                _DT[q.dtype], _ptr(positions), step, _ptr(freqs), 2 * freqs.numel(), ROPE_LAYOUTS[layout], float(gain), B, N, D,
+                                _stream()), name)
+    return q_out, k_out
+
+
+def thrift_rope(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: str = "half", gain: float = 1.0,
+                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """q [B,Hq,N,D] and k [B,Hkv,N,D] (or None) with their first 2 * len(freqs) channels turned to positions ([B,N] or [N], default
+    0 .. N-1): (q_out, k_out), contiguous unless given.  Inputs and outputs may be views (a fused projection's [B,N,H,D])."""
+    return _rope("thrift_rope", q, k, freqs, positions, layout, gain, q_out, k_out)
+
+
+def thrift_rope_backward(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: str = "half", gain: float = 1.0,
+                         q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+    """Gradients of thrift_rope's inputs from those of its outputs, q and k (or None); arguments as thrift_rope."""
+    return _rope("thrift_rope_backward", q, k, freqs, positions, layout, gain, q_out, k_out)
+
+
+class PageMap(NamedTuple):
+    """Places of a step's new tokens (include/thrift.h, thrift_page_map)."""
+    slots: torch.Tensor        # [rows] int32
+    positions: torch.Tensor    # [rows] int32
+    starts: torch.Tensor       # [B+1] int32
+    seqlens: torch.Tensor      # [B] int32, after the call
+    free_count: torch.Tensor   # [1] int32, after the call
+
+
+def _ints(shape, *tensors: torch.Tensor) -> None:
+    for t in tensors:
+        assert t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape), (t.dtype, tuple(t.shape), tuple(shape))
+
+
+def _pool(seqlens, block_table, free_pages, free_count) -> Tuple[int, int]:
+    assert block_table.dim() == 2 and free_pages.dim() == 1, (tuple(block_table.shape), tuple(free_pages.shape))
+    B, max_pages = block_table.shape
+    _ints((B, max_pages), block_table), _ints((B,), seqlens), _ints(free_pages.shape, free_pages), _ints((1,), free_count)
+    return B, max_pages
+
+
+def thrift_page_map(seqlens, new_lens, block_table, free_pages, free_count, page_size: int, n_pages: int, rows: int) -> PageMap:
+    """Pages, block-table entries (written into block_table), slots and positions of new_lens [B] new tokens per sequence."""
+    B, max_pages = _pool(seqlens, block_table, free_pages, free_count)
+    _ints((B,), new_lens)
+    _here(seqlens, new_lens, block_table, free_pages, free_count)
+    sizes = (rows, rows, B + 1, B, 1)
+    ends = [sum(-(-n // 4) * 4 for n in sizes[:i + 1]) for i in range(5)]
+    space = torch.empty(ends[-1], dtype=torch.int32, device=seqlens.device)
+    m = PageMap(*(space[e - -(-n // 4) * 4:][:n] for e, n in zip(ends, sizes)))
+    _check(lib().thrift_page_map(_ptr(seqlens), _ptr(new_lens), B, int(page_size), int(n_pages), _ptr(block_table), max_pages,
+                                 _ptr(free_pages), free_pages.numel(), _ptr(free_count), int(rows), *(_ptr(t) for t in m), _stream()),
+           "thrift_page_map")
+    return m
+
+
+def thrift_page_release(seqlens, drop, block_table, free_pages, free_count, page_size: int, n_pages: int) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Puts the pages of the sequences with drop [B] != 0 back on the stack: (seqlens, free_count) after the call."""
+    B, max_pages = _pool(seqlens, block_table, free_pages, free_count)
+    _ints((B,), drop)
+    _here(seqlens, drop, block_table, free_pages, free_count)
+    after, count = torch.empty_like(seqlens), torch.empty_like(free_count)
+    _check(lib().thrift_page_release(_ptr(seqlens), _ptr(drop), B, int(page_size), int(n_pages), _ptr(block_table), max_pages,
+                                     _ptr(free_pages), free_pages.numel(), _ptr(free_count), _ptr(after), _ptr(count), _stream()),
+           "thrift_page_release")
+    return after, count
+
+
+def _pages(k_pages, v_pages) -> None:
+    assert k_pages.dim() == 4 and k_pages.dtype in (torch.float16, torch.bfloat16), (tuple(k_pages.shape), k_pages.dtype)
+    assert k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype and k_pages.is_contiguous() and v_pages.is_contiguous()
+
+
+def thrift_paged_append(k, v, slots, k_pages, v_pages, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                        positions: Optional[torch.Tensor] = None, freqs: Optional[torch.Tensor] = None, layout: str = "half",
+                        gain: float = 1.0) -> Optional[torch.Tensor]:
+    """k, v [T,Hkv,D] into the pages [n_pages,Hkv,page_size,D] at slots [T]; with freqs, k and q [T,Hq,D] are rotated to
+    positions [T].  Returns q_out (contiguous; rows of skipped tokens are left as they were)."""
+    _pages(k_pages, v_pages)
+    T, Hkv, D = k.shape
+    n_pages, _, page_size, _ = k_pages.shape
+    _heads(k, (T, Hkv, D), k_pages.dtype), _heads(v, (T, Hkv, D), k_pages.dtype), _ints((T,), slots)
+    assert k_pages.shape[1] == Hkv and k_pages.shape[3] == D, (tuple(k_pages.shape), tuple(k.shape))
+    rot = 0
+    if freqs is not None:
+        assert freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and freqs.numel() > 0, (freqs.dtype, tuple(freqs.shape))
+        assert positions is not None
+        _ints((T,), positions)
+        rot = 2 * freqs.numel()
+    if q is None:
+        assert q_out is None
+    else:
+        _heads(q, (T, q.shape[1], D), k_pages.dtype)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        assert q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous(), (tuple(q_out.shape), q_out.dtype)
+    _here(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs)
+    s = lambda t: None if t is None else _strides(t, (0, 1))
+    _check(lib().thrift_paged_append(_ptr(q), s(q), _ptr(q_out), 0 if q is None else q.shape[1], _ptr(k), s(k), _ptr(v), s(v), Hkv,
+                                     _DT[k.dtype], T, _ptr(slots), _ptr(positions), _ptr(freqs), rot, ROPE_LAYOUTS[layout], float(gain),
+                                     _ptr(k_pages), _ptr(v_pages), n_pages, page_size, D, _stream()), "thrift_paged_append")
+    return q_out
+
+
+def paged_decode_workspace_bytes(B: int, Hq: int, Hkv: int, max_pages: int, page_size: int, D: int) -> int:
+    return int(lib().thrift_paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D))
+
+
+def thrift_paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                        out_dtype: Optional[torch.dtype] = None, lse: Optional[torch.Tensor] = None, return_lse: bool = False,
+                        workspace: Optional[torch.Tensor] = None):
+    """Attention of q [B,Hq,D] over the first seqlens [B] tokens of each sequence's pages: out, or (out, lse) with return_lse."""
+    _pages(k_pages, v_pages)
+    B, Hq, D = q.shape
+    n_pages, Hkv, page_size, _ = k_pages.shape
+    assert _dev(q).dtype == k_pages.dtype and k_pages.shape[3] == D, (q.dtype, k_pages.dtype, tuple(q.shape), tuple(k_pages.shape))
+    assert block_table.dim() == 2, tuple(block_table.shape)
+    max_pages = block_table.shape[1]
+    _ints((B, max_pages), block_table), _ints((B,), seqlens)
+    if out is None:
+        out = torch.empty(B, Hq, D, dtype=out_dtype or q.dtype, device=q.device)
+    assert tuple(_dev(out).shape) == (B, Hq, D) and out.dtype in _DT, (tuple(out.shape), out.dtype)
+    if lse is None and return_lse:
+        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
+    assert lse is None or tuple(_dev(lse, torch.float32).shape) == (B, Hq)
+    if workspace is None:
+        need = paged_decode_workspace_bytes(B, Hq, Hkv, max_pages, page_size, D)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    _dev(workspace, torch.uint8)
+    _here(q, k_pages, v_pages, block_table, seqlens, out, lse, workspace)
+    _check(lib().thrift_paged_decode(_ptr(q), _DT[q.dtype], _ptr(k_pages), _ptr(v_pages), n_pages, _ptr(block_table), max_pages, _ptr(seqlens),
+                                     B, Hq, Hkv, D, page_size, float(softmax_scale), _ptr(out), _DT[out.dtype], _ptr(lse),
+                                     _ptr(workspace), workspace.numel(), _stream()), "thrift_paged_decode")
+    return (out, lse) if return_lse else out
+
+
+class PageTable:
+    """Block tables, lengths and the stack of free pages of up to B sequences; one serves the caches of all layers."""
+
+    def __init__(self, B: int, max_pages: int, page_size: int, n_pages: int, device):
+        i32 = torch.int32
+        self.B, self.max_pages, self.page_size, self.n_pages = B, max_pages, page_size, n_pages
+        self.block_table = torch.full((B, max_pages), -1, dtype=i32, device=device)
+        self.seqlens = torch.zeros(B, dtype=i32, device=device)
+        self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=i32, device=device)       # page 0 is taken first
+        self.free_count = torch.full((1,), n_pages, dtype=i32, device=device)
+
+    def map(self, new_lens, rows: int) -> PageMap:
+        """Gives new_lens [B] new tokens their places; seqlens and free_count advance (new tensors)."""
+        m = thrift_page_map(self.seqlens, new_lens, self.block_table, self.free_pages, self.free_count, self.page_size, self.n_pages, rows)
+        self.seqlens, self.free_count = m.seqlens, m.free_count
+        return m
+
+    def release(self, drop) -> None:
+        """Ends the sequences with drop [B] != 0: their pages are free again, their lengths 0."""
+        self.seqlens, self.free_count = thrift_page_release(self.seqlens, drop, self.block_table, self.free_pages, self.free_count,
+                                                            self.page_size, self.n_pages)
+
+
+class PagedKVCache:
+    """16-bit pages of one layer; the places of tokens come from a PageTable."""
+
+    def __init__(self, table: PageTable, Hkv: int, D: int, dtype):
+        shape = (table.n_pages, Hkv, table.page_size, D)
+        self.table = table
+        self.k_pages = torch.empty(shape, dtype=dtype, device=table.block_table.device)
+        self.v_pages = torch.empty(shape, dtype=dtype, device=table.block_table.device)
+
+    def append(self, k, v, m: PageMap, q: Optional[torch.Tensor] = None, freqs: Optional[torch.Tensor] = None, layout: str = "half",
+               gain: float = 1.0, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """k, v [T,Hkv,D] of the step's rows into the pages, rotated with q [T,Hq,D] where freqs is given; returns the rotated q."""
+        return thrift_paged_append(k, v, m.slots, self.k_pages, self.v_pages, q, q_out, m.positions, freqs, layout, gain)
+
+    def decode(self, q, softmax_scale: float = 0.0, **kw):
+        """Attention of q [B,Hq,D], the newest token of every sequence (thrift_paged_decode)."""
+        return thrift_paged_decode(q, self.k_pages, self.v_pages, self.table.block_table, self.table.seqlens, softmax_scale, **kw)
 
 
 # ---- Alg. 1 end to end: the user-level form of the paper's signature ----

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libthrift_hip.so")
 CALL = os.path.join(HERE, "_call.so")          # the Python entry of the calls of a serving loop (host code only)
-SOURCES = ["thrift_api.hip", "thrift_prepass.hip", "thrift_prefill.hip", "thrift_prefill_split.hip", "thrift_decode.hip", "thrift_decode_split.hip", "thrift_cache.hip", "thrift_probe.hip"]
+SOURCES = ["thrift_api.hip", "thrift_prepass.hip", "thrift_prefill.hip", "thrift_prefill_split.hip", "thrift_decode.hip", "thrift_decode_split.hip", "thrift_cache.hip", "thrift_rope.hip", "thrift_pages.hip", "thrift_paged_decode.hip", "thrift_probe.hip"]
 DMA_SOURCES = ["thrift_prefill.hip", "thrift_prefill_split.hip", "thrift_decode.hip", "thrift_decode_split.hip"]      # kernels whose inline assembly sets M0 and keeps DMA in flight
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # NaN inputs are outside the contract (include/thrift.h); without this every maximum of matrix-unit results
@@ -20,6 +20,12 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          # packed-FP32 VALU forms are kept out of the generated code on the test machines
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", INCLUDE, "-I", CSRC]
+# rotary positions and the paged cache pass a NaN of their inputs on as plain arithmetic does
+HONOR_NANS = ["thrift_rope.hip", "thrift_pages.hip", "thrift_paged_decode.hip"]
+
+
+def flags(src):
+    return FLAGS + (["-fhonor-nans"] if src in HONOR_NANS else [])
 
 
 def scratch_in_loops(asm_text: str):
@@ -278,7 +284,7 @@ def build(verbose: bool = False, extra=()):
     procs = []
     for src in SOURCES:
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-        cmd = ["hipcc", *FLAGS, *extra, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = ["hipcc", *flags(src), *extra, "-c", os.path.join(CSRC, src), "-o", obj]
         procs.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
         objs.append(obj)
     call_obj = os.path.join(CSRC, "thrift_call.o")
@@ -287,7 +293,7 @@ def build(verbose: bool = False, extra=()):
     listings = []
     for src in DMA_SOURCES:
         listing = os.path.join(CSRC, src.replace(".hip", ".gfx950.s"))
-        lcmd = ["hipcc", *FLAGS, *extra, "-S", "--cuda-device-only", os.path.join(CSRC, src), "-o", listing]
+        lcmd = ["hipcc", *flags(src), *extra, "-S", "--cuda-device-only", os.path.join(CSRC, src), "-o", listing]
         listings.append((src, listing, lcmd, subprocess.Popen(lcmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
     for cmd, p in procs:
         out, _ = p.communicate()

@@ -6,6 +6,7 @@
 #include <mutex>
 
 #include "thrift_launch.h"
+#include "thrift_paged.h"
 
 using namespace thrift;
 
@@ -590,6 +591,166 @@ thrift_status thrift_kv_cache_append(const void* k_new, const void* v_new, thrif
                                      int B, int Hkv, int Nkv, int D, int Bk, void* stream) {
   return thrift_kv_cache_append_advance(k_new, v_new, dt, n_new, seqlens, new_lens, nullptr, k16, v16, k4, ks, v4, vs, kmean,
                                         B, Hkv, Nkv, D, Bk, stream);
+}
+
+// ---- rotary positions and the paged cache ----
+
+static bool rope_ok(int rot, int layout, int D) {
+  return D >= 2 && D <= kRopeMaxDim && D % 2 == 0 && rot >= 2 && rot <= D && rot % 2 == 0 &&
+         (layout == THRIFT_ROPE_HALF || layout == THRIFT_ROPE_INTERLEAVED);
+}
+
+thrift_status thrift_rope_frequencies(int rot, double base, int scaling, double factor, double original, double slow, double fast,
+                                      double* freqs, float* gain) {
+  if (!freqs) return THRIFT_ERR_NULL;
+  if (rot < 2 || rot > kRopeMaxDim || rot % 2 != 0 || !(base > 1.0) || !isfinite(base) || scaling < THRIFT_ROPE_PLAIN || scaling > THRIFT_ROPE_BY_PARTS)
+    return THRIFT_ERR_SHAPE;
+  if (scaling != THRIFT_ROPE_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return THRIFT_ERR_SHAPE;
+  if (scaling == THRIFT_ROPE_NTK) {
+    if (rot < 4) return THRIFT_ERR_SHAPE;
+    base *= pow(factor, (double)rot / (rot - 2));
+    if (!isfinite(base)) return THRIFT_ERR_SHAPE;
+  }
+  if (scaling == THRIFT_ROPE_BY_PARTS &&
+      (!(original > 0.0) || !isfinite(original) || !(slow >= 0.0) || !(fast > slow) || !isfinite(fast)))
+    return THRIFT_ERR_SHAPE;
+  for (int i = 0; i < rot / 2; ++i) {
+    const double theta = pow(base, -2.0 * i / rot);
+    double keep = scaling == THRIFT_ROPE_LINEAR ? 0.0 : 1.0;      // 1: left as it is, 0: interpolated
+    if (scaling == THRIFT_ROPE_BY_PARTS) keep = fmin(1.0, fmax(0.0, (original * theta / (2.0 * M_PI) - slow) / (fast - slow)));
+    freqs[i] = keep == 1.0 ? theta : theta * ((1.0 - keep) / factor + keep);
+  }
+  if (gain) *gain = scaling == THRIFT_ROPE_BY_PARTS ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+  return THRIFT_OK;
+}
+
+static RopeSide rope_side(const void* x, const int64_t* xs, void* y, const int64_t* ys, int heads, int N, int D) {
+  RopeSide r;
+  r.x = (const uint16_t*)x; r.y = (uint16_t*)y; r.heads = x ? heads : 0;
+  const long head = (long)N * D;
+  r.xb = xs ? (long)xs[0] : head * heads; r.xh = xs ? (long)xs[1] : head; r.xn = xs ? (long)xs[2] : D;
+  r.yb = ys ? (long)ys[0] : head * heads; r.yh = ys ? (long)ys[1] : head; r.yn = ys ? (long)ys[2] : D;
+  return r;
+}
+
+static thrift_status rope_impl(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides, int Hq,
+                               const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides, int Hkv, thrift_dtype dt,
+                               const int32_t* positions, int64_t positions_stride, const double* freqs, int rot, int layout, float gain,
+                               int B, int N, int D, float sign, void* stream) {
+  if (!q || !q_out || !freqs || (k == nullptr) != (k_out == nullptr)) return THRIFT_ERR_NULL;
+  if (!is16(dt)) return THRIFT_ERR_DTYPE;
+  if (Hq <= 0 || (k && Hkv <= 0) || !rope_ok(rot, layout, D) || !fits_int(B, N) || !fits_int(Hq, D) || (k && !fits_int(Hkv, D)))
+    return THRIFT_ERR_SHAPE;
+  if (thrift_status s = check_arch()) return s;
+  RopeArgs a;
+  a.side[0] = rope_side(q, q_strides, q_out, q_out_strides, Hq, N, D);
+  a.side[1] = rope_side(k, k_strides, k_out, k_out_strides, Hkv, N, D);
+  a.positions = positions; a.positions_stride = (long)positions_stride; a.freqs = freqs;
+  a.B = B; a.N = N; a.D = D; a.rot = rot; a.layout = layout; a.gain = gain; a.sign = sign;
+  launch_rope(a, dt, (hipStream_t)stream);
+  return after_launch();
+}
+
+thrift_status thrift_rope(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides, int Hq,
+                          const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides, int Hkv, thrift_dtype dt,
+                          const int32_t* positions, int64_t positions_stride, const double* freqs, int rot, int layout, float gain,
+                          int B, int N, int D, void* stream) {
+  return rope_impl(q, q_strides, q_out, q_out_strides, Hq, k, k_strides, k_out, k_out_strides, Hkv, dt, positions, positions_stride, freqs, rot,
+                   layout, gain, B, N, D, 1.f, stream);
+}
+
+thrift_status thrift_rope_backward(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides, int Hq,
+                                   const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides, int Hkv, thrift_dtype dt,
+                                   const int32_t* positions, int64_t positions_stride, const double* freqs, int rot, int layout, float gain,
+                                   int B, int N, int D, void* stream) {
+  return rope_impl(q, q_strides, q_out, q_out_strides, Hq, k, k_strides, k_out, k_out_strides, Hkv, dt, positions, positions_stride, freqs, rot,
+                   layout, gain, B, N, D, -1.f, stream);
+}
+
+static bool page_size_ok(int page_size) { return page_size >= 16 && page_size <= 256 && (page_size & (page_size - 1)) == 0; }
+
+thrift_status thrift_page_map(const int32_t* seqlens, const int32_t* new_lens, int B, int page_size, int n_pages,
+                              int32_t* block_table, int max_pages, const int32_t* free_pages, int free_capacity, const int32_t* free_count,
+                              int rows, int32_t* slots, int32_t* positions, int32_t* starts, int32_t* seqlens_out, int32_t* free_count_out,
+                              void* stream) {
+  if (!seqlens || !new_lens || !block_table || !free_pages || !free_count || !slots || !positions || !starts || !seqlens_out || !free_count_out)
+    return THRIFT_ERR_NULL;
+  if (B <= 0 || B > kMapMaxSeqs || !page_size_ok(page_size) || rows <= 0 || free_capacity <= 0 || !fits_int(n_pages, page_size) ||
+      !fits_int(max_pages, page_size) || (long)max_pages * page_size + rows > 0x7fffffffL || seqlens_out == seqlens || free_count_out == free_count)
+    return THRIFT_ERR_SHAPE;
+  if (thrift_status s = check_arch()) return s;
+  PageMapArgs a;
+  a.seqlens = seqlens; a.new_lens = new_lens; a.table = block_table; a.free_pages = free_pages; a.free_count = free_count;
+  a.slots = slots; a.positions = positions; a.starts = starts; a.seqlens_out = seqlens_out; a.free_count_out = free_count_out;
+  a.B = B; a.page_size = page_size; a.n_pages = n_pages; a.max_pages = max_pages; a.free_capacity = free_capacity; a.rows = rows;
+  launch_page_map(a, (hipStream_t)stream);
+  return after_launch();
+}
+
+thrift_status thrift_page_release(const int32_t* seqlens, const int32_t* drop, int B, int page_size, int n_pages,
+                                  const int32_t* block_table, int max_pages, int32_t* free_pages, int free_capacity, const int32_t* free_count,
+                                  int32_t* seqlens_out, int32_t* free_count_out, void* stream) {
+  if (!seqlens || !drop || !block_table || !free_pages || !free_count || !seqlens_out || !free_count_out) return THRIFT_ERR_NULL;
+  if (B <= 0 || B > kMapMaxSeqs || !page_size_ok(page_size) || free_capacity <= 0 || !fits_int(n_pages, page_size) ||
+      !fits_int(max_pages, page_size) || seqlens_out == seqlens || free_count_out == free_count)
+    return THRIFT_ERR_SHAPE;
+  if (thrift_status s = check_arch()) return s;
+  PageReleaseArgs a;
+  a.seqlens = seqlens; a.drop = drop; a.table = block_table; a.free_pages = free_pages; a.free_count = free_count;
+  a.seqlens_out = seqlens_out; a.free_count_out = free_count_out;
+  a.B = B; a.page_size = page_size; a.n_pages = n_pages; a.max_pages = max_pages; a.free_capacity = free_capacity;
+  launch_page_release(a, (hipStream_t)stream);
+  return after_launch();
+}
+
+thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
+                                  const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,
+                                  const int32_t* positions, const double* freqs, int rot, int layout, float gain,
+                                  void* k_pages, void* v_pages, int n_pages, int page_size, int D, void* stream) {
+  if (!k || !v || !slots || !k_pages || !v_pages || (q && !q_out) || (rot != 0 && (!positions || !freqs))) return THRIFT_ERR_NULL;
+  if (!is16(dt)) return THRIFT_ERR_DTYPE;
+  if (T <= 0 || (q && (Hq <= 0 || !fits_int(Hq, D))) || Hkv <= 0 || !fits_int(Hkv, D) || D < 2 || D > kRopeMaxDim || D % 2 != 0 ||
+      (rot != 0 && !rope_ok(rot, layout, D)) || !page_size_ok(page_size) || !fits_int(n_pages, page_size))
+    return THRIFT_ERR_SHAPE;
+  if (thrift_status s = check_arch()) return s;
+  PagedAppendArgs a;
+  a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.q_out = (uint16_t*)q_out;
+  a.qt = q_strides ? (long)q_strides[0] : (long)Hq * D; a.qh = q_strides ? (long)q_strides[1] : D;
+  a.kt = k_strides ? (long)k_strides[0] : (long)Hkv * D; a.kh = k_strides ? (long)k_strides[1] : D;
+  a.vt = v_strides ? (long)v_strides[0] : (long)Hkv * D; a.vh = v_strides ? (long)v_strides[1] : D;
+  a.slots = slots; a.positions = positions; a.freqs = freqs; a.k_pages = (uint16_t*)k_pages; a.v_pages = (uint16_t*)v_pages;
+  a.T = T; a.Hq = q ? Hq : 0; a.Hkv = Hkv; a.D = D; a.rot = rot; a.layout = layout; a.n_pages = n_pages; a.page_size = page_size; a.gain = gain;
+  launch_paged_append(a, dt, (hipStream_t)stream);
+  return after_launch();
+}
+
+static bool paged_decode_ok(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
+  return B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= 32 && (D == 64 || D == 128 || D == 256) && page_size_ok(page_size) &&
+         fits_int(max_pages, page_size) && fits_int(B, Hq, D);
+}
+
+size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
+  return paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) ? paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D) : 0;
+}
+
+thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,
+                                  const int32_t* block_table, int max_pages, const int32_t* seqlens, int B, int Hq, int Hkv, int D,
+                                  int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !k_pages || !v_pages || !block_table || !seqlens || !out) return THRIFT_ERR_NULL;
+  if (!is16(dt) || !is_out(out_dt)) return THRIFT_ERR_DTYPE;
+  if (!paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) || !fits_int(n_pages, page_size)) return THRIFT_ERR_SHAPE;
+  const size_t need = paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D);
+  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15) != 0)) return THRIFT_ERR_WORKSPACE;
+  if (thrift_status s = check_arch()) return s;
+  PagedDecodeArgs a;
+  a.q = (const uint16_t*)q; a.k_pages = (const uint16_t*)k_pages; a.v_pages = (const uint16_t*)v_pages; a.table = block_table;
+  a.seqlens = seqlens; a.out = out; a.lse = lse; a.workspace = workspace;
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.n_pages = n_pages; a.max_pages = max_pages; a.page_size = page_size;
+  a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D);
+  a.dt = dt; a.out_dt = out_dt;
+  launch_paged_decode(a, (hipStream_t)stream);
+  return after_launch();
 }
 
 thrift_status thrift_peak_probe(int kind, thrift_dtype dt, int iters, void* buffer, size_t bytes, double* work, void* stream) {
