@@ -726,7 +726,7 @@ thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void*
 
 static bool paged_decode_ok(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
   return B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= 32 && (D == 64 || D == 128 || D == 256) && page_size_ok(page_size) &&
-         fits_int(max_pages, page_size) && fits_int(B, Hq, D);
+         fits_int(max_pages, page_size) && fits_int(B, Hq, 256) && fits_int(2L * B, Hkv, ((long)max_pages * page_size + 31) / 32);
 }
 
 size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
