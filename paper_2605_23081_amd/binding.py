@@ -100,7 +100,7 @@ class _General:
     def decode(*_):
         return None
 
-    append = attention = decode
+    append = attention = rope = page_map = paged_append = paged_decode = decode
 
 
 def _native():
@@ -123,6 +123,13 @@ def _raw_stream() -> int:
         return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     except RuntimeError:                                    # no device: no device tensors either, the general path says so
         return 0
+
+
+def _device() -> int:
+    try:
+        return torch._C._cuda_getDevice()
+    except RuntimeError:
+        return -1
 
 
 def _result(r, where: str):
@@ -521,6 +528,9 @@ def _heads(t: torch.Tensor, shape, dtype) -> None:
 
 
 def _rope(name: str, q, k, freqs, positions, layout: str, gain: float, q_out, k_out):
+    r = (_call or _native()).rope(int(name != "thrift_rope"), q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, _device(), _raw_stream())
+    if r is not None:
+        return _result(r, name)
     assert q.dtype in (torch.float16, torch.bfloat16), q.dtype
     B, Hq, N, D = q.shape
     _heads(q, q.shape, q.dtype)
@@ -584,6 +594,9 @@ def _pool(seqlens, block_table, free_pages, free_count) -> Tuple[int, int]:
 
 def thrift_page_map(seqlens, new_lens, block_table, free_pages, free_count, page_size: int, n_pages: int, rows: int) -> PageMap:
     """Pages, block-table entries (written into block_table), slots and positions of new_lens [B] new tokens per sequence."""
+    r = (_call or _native()).page_map(seqlens, new_lens, block_table, free_pages, free_count, page_size, n_pages, rows, _device(), _raw_stream())
+    if r is not None:
+        return PageMap._make(_result(r, "thrift_page_map"))
     B, max_pages = _pool(seqlens, block_table, free_pages, free_count)
     _ints((B,), new_lens)
     _here(seqlens, new_lens, block_table, free_pages, free_count)
@@ -619,6 +632,9 @@ def thrift_paged_append(k, v, slots, k_pages, v_pages, q: Optional[torch.Tensor]
                         gain: float = 1.0) -> Optional[torch.Tensor]:
     """k, v [T,Hkv,D] into the pages [n_pages,Hkv,page_size,D] at slots [T]; with freqs, k and q [T,Hq,D] are rotated to
     positions [T].  Returns q_out (contiguous; rows of skipped tokens are left as they were)."""
+    r = (_call or _native()).paged_append(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs, ROPE_LAYOUTS[layout], gain, _device(), _raw_stream())
+    if r is not None:
+        return None if r is True else _result(r, "thrift_paged_append")
     _pages(k_pages, v_pages)
     T, Hkv, D = k.shape
     n_pages, _, page_size, _ = k_pages.shape
@@ -653,6 +669,11 @@ def thrift_paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale
                         out_dtype: Optional[torch.dtype] = None, lse: Optional[torch.Tensor] = None, return_lse: bool = False,
                         workspace: Optional[torch.Tensor] = None):
     """Attention of q [B,Hq,D] over the first seqlens [B] tokens of each sequence's pages: out, or (out, lse) with return_lse."""
+    if out is not None or out_dtype is None:
+        r = (_call or _native()).paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale, out, lse, int(bool(return_lse)), workspace,
+                                              _device(), _raw_stream())
+        if r is not None:
+            return _result(r, "thrift_paged_decode")
     _pages(k_pages, v_pages)
     B, Hq, D = q.shape
     n_pages, Hkv, page_size, _ = k_pages.shape

@@ -186,6 +186,191 @@ PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return answer(st, out);
 }
 
+// ---- rotary positions and the paged cache; these calls also refuse tensors of another device than the current one ----
+
+// strided heads: the channels of a head contiguous
+bool heads(PyObject* o, int device, const Tensor** t) {
+  if (!THPVariable_Check(o)) return false;
+  *t = &THPVariable_Unpack(o);
+  if (!(*t)->is_cuda() || (*t)->device().index() != device || (*t)->dim() == 0) return false;
+  const auto s = (*t)->sizes();
+  for (const int64_t x : s) if (x < 1 || x > 0x7fffffff) return false;
+  return s.back() == 1 || (*t)->stride(-1) == 1;
+}
+bool plain(PyObject* o, int device, const Tensor** t) { return tensor(o, t) && (*t)->device().index() == device; }
+bool plain_or_none(PyObject* o, int device, const Tensor** t) {
+  if (o == Py_None) { *t = nullptr; return true; }
+  return plain(o, device, t);
+}
+bool like(const Tensor& t, const Tensor& of, at::IntArrayRef shape) { return t.scalar_type() == of.scalar_type() && t.sizes() == shape; }
+// no two elements share an address (sufficient: every stride passes what the smaller ones reach)
+bool apart(const Tensor& t) {
+  int64_t stride[8], size[8];
+  int n = 0;
+  if (t.dim() > 8) return false;
+  for (int64_t d = 0; d < t.dim(); ++d) {
+    if (t.size(d) <= 1) continue;
+    int i = n++;
+    for (; i > 0 && stride[i - 1] > t.stride(d); --i) stride[i] = stride[i - 1], size[i] = size[i - 1];
+    stride[i] = t.stride(d), size[i] = t.size(d);
+  }
+  int64_t reach = 1;
+  for (int i = 0; i < n; ++i) {
+    if (stride[i] < reach) return false;
+    reach += stride[i] * (size[i] - 1);
+  }
+  return true;
+}
+
+// rope(backward, q, k, freqs, positions, layout, gain, q_out, k_out, device, stream): (q_out, k_out)
+PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const Tensor *q, *k = nullptr, *freqs, *positions = nullptr, *qo = nullptr, *ko = nullptr;
+  int backward, layout, device;
+  double gain;
+  void* stream;
+  thrift_dtype dt;
+  if (n != 11 || !integer(a[9], &device) || !integer(a[0], &backward) || !heads(a[1], device, &q) || (a[2] != Py_None && !heads(a[2], device, &k)) ||
+      !plain(a[3], device, &freqs) || (a[4] != Py_None && !heads(a[4], device, &positions)) || !integer(a[5], &layout) || !real(a[6], &gain) ||
+      (a[7] != Py_None && !heads(a[7], device, &qo)) || (a[8] != Py_None && !heads(a[8], device, &ko)) || !stream_of(a[10], &stream) ||
+      !dtype16(*q, &dt) || q->dim() != 4 || freqs->scalar_type() != at::kDouble || freqs->dim() != 1 || freqs->numel() > 0x3fffffff)
+    Py_RETURN_NONE;
+  const int64_t B = q->size(0), N = q->size(2), D = q->size(3);
+  if (k ? (k->dim() != 4 || !like(*k, *q, {B, k->size(1), N, D})) : ko != nullptr) Py_RETURN_NONE;
+  if ((qo && (!like(*qo, *q, q->sizes()) || !apart(*qo))) || (ko && (!like(*ko, *k, k->sizes()) || !apart(*ko)))) Py_RETURN_NONE;
+  if (positions && (positions->scalar_type() != at::kInt || !(positions->sizes() == at::IntArrayRef{N} || positions->sizes() == at::IntArrayRef{B, N})))
+    Py_RETURN_NONE;
+  const int64_t step = positions && positions->dim() == 2 ? positions->stride(0) : 0;
+  const Tensor q_out = qo ? *qo : at::empty(q->sizes(), q->options());
+  const Tensor k_out = !k ? Tensor() : ko ? *ko : at::empty(k->sizes(), k->options());
+  int64_t st[4][3];
+  for (int i = 0; i < 3; ++i) {
+    st[0][i] = q->stride(i), st[1][i] = q_out.stride(i);
+    if (k) st[2][i] = k->stride(i), st[3][i] = k_out.stride(i);
+  }
+  thrift_status r;
+  {
+    const Unlocked unlocked;
+    r = (backward ? thrift_rope_backward : thrift_rope)(
+        ptr(q), st[0], q_out.data_ptr(), st[1], (int)q->size(1), ptr(k), st[2], k ? k_out.data_ptr() : nullptr, st[3], k ? (int)k->size(1) : 0, dt,
+        ptr_as<int32_t>(positions), step, ptr_as<double>(freqs), 2 * (int)freqs->numel(), layout, (float)gain, (int)B, (int)N, (int)D, stream);
+  }
+  if (r != THRIFT_OK) return PyLong_FromLong((long)r);
+  PyObject* both = PyTuple_New(2);
+  if (both == nullptr) return nullptr;
+  PyTuple_SET_ITEM(both, 0, THPVariable_Wrap(q_out));
+  PyTuple_SET_ITEM(both, 1, k ? THPVariable_Wrap(k_out) : (Py_INCREF(Py_None), Py_None));
+  return both;
+}
+
+// page_map(seqlens, new_lens, block_table, free_pages, free_count, page_size, n_pages, rows, device, stream): its five outputs
+PyObject* page_map(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const Tensor *lens, *fresh, *table, *free, *count;
+  int page, n_pages, rows, device;
+  void* stream;
+  if (n != 10 || !integer(a[8], &device) || !plain(a[0], device, &lens) || !plain(a[1], device, &fresh) || !plain(a[2], device, &table) ||
+      !plain(a[3], device, &free) || !plain(a[4], device, &count) || !integer(a[5], &page) || !integer(a[6], &n_pages) || !integer(a[7], &rows) ||
+      !stream_of(a[9], &stream) || table->dim() != 2 || free->dim() != 1 || rows < 1)
+    Py_RETURN_NONE;
+  const int64_t B = table->size(0), width = table->size(1);
+  if (B > 0x7ffffffe || width > 0x7fffffff || free->numel() > 0x7fffffff || table->scalar_type() != at::kInt || free->scalar_type() != at::kInt ||
+      !is(*lens, at::kInt, {B}) || !is(*fresh, at::kInt, {B}) || !is(*count, at::kInt, {1}))
+    Py_RETURN_NONE;
+  Tensor out[5];
+  const int64_t sizes[5] = {rows, rows, B + 1, B, 1};
+  for (int i = 0; i < 5; ++i) out[i] = at::empty({sizes[i]}, lens->options());
+  const auto p = [&](int i) { return out[i].data_ptr<int32_t>(); };
+  thrift_status r;
+  {
+    const Unlocked unlocked;
+    r = thrift_page_map(ptr_as<int32_t>(lens), ptr_as<int32_t>(fresh), (int)B, page, n_pages, ptr_as<int32_t>(table), (int)width,
+                                            ptr_as<int32_t>(free), (int)free->numel(), ptr_as<int32_t>(count), rows, p(0), p(1), p(2), p(3), p(4), stream);
+  }
+  if (r != THRIFT_OK) return PyLong_FromLong((long)r);
+  PyObject* all = PyTuple_New(5);
+  if (all == nullptr) return nullptr;
+  for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(all, i, THPVariable_Wrap(out[i]));
+  return all;
+}
+
+bool pages(PyObject* ko, PyObject* vo, int device, const Tensor** k, const Tensor** v, thrift_dtype* dt) {
+  if (!plain(ko, device, k) || !plain(vo, device, v) || !dtype16(**k, dt) || (*k)->dim() != 4 || !like(**v, **k, (*k)->sizes())) return false;
+  for (const int64_t x : (*k)->sizes()) if (x < 1 || x > 0x7fffffff) return false;
+  return true;
+}
+
+// paged_append(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs, layout, gain, device, stream): q_out, or True without q
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const Tensor *k, *v, *slots, *kp, *vp, *q = nullptr, *qo, *positions, *freqs;
+  int layout, device;
+  double gain;
+  void* stream;
+  thrift_dtype dt;
+  if (n != 13 || !integer(a[11], &device) || !heads(a[0], device, &k) || !heads(a[1], device, &v) || !plain(a[2], device, &slots) ||
+      !pages(a[3], a[4], device, &kp, &vp, &dt) || (a[5] != Py_None && !heads(a[5], device, &q)) || !plain_or_none(a[6], device, &qo) ||
+      !plain_or_none(a[7], device, &positions) || !plain_or_none(a[8], device, &freqs) || !integer(a[9], &layout) || !real(a[10], &gain) ||
+      !stream_of(a[12], &stream) || k->dim() != 3 || (qo && !q))
+    Py_RETURN_NONE;
+  const int64_t T = k->size(0), Hkv = kp->size(1), D = kp->size(3);
+  if (!like(*k, *kp, {T, Hkv, D}) || !like(*v, *kp, {T, Hkv, D}) || !is(*slots, at::kInt, {T}) ||
+      (q && (q->dim() != 3 || !like(*q, *kp, {T, q->size(1), D}))) || (qo && !like(*qo, *q, q->sizes())))
+    Py_RETURN_NONE;
+  if (freqs && (freqs->scalar_type() != at::kDouble || freqs->dim() != 1 || freqs->numel() < 1 || freqs->numel() > 0x3fffffff || !positions ||
+                !is(*positions, at::kInt, {T})))
+    Py_RETURN_NONE;
+  const Tensor q_out = !q ? Tensor() : qo ? *qo : at::empty(q->sizes(), q->options());
+  int64_t st[3][2];
+  for (int i = 0; i < 2; ++i) {
+    st[0][i] = q ? q->stride(i) : 0, st[1][i] = k->stride(i), st[2][i] = v->stride(i);
+  }
+  thrift_status r;
+  {
+    const Unlocked unlocked;
+    r = thrift_paged_append(ptr(q), st[0], q ? q_out.data_ptr() : nullptr, q ? (int)q->size(1) : 0, ptr(k), st[1], ptr(v), st[2], (int)Hkv,
+                                                dt, (int)T, ptr_as<int32_t>(slots), ptr_as<int32_t>(positions), ptr_as<double>(freqs),
+                                                freqs ? 2 * (int)freqs->numel() : 0, layout, (float)gain, ptr(kp), ptr(vp), (int)kp->size(0),
+                                                (int)kp->size(2), (int)D, stream);
+  }
+  if (r != THRIFT_OK) return PyLong_FromLong((long)r);
+  if (!q) Py_RETURN_TRUE;
+  return THPVariable_Wrap(q_out);
+}
+
+// paged_decode(q, k_pages, v_pages, block_table, seqlens, scale, out, lse, return_lse, workspace, device, stream): out, or (out, lse)
+PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const Tensor *q, *kp, *vp, *table, *lens, *out_given, *lse_given, *ws_given;
+  int return_lse, device;
+  double scale;
+  void* stream;
+  thrift_dtype dt, odt;
+  if (n != 12 || !integer(a[10], &device) || !plain(a[0], device, &q) || !pages(a[1], a[2], device, &kp, &vp, &dt) || !plain(a[3], device, &table) ||
+      !plain(a[4], device, &lens) || !real(a[5], &scale) || !plain_or_none(a[6], device, &out_given) || !plain_or_none(a[7], device, &lse_given) ||
+      !integer(a[8], &return_lse) || !plain_or_none(a[9], device, &ws_given) || !stream_of(a[11], &stream) || q->dim() != 3 || table->dim() != 2)
+    Py_RETURN_NONE;
+  const int64_t B = q->size(0), Hq = q->size(1), D = q->size(2), width = table->size(1);
+  if (B > 0x7fffffff || Hq > 0x7fffffff || width > 0x7fffffff || !like(*q, *kp, {B, Hq, kp->size(3)}) || !is(*table, at::kInt, {B, width}) ||
+      !is(*lens, at::kInt, {B}) || (out_given && out_given->sizes() != q->sizes()) || (lse_given && !is(*lse_given, at::kFloat, {B, Hq})) ||
+      (ws_given && ws_given->scalar_type() != at::kByte))
+    Py_RETURN_NONE;
+  const Tensor out = out_given ? *out_given : at::empty({B, Hq, D}, q->options());
+  if (!dtype_out(out, &odt)) Py_RETURN_NONE;
+  const Tensor lse = lse_given ? *lse_given : return_lse ? at::empty({B, Hq}, q->options().dtype(at::kFloat)) : Tensor();
+  const int Hkv = (int)kp->size(1), page = (int)kp->size(2);
+  const Tensor ws = ws_given ? *ws_given : bytes_like(*q, thrift_paged_decode_workspace((int)B, (int)Hq, Hkv, (int)width, page, (int)D));
+  thrift_status r;
+  {
+    const Unlocked unlocked;
+    r = thrift_paged_decode(ptr(q), dt, ptr(kp), ptr(vp), (int)kp->size(0), ptr_as<int32_t>(table), (int)width, ptr_as<int32_t>(lens),
+                                                (int)B, (int)Hq, Hkv, (int)D, page, (float)scale, out.data_ptr(), odt,
+                                                lse.defined() ? lse.data_ptr<float>() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream);
+  }
+  if (r != THRIFT_OK || !return_lse) return answer(r, out);
+  PyObject* both = PyTuple_New(2);
+  if (both == nullptr) return nullptr;
+  PyTuple_SET_ITEM(both, 0, THPVariable_Wrap(out));
+  PyTuple_SET_ITEM(both, 1, THPVariable_Wrap(lse));
+  return both;
+}
+
 // A tensor whose sizes or storage cannot be asked for (a fake one, one under a transform) throws: not a plain argument.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -201,6 +386,10 @@ PyMethodDef methods[] = {
     {"decode", (PyCFunction)(void (*)(void))guarded<decode>, METH_FASTCALL, nullptr},
     {"append", (PyCFunction)(void (*)(void))guarded<append>, METH_FASTCALL, nullptr},
     {"attention", (PyCFunction)(void (*)(void))guarded<attention>, METH_FASTCALL, nullptr},
+    {"rope", (PyCFunction)(void (*)(void))guarded<rope>, METH_FASTCALL, nullptr},
+    {"page_map", (PyCFunction)(void (*)(void))guarded<page_map>, METH_FASTCALL, nullptr},
+    {"paged_append", (PyCFunction)(void (*)(void))guarded<paged_append>, METH_FASTCALL, nullptr},
+    {"paged_decode", (PyCFunction)(void (*)(void))guarded<paged_decode>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -409,3 +409,57 @@ def test_a_servers_steps(T, dtype, layout):
         for b in range(B):
             if drop[b]:
                 past[b] = None
+
+
+def test_the_general_path_gives_the_same_results(T, monkeypatch):
+    """Without the module _call, and for what it does not serve, the calls go through ctypes."""
+    q, k = _randn(2, 4, 9, 128, dtype=torch.float16), _randn(2, 2, 9, 128, dtype=torch.float16, seed=1)
+    freqs, gain = T.rope_frequencies(64, 1e4, "by_parts", 2.0, 512, device="cuda")
+    rows = k.transpose(1, 2).reshape(18, 2, 128)
+    lens = _ints([0, 40])
+
+    def results():
+        table = T.PageTable(2, 8, 16, 16, "cuda")
+        cache = T.PagedKVCache(table, 2, 128, torch.float16)
+        m = table.map(_ints([9, 9]), 20)
+        rest = torch.zeros(2, 2, 128, dtype=torch.float16, device="cuda")
+        x = torch.cat([rows, rest])
+        kq = cache.append(x, x, m, x, freqs, "interleaved", gain, q_out=torch.zeros(20, 2, 128, dtype=torch.float16, device="cuda"))
+        assert cache.append(x, x, m, None, freqs, "half", gain) is None
+        out, lse = cache.decode(q[:, :, 0].contiguous(), return_lse=True)
+        own = torch.empty(2, 4, dtype=torch.float32, device="cuda")
+        again = cache.decode(q[:, :, 0].contiguous(), out=torch.empty(2, 4, 128, dtype=torch.float32, device="cuda"), lse=own)
+        into = torch.empty(2, 9, 4, 128, dtype=torch.float16, device="cuda").transpose(1, 2)
+        return [*T.thrift_rope(q, k, freqs, None, "half", gain), *T.thrift_rope_backward(q, k, freqs, lens[:1].expand(9).contiguous(), "interleaved", gain, q_out=into),
+                T.thrift_rope(q, None, freqs)[0], *m, kq, out, lse, again, own, table.seqlens, table.free_count]
+
+    want = results()
+    monkeypatch.setattr(T, "_call", T._General)
+    for i, (a, b) in enumerate(zip(results(), want)):
+        assert torch.equal(a, b), i
+    with pytest.raises(AssertionError):
+        T.thrift_rope(q, k.float(), freqs)
+
+
+def test_the_module_leaves_other_arguments_to_the_general_path(T):
+    m = T._native()
+    q = torch.zeros(1, 2, 3, 128, dtype=torch.float16, device="cuda")
+    freqs = torch.zeros(64, dtype=torch.float64, device="cuda")
+    one = lambda **kw: m.rope(*{**dict(backward=0, q=q, k=None, freqs=freqs, positions=None, layout=0, gain=1.0, qo=None, ko=None, device=0, stream=0), **kw}.values())
+    assert isinstance(one(), tuple)
+    for bad in (dict(device=1), dict(q=q.float()), dict(q=q.cpu()), dict(q=q[0]), dict(k=q[:, :, :2]), dict(freqs=freqs.float()), dict(positions=torch.zeros(2, dtype=I32, device="cuda")),
+                dict(qo=q[:, :1].expand(1, 2, 3, 128)), dict(qo=q.bfloat16()), dict(ko=q), dict(q=q.transpose(2, 3)), dict(layout="half"), dict(q=q[:0])):
+        assert one(**bad) is None, bad
+    assert one(layout=5) == 2 and one(freqs=torch.zeros(65, dtype=torch.float64, device="cuda")) == 2
+    pages = torch.zeros(4, 2, 16, 128, dtype=torch.float16, device="cuda")
+    k, slots, table, lens = torch.zeros(3, 2, 128, dtype=torch.float16, device="cuda"), _ints([0, 1, 2]), _ints([[0], [1], [2]]), _ints([1, 1, 1])
+    assert m.paged_append(k, k, slots, pages, pages, None, None, None, None, 0, 1.0, 0, 0) is True
+    assert m.paged_append(k, k, slots, pages, pages, None, None, None, None, 0, 1.0, 1, 0) is None
+    assert m.paged_append(k, k, slots, pages, pages[:, :1], None, None, None, None, 0, 1.0, 0, 0) is None
+    assert m.paged_append(k, k, slots.long(), pages, pages, None, None, None, None, 0, 1.0, 0, 0) is None
+    assert m.paged_append(k, k, slots, pages, pages, None, None, None, freqs, 0, 1.0, 0, 0) is None
+    assert m.paged_decode(k, pages, pages, table, lens, 0.0, None, None, 0, None, 1, 0) is None
+    assert m.paged_decode(k, pages, pages, table[:2], lens, 0.0, None, None, 0, None, 0, 0) is None
+    assert m.paged_decode(k, pages, pages, table, lens, 0.0, None, None, 0, torch.empty(16, dtype=torch.uint8, device="cuda"), 0, 0) == 5
+    assert m.page_map(lens, lens, table, slots, lens[:1], 16, 4, 3, 1, 0) is None and m.page_map(lens, lens, table, slots, lens, 16, 4, 3, 0, 0) is None
+    assert m.page_map(lens, lens, table, slots, lens[:1], 17, 4, 3, 0, 0) == 2 and len(m.page_map(lens, lens, table, slots, lens[:1], 16, 4, 3, 0, 0)) == 5

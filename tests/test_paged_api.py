@@ -154,3 +154,27 @@ def test_elements_that_coincide_are_seen():
     x = torch.zeros(4, 6, 8)
     assert T._apart(x) and T._apart(x.transpose(0, 2)) and T._apart(x[:, ::2]) and T._apart(x[:1].expand(1, 6, 8)) and T._apart(torch.zeros(5, 1, 3))
     assert not T._apart(x[:1].expand(4, 6, 8)) and not T._apart(x.as_strided((4, 8), (4, 1))) and T._apart(x.as_strided((4, 8), (8, 1)))
+
+
+def test_tensors_without_storage_are_left_to_the_general_path():
+    """Under a transform a tensor has sizes but no data pointer; refusing it must not end the process."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    m = T._native()
+    h, i32 = torch.float16, torch.int32
+    with FakeTensorMode():
+        z = lambda *s, dt=h: torch.zeros(*s, dtype=dt, device="cuda")
+        q, freqs, k, pages = z(1, 2, 3, 128), z(64, dt=torch.float64), z(3, 2, 128), z(4, 2, 16, 128)
+        ints, table, ws = z(3, dt=i32), z(3, 1, dt=i32), z(1 << 20, dt=torch.uint8)
+        out, lse = z(3, 2, 128), z(3, 2, dt=torch.float32)
+    seen = []
+
+    def served(q, k):
+        seen.append(m.rope(0, q, None, freqs, None, 0, 1.0, q, None, 0, 0))
+        seen.append(m.page_map(ints, ints, table, ints, ints[:1], 16, 4, 3, 0, 0))
+        seen.append(m.paged_append(k, k, ints, pages, pages, None, None, None, None, 0, 1.0, 0, 0))
+        seen.append(m.paged_decode(k, pages, pages, table, ints, 0.0, out, lse, 1, ws, 0, 0))
+        return q
+
+    torch.vmap(served)(q.unsqueeze(0), k.unsqueeze(0))
+    assert seen == [None] * 4
+    assert m.rope() is None and m.page_map() is None and m.paged_append() is None and m.paged_decode() is None
