@@ -404,8 +404,8 @@ thrift_status thrift_rope_frequencies(int rot, double base, int scaling, double 
  *     Any strides of an input are allowed (0 repeats it); the elements of an output must not coincide.  q_out may be q with the
  *     same strides (in place), k_out likewise k; apart from that outputs overlap nothing.
  *   positions (nullable) int32: token (b, n) is at positions[b * positions_stride + n]; NULL: n
- *   freqs (device) [rot/2] fp64; rot even, 2 .. D; D <= 1024; layout: thrift_rope_layout
- * Every size runs; 16-byte accesses are used where addresses and strides allow them (D, rot/2 resp. rot multiples of 8).
+ *   freqs (device) [rot/2] fp64; rot even, 2 .. D; D even, <= 1024; B * N below 2^23; layout: thrift_rope_layout
+ * 16-byte accesses are used where D, rot, addresses and strides are multiples of 16, 16, 16 bytes and 8 elements.
  */
 thrift_status thrift_rope(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides, int Hq,
                           const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides, int Hkv, thrift_dtype dt,
@@ -461,7 +461,7 @@ thrift_status thrift_page_release(const int32_t* seqlens, const int32_t* drop, i
  *     nowhere and its q_out row is left as it was.  No slot may occur twice.
  *   positions [T], freqs, rot, layout, gain as thrift_rope; rot == 0: nothing is rotated (positions and freqs unused, q copied)
  *   k_pages, v_pages [n_pages,Hkv,page_size,D] 16-bit (dt)
- * D even, <= 1024.
+ * D even, <= 1024; T below 2^23.
  */
 thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
                                   const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,

@@ -639,7 +639,7 @@ static thrift_status rope_impl(const void* q, const int64_t* q_strides, void* q_
                                int B, int N, int D, float sign, void* stream) {
   if (!q || !q_out || !freqs || (k == nullptr) != (k_out == nullptr)) return THRIFT_ERR_NULL;
   if (!is16(dt)) return THRIFT_ERR_DTYPE;
-  if (Hq <= 0 || (k && Hkv <= 0) || !rope_ok(rot, layout, D) || !fits_int(B, N) || !fits_int(Hq, D) || (k && !fits_int(Hkv, D)))
+  if (Hq <= 0 || (k && Hkv <= 0) || !rope_ok(rot, layout, D) || !fits_int(B, N, 256) || !fits_int(Hq, D) || (k && !fits_int(Hkv, D)))
     return THRIFT_ERR_SHAPE;
   if (thrift_status s = check_arch()) return s;
   RopeArgs a;
@@ -709,7 +709,7 @@ thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void*
                                   void* k_pages, void* v_pages, int n_pages, int page_size, int D, void* stream) {
   if (!k || !v || !slots || !k_pages || !v_pages || (q && !q_out) || (rot != 0 && (!positions || !freqs))) return THRIFT_ERR_NULL;
   if (!is16(dt)) return THRIFT_ERR_DTYPE;
-  if (T <= 0 || (q && (Hq <= 0 || !fits_int(Hq, D))) || Hkv <= 0 || !fits_int(Hkv, D) || D < 2 || D > kRopeMaxDim || D % 2 != 0 ||
+  if (!fits_int(T, 256) || (q && (Hq <= 0 || !fits_int(Hq, D))) || Hkv <= 0 || !fits_int(Hkv, D) || D < 2 || D > kRopeMaxDim || D % 2 != 0 ||
       (rot != 0 && !rope_ok(rot, layout, D)) || !page_size_ok(page_size) || !fits_int(n_pages, page_size))
     return THRIFT_ERR_SHAPE;
   if (thrift_status s = check_arch()) return s;

@@ -162,19 +162,20 @@ __global__ void __launch_bounds__(kAppendRowThreads) paged_append_kernel(PagedAp
   for (int i = threadIdx.x; i < half + (a.D - a.rot); i += kAppendRowThreads) {
     float c = 1.f, s = 0.f;
     if (i < half) turn(position, a.freqs[i], a.gain, c, s);
-    auto rotate = [&](const uint16_t* x, uint16_t* y) {
+    auto turn_head = [&](const uint16_t* x, uint16_t* y) {
       if (i >= half) {
         y[half + i] = x[half + i];
         return;
       }
       const int i0 = a.layout == THRIFT_ROPE_HALF ? i : 2 * i, i1 = a.layout == THRIFT_ROPE_HALF ? i + half : 2 * i + 1;
-      const float x0 = T::to_float(x[i0]), x1 = T::to_float(x[i1]);
-      y[i0] = T::from_float(x0 * c - x1 * s);
-      y[i1] = T::from_float(x1 * c + x0 * s);
+      float y0, y1;
+      rotate(T::to_float(x[i0]), T::to_float(x[i1]), c, s, y0, y1);
+      y[i0] = T::from_float(y0);
+      y[i1] = T::from_float(y1);
     };
     if (a.q != nullptr)
-      for (int h = 0; h < a.Hq; ++h) rotate(a.q + t * a.qt + h * a.qh, a.q_out + ((size_t)t * a.Hq + h) * a.D);
-    for (int h = 0; h < a.Hkv; ++h) rotate(a.k + t * a.kt + h * a.kh, a.k_pages + to + h * head);
+      for (int h = 0; h < a.Hq; ++h) turn_head(a.q + t * a.qt + h * a.qh, a.q_out + ((size_t)t * a.Hq + h) * a.D);
+    for (int h = 0; h < a.Hkv; ++h) turn_head(a.k + t * a.kt + h * a.kh, a.k_pages + to + h * head);
   }
   for (int h = 0; h < a.Hkv; ++h)
     for (int i = threadIdx.x; i < a.D; i += kAppendRowThreads) a.v_pages[to + h * head + i] = a.v[t * a.vt + h * a.vh + i];

@@ -29,20 +29,86 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs a) {
           continue;
         }
         const int i0 = a.layout == THRIFT_ROPE_HALF ? i : 2 * i, i1 = a.layout == THRIFT_ROPE_HALF ? i + half : 2 * i + 1;
-        const float x0 = T::to_float(x[i0]), x1 = T::to_float(x[i1]);
-        y[i0] = T::from_float(x0 * c - x1 * s);
-        y[i1] = T::from_float(x1 * c + x0 * s);
+        float y0, y1;
+        rotate(T::to_float(x[i0]), T::to_float(x[i1]), c, s, y0, y1);
+        y[i0] = T::from_float(y0);
+        y[i1] = T::from_float(y1);
       }
     }
   }
 }
 
+template <typename T, int LAYOUT>
+__global__ void __launch_bounds__(kHeadThreads) rope_items_kernel(RopeArgs a, HeadShape z) {
+  __shared__ float2 table[kAngles];
+  const int tid = threadIdx.x, half = a.rot / 2, all = a.B * a.N;
+  const int first = (int)(blockIdx.x / z.splits) * z.tokens, split = blockIdx.x % z.splits;
+  const int item = tid % z.items, rest = tid / z.items, local = rest % z.tokens, group = rest / z.tokens;
+  const int token = first + local, heads = a.side[0].heads + a.side[1].heads;
+  const bool busy = group < z.lanes && token < all;
+  const int b = token / a.N, n = token - b * a.N;
+  const Item<LAYOUT> it(item, a.D, a.rot);
+  const uint16_t* x[2];
+  uint16_t* y[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    x[s] = a.side[s].x + b * a.side[s].xb + n * a.side[s].xn;
+    y[s] = a.side[s].y + b * a.side[s].yb + n * a.side[s].yn;
+  }
+  const int step = z.lanes * z.splits;
+  int h = busy ? split * z.lanes + group : heads;
+  auto load = [&](int head, v4i (&c)[2]) {
+    const int s = head >= a.side[0].heads, i = head - (s ? a.side[0].heads : 0);
+    const uint16_t* p = x[s] + i * a.side[s].xh;
+    c[0] = *reinterpret_cast<const v4i*>(p + it.at[0]), c[1] = *reinterpret_cast<const v4i*>(p + it.at[1]);
+  };
+  v4i c[2];
+  if (h < heads) load(h, c);                 // on its way while the angles are formed
+  for (int i = tid; i < z.tokens * half; i += kHeadThreads) {
+    const int t = first + i / half, pair = i % half;
+    if (t >= all) break;
+    const int tb = t / a.N, tn = t - tb * a.N;
+    float cs, sn;
+    turn(a.positions ? a.positions[tb * a.positions_stride + tn] : tn, a.freqs[pair], a.gain, cs, sn);
+    table[i] = make_float2(cs, a.sign * sn);
+  }
+  __syncthreads();
+  float2 cs[8];
+  if (busy) it.angles(table + local * half, cs);
+  while (h < heads) {
+    const int s = h >= a.side[0].heads, i = h - (s ? a.side[0].heads : 0);
+    uint16_t* p = y[s] + i * a.side[s].yh;
+    h += step;
+    v4i next[2];
+    if (h < heads) load(h, next);
+    turn_item<T, LAYOUT>(it, c, cs);
+    *reinterpret_cast<v4i*>(p + it.at[0]) = c[0], *reinterpret_cast<v4i*>(p + it.at[1]) = c[1];
+    c[0] = next[0], c[1] = next[1];
+  }
+}
+
+bool in_chunks(const RopeSide& s) {
+  return s.heads == 0 || (((uintptr_t)s.x | (uintptr_t)s.y) % 16 == 0 && (s.xb | s.xh | s.xn | s.yb | s.yh | s.yn) % 8 == 0);
+}
+
+template <typename T>
+void launch(const RopeArgs& a, hipStream_t st) {
+  const long tokens = (long)a.B * a.N;
+  if (a.D % 16 != 0 || a.rot % 16 != 0 || !in_chunks(a.side[0]) || !in_chunks(a.side[1])) {
+    rope_kernel<T><<<dim3((unsigned)tokens), dim3(kRopeThreads), 0, st>>>(a);
+    return;
+  }
+  const HeadShape z = head_shape(tokens, a.side[0].heads + a.side[1].heads, a.D, a.rot);
+  const dim3 grid((unsigned)((tokens + z.tokens - 1) / z.tokens * z.splits)), block(kHeadThreads);
+  if (a.layout == THRIFT_ROPE_HALF) rope_items_kernel<T, THRIFT_ROPE_HALF><<<grid, block, 0, st>>>(a, z);
+  else rope_items_kernel<T, THRIFT_ROPE_INTERLEAVED><<<grid, block, 0, st>>>(a, z);
+}
+
 }  // namespace
 
 void launch_rope(const RopeArgs& a, thrift_dtype dt, hipStream_t st) {
-  const unsigned grid = (unsigned)((long)a.B * a.N);
-  if (dt == THRIFT_F16) rope_kernel<F16><<<dim3(grid), dim3(kRopeThreads), 0, st>>>(a);
-  else rope_kernel<BF16><<<dim3(grid), dim3(kRopeThreads), 0, st>>>(a);
+  if (dt == THRIFT_F16) launch<F16>(a, st);
+  else launch<BF16>(a, st);
 }
 
 }  // namespace thrift

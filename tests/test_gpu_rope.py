@@ -36,7 +36,8 @@ def _check(T, q, k, freqs, positions, layout, gain, got, sign=1.0):
 
 # sizes on both sides of the 16-byte accesses: heads of 2 to 256 channels, parts of them, one token to some hundreds
 SIZES = [(1, 1, 1, 1, 128, 128), (3, 1, 32, 8, 128, 128), (2, 7, 4, 2, 128, 64), (1, 130, 8, 8, 64, 64), (2, 33, 6, 3, 256, 256), (1, 19, 5, 1, 96, 48),
-         (1, 5, 2, 2, 128, 6), (2, 9, 3, 1, 80, 80), (1, 3, 2, 1, 2, 2), (1, 4, 3, 2, 30, 14), (1, 257, 40, 8, 128, 128), (5, 1, 3, 2, 1024, 1024), (1, 2, 64, 8, 128, 32)]
+         (1, 5, 2, 2, 128, 6), (2, 9, 3, 1, 80, 80), (1, 3, 2, 1, 2, 2), (1, 4, 3, 2, 30, 14), (1, 257, 40, 8, 128, 128), (5, 1, 3, 2, 1024, 1024), (1, 2, 64, 8, 128, 32),
+         (1, 5003, 2, 1, 128, 128), (3, 1501, 2, 1, 64, 32), (1, 9001, 1, 1, 48, 16), (2, 1050, 3, 2, 256, 256), (1, 1100, 9, 4, 16, 16), (1, 700, 40, 8, 512, 256)]
 
 
 @pytest.mark.parametrize("B,N,Hq,Hkv,D,rot", SIZES)
