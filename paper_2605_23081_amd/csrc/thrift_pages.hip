@@ -181,6 +181,65 @@ __global__ void __launch_bounds__(kAppendRowThreads) paged_append_kernel(PagedAp
     for (int i = threadIdx.x; i < a.D; i += kAppendRowThreads) a.v_pages[to + h * head + i] = a.v[t * a.vt + h * a.vh + i];
 }
 
+// The same in 16-byte chunks (thrift_rotary.h): the query heads of a row, then its key heads, then its value heads, which are copied.
+template <typename T, int LAYOUT>
+__global__ void __launch_bounds__(kHeadThreads) paged_append_items_kernel(PagedAppendArgs a, HeadShape z) {
+  __shared__ float2 table[kAngles];
+  const int tid = threadIdx.x, half = a.rot / 2;
+  const int first = (int)(blockIdx.x / z.splits) * z.tokens, split = blockIdx.x % z.splits;
+  const int item = tid % z.items, rest = tid / z.items, local = rest % z.tokens, group = rest / z.tokens;
+  const int t = first + local, turned = a.Hq + a.Hkv, heads = turned + a.Hkv;
+  const int slot = group < z.lanes && t < a.T ? a.slots[t] : -1;
+  const bool busy = slot >= 0 && slot < a.n_pages * a.page_size;
+  const Item<LAYOUT> it(item, a.D, a.rot);
+  const uint16_t *q = a.q + t * a.qt, *k = a.k + t * a.kt, *v = a.v + t * a.vt;
+  const int shift = 31 - __builtin_clz(a.page_size);
+  const size_t head = (size_t)a.D << shift;                         // elements of a head in a page
+  const size_t to = (size_t)(slot >> shift) * a.Hkv * head + (size_t)(slot & (a.page_size - 1)) * a.D;
+  uint16_t* q_out = a.q_out + (size_t)t * a.Hq * a.D;
+  const int step = z.lanes * z.splits;
+  int h = busy ? split * z.lanes + group : heads;
+  auto load = [&](int i, v4i (&c)[2]) {
+    const uint16_t* p = i < a.Hq ? q + i * a.qh : i < turned ? k + (i - a.Hq) * a.kh : v + (i - turned) * a.vh;
+    c[0] = *reinterpret_cast<const v4i*>(p + it.at[0]), c[1] = *reinterpret_cast<const v4i*>(p + it.at[1]);
+  };
+  v4i c[2];
+  if (h < heads) load(h, c);                 // on its way while the angles are formed
+  for (int i = tid; i < z.tokens * half; i += kHeadThreads) {
+    const int row = first + i / half;
+    if (row >= a.T) break;
+    float cs, sn;
+    turn(a.positions[row], a.freqs[i % half], a.gain, cs, sn);
+    table[i] = make_float2(cs, sn);
+  }
+  __syncthreads();
+  float2 cs[8];
+  if (busy) it.angles(table + local * half, cs);
+  while (h < heads) {
+    uint16_t* p = h < a.Hq ? q_out + (size_t)h * a.D : h < turned ? a.k_pages + to + (h - a.Hq) * head : a.v_pages + to + (h - turned) * head;
+    const bool value = h >= turned;
+    h += step;
+    v4i next[2];
+    if (h < heads) load(h, next);
+    if (!value) turn_item<T, LAYOUT>(it, c, cs);
+    *reinterpret_cast<v4i*>(p + it.at[0]) = c[0], *reinterpret_cast<v4i*>(p + it.at[1]) = c[1];
+    c[0] = next[0], c[1] = next[1];
+  }
+}
+
+template <typename T>
+void launch_append(const PagedAppendArgs& a, hipStream_t st) {
+  const uintptr_t at = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.k_pages | (uintptr_t)a.v_pages;
+  if (a.D % 16 != 0 || a.rot % 16 != 0 || at % 16 != 0 || ((a.q ? a.qt | a.qh : 0) | a.kt | a.kh | a.vt | a.vh) % 8 != 0) {
+    paged_append_kernel<T><<<dim3((unsigned)a.T), dim3(kAppendRowThreads), 0, st>>>(a);
+    return;
+  }
+  const HeadShape z = head_shape(a.T, a.Hq + 2 * a.Hkv, a.D, a.rot);
+  const dim3 grid((unsigned)((a.T + z.tokens - 1) / z.tokens * z.splits)), block(kHeadThreads);
+  if (a.layout == THRIFT_ROPE_HALF) paged_append_items_kernel<T, THRIFT_ROPE_HALF><<<grid, block, 0, st>>>(a, z);
+  else paged_append_items_kernel<T, THRIFT_ROPE_INTERLEAVED><<<grid, block, 0, st>>>(a, z);
+}
+
 }  // namespace
 
 void launch_page_map(const PageMapArgs& a, hipStream_t st) {
@@ -194,8 +253,8 @@ void launch_page_release(const PageReleaseArgs& a, hipStream_t st) {
 }
 
 void launch_paged_append(const PagedAppendArgs& a, thrift_dtype dt, hipStream_t st) {
-  if (dt == THRIFT_F16) paged_append_kernel<F16><<<dim3((unsigned)a.T), dim3(kAppendRowThreads), 0, st>>>(a);
-  else paged_append_kernel<BF16><<<dim3((unsigned)a.T), dim3(kAppendRowThreads), 0, st>>>(a);
+  if (dt == THRIFT_F16) launch_append<F16>(a, st);
+  else launch_append<BF16>(a, st);
 }
 
 }  // namespace thrift

@@ -148,7 +148,7 @@ def test_map_and_release_keep_the_pool_whole(T):
 # ---- appends ----
 
 @pytest.mark.parametrize("T_,Hq,Hkv,D,rot,page", [(1, 32, 8, 128, 128, 16), (37, 6, 2, 128, 64, 32), (5, 3, 3, 64, 64, 256), (130, 8, 1, 256, 256, 64), (9, 2, 1, 96, 40, 16),
-                                                  (70, 4, 4, 128, 0, 16), (3, 2, 2, 30, 14, 16), (300, 64, 8, 128, 128, 64), (2, 1, 1, 2, 2, 16), (4, 2, 1, 1024, 512, 16)])
+                                                  (70, 4, 4, 128, 0, 16), (3, 2, 2, 30, 14, 16), (300, 64, 8, 128, 128, 64), (5003, 2, 1, 128, 64, 16), (1100, 3, 1, 64, 64, 32), (2100, 1, 2, 48, 16, 16), (2, 1, 1, 2, 2, 16), (4, 2, 1, 1024, 512, 16)])
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_append_against_64_bits(T, T_, Hq, Hkv, D, rot, page, layout, dtype):
