@@ -7,14 +7,15 @@
 //   O^T += V^T P^T channels x heads.  A lane reads the channels D/16 c .. of the rows of its eight keys and pairs the rows' halves
 //                  up (one byte permute per two elements); matrix tile j holds channel j of every lane.  The eight keys are those whose
 //                  scores the lane holds, so that P goes from S to the next product without leaving the lane.
-// No tile passes through LDS and nothing waits for a barrier inside the walk.  P is split into two 16-bit pieces, high and low,
-// for two products: rounding it once would cost an output of 16 bits as much accuracy again as the output's own rounding.
-// P is scaled by 2^15, so that an fp16 piece is a normal number down to 2^-29 of the largest.
+// No tile passes through LDS.  P is split into two 16-bit pieces, high and low, for two products: rounding it once would cost an
+// output of 16 bits as much accuracy again as the output's own rounding.  P is scaled by 2^15, so that an fp16 piece is a normal
+// number down to 2^-29 of the largest.
 //
 // The steps of all rows are counted through on the GPU from the lengths and cut into equal shares, one per workgroup, whatever the
-// lengths are.  In a workgroup the steps of a row go to the four wavefronts in turn; their states are joined in LDS when the row
-// or the share ends.  A row inside one share is written by its workgroup; otherwise each share leaves a partial, and a second launch
-// joins a row's partials in the order of the shares.
+// lengths are; a wavefront walks a quarter of it.  It asks for the keys of its next step as soon as the scores of this one are
+// formed, and for its values as soon as this one's are added, also where the next step is in another row; wavefronts wait for each
+// other only at the end, where parts of one row that neighbours hold are joined through LDS.  A row inside one share is written by
+// its workgroup; otherwise each share leaves a partial, and a second launch joins a row's partials in the order of the shares.
 #include "thrift_device.h"
 #include "thrift_launch.h"
 #include "thrift_paged.h"
@@ -25,8 +26,10 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kStep = 32;                  // keys per step of a wavefront
-constexpr int kLeastShare = kWaves;        // steps
 constexpr float kShift = 15.f;
+// One workgroup per CU: its four wavefronts have 64 KiB on their way, 16 MiB on the chip.  More of them ask for more than the memory takes at a
+// time, and what waits in front of it is served unevenly.
+constexpr int kShares = kCus;
 
 // scalar loads: the lengths and the table do not change during the launch
 typedef const __attribute__((address_space(4))) int32_t* scalar_ints;
@@ -60,55 +63,51 @@ __device__ __forceinline__ float over_groups_sum(float x) {
   return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
-// Workspace: [0] steps per share, then the first step of every row, then the partials (two per share): O [D], then m - 15 and the sum.
+// Workspace: the row that every share leaves unfinished, and two partials per share: of a row that an earlier share has begun, and of
+// that unfinished row.  O [D], then m - 15 and the sum.
 struct Space {
-  int* share;
-  int* row_start;            // [B*Hkv]
-  float* part_o;             // [2*shares][G][D]
-  float* part_ml;            // [2*shares][G][2]
+  int2* tail;                // [kShares] row (-1: none) and number of shares that it lies in
+  float* part_o;             // [2*kShares][G][D]
+  float* part_ml;            // [2*kShares][G][2]
 };
 
 struct Launch {
   Space w;
-  int G, shift, shares;
+  int G, shift;
   float c;                   // softmax scale * log2(e)
 };
 
-// The state of one head: o [D] spread over the four lanes of the head, m (less 15) and this lane's part of the sum
-template <int NB, int VC>
-struct State {
-  v4f o[NB][VC];
-  float m[NB], l[NB];
+// a step: which keys of which row
+struct Step {
+  int b, hk, t, len, steps;                // sequence, KV head, number in the row; the sequence's length and steps
 };
 
-// workgroups per CU that the registers allow
-constexpr int resident(int D, int NB) { return D == 64 ? (NB == 1 ? 4 : 3) : D == 128 ? (NB == 1 ? 3 : 2) : (NB == 1 ? 2 : 1); }
-
 template <typename T, int D, int NB>
-__global__ void __launch_bounds__(kThreads, resident(D, NB)) paged_decode_kernel(PagedDecodeArgs a, Launch z) {
+__global__ void __launch_bounds__(kThreads, D * NB <= 128 ? 2 : 1) paged_decode_kernel(PagedDecodeArgs a, Launch z) {
   constexpr int KS = D / 32;               // 16-byte pieces of a key's row per lane
   constexpr int VC = D / 16;               // channels of a value's row per lane
   constexpr int NR = NB * (VC * 4 + 2);    // registers of a state
-  __shared__ __align__(16) float joined[2][NR][64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ float parts[kWaves][NR][64];  // a wavefront's part of a row that an earlier one has begun
+  __shared__ int ended[kWaves];            // whether the row ends with that part
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, grp = lane >> 4;
-  const scalar_ints seqlens = scalar(a.seqlens);
   const int capacity = a.max_pages << z.shift;
   auto length = [&](int n) { return min(capacity, max(0, n)); };
   auto steps_of = [&](int len) { return (len + kStep - 1) / kStep; };
 
-  // ---- this workgroup's share: total, first step, and the sequence it lies in ----
-  int u, u_end, b = 0, left;               // left: steps of the sequence in front of u
+  // ---- this workgroup's share, steps u .. u_end - 1, and the first one's place ----
+  int u = 0, u_end = 0, each = 0, window = 0, lens;         // lens: length of sequence window + lane
+  Step cur;
   {
-    int n = a.B, base = 0, total = 0;
-    u = 0; u_end = 0;
+    int n = a.B, base = 0, b = 0;
     bool first = true;
-    do {
+    do {                                   // 64 parts of what is left; the part with step u; once more inside it
       const int per = (n + 63) / 64;
       int sum = 0;
       for (int i = 0; i < per; ++i) {
         const int at = lane * per + i;
-        if (at < n) sum += a.Hkv * steps_of(length(a.seqlens[b + at]));
+        lens = b + at < a.B ? length(a.seqlens[b + at]) : 0;     // the last round's reach past its part: the sequences that follow
+        if (at < n) sum += a.Hkv * steps_of(lens);
       }
       int incl = sum;
 #pragma unroll
@@ -117,301 +116,400 @@ __global__ void __launch_bounds__(kThreads, resident(D, NB)) paged_decode_kernel
         if (lane >= d) incl += other;
       }
       if (first) {
-        total = __builtin_amdgcn_readlane(incl, 63);
-        const int share = max(kLeastShare, (total + z.shares - 1) / z.shares);
-        if (blockIdx.x == 0 && tid == 0) z.w.share[0] = share;
-        const long from = (long)blockIdx.x * share;
-        if (from >= total) return;
-        u = (int)from;
-        u_end = min(total, u + share);
+        const int total = __builtin_amdgcn_readlane(incl, 63);
+        const int quarter = max(1, (total + kShares * kWaves - 1) / (kShares * kWaves));
+        if (threadIdx.x == 0) z.w.tail[blockIdx.x] = make_int2(-1, 0);
+        const long begin = (long)blockIdx.x * kWaves * quarter;
+        if (begin >= total) return;        // the whole workgroup
+        u = (int)begin, u_end = min(total, u + quarter * kWaves);
+        each = quarter;
         first = false;
       }
       const int at = __builtin_ctzll(__ballot(base + incl > u));
       base += __builtin_amdgcn_readlane(incl - sum, at);
+      window = b;
       b += at * per;
       n = min(per, n - at * per);
     } while (n > 1);
-    left = u - base;
+    // wavefront-uniform, and known to be: descriptors of loads are scalar
+    u = __builtin_amdgcn_readfirstlane(u), u_end = __builtin_amdgcn_readfirstlane(u_end);
+    window = __builtin_amdgcn_readfirstlane(window), base = __builtin_amdgcn_readfirstlane(base);
+    cur.b = __builtin_amdgcn_readfirstlane(b);
+    cur.len = __builtin_amdgcn_readlane(lens, cur.b - window);
+    cur.steps = steps_of(cur.len);
+    cur.hk = __builtin_amdgcn_readfirstlane((u - base) / cur.steps);
+    cur.t = (u - base) - cur.hk * cur.steps;
   }
-  b = __builtin_amdgcn_readfirstlane(b);
-  int len = length(seqlens[b]), steps = steps_of(len);
-  int hk = left / steps, t = left - hk * steps;
+  auto advance = [&](Step& s) {            // there is a step behind
+    if (++s.t < s.steps) return;
+    s.t = 0;
+    if (++s.hk < a.Hkv) return;
+    s.hk = 0;
+    while (true) {
+      const unsigned long long later = __ballot(lens > 0 && lane > s.b - window);
+      if (later != 0) {
+        const int at = __builtin_ctzll(later);
+        s.b = window + at, s.len = __builtin_amdgcn_readlane(lens, at);
+        break;
+      }
+      window += 64, s.b = window - 1;
+      lens = window + lane < a.B ? length(a.seqlens[window + lane]) : 0;
+    }
+    s.steps = steps_of(s.len);
+  };
 
-  while (true) {
-    // ---- one segment: steps t .. t_end - 1 of row (b, hk) ----
-    const int t_end = min(steps, t + (u_end - u));
-    const scalar_ints table = scalar(a.table + (size_t)b * a.max_pages);
-    const size_t row = (size_t)b * a.Hkv + hk;
-    if (t == 0 && tid == 0) z.w.row_start[row] = u;
+  v4i q[NB][KS], q_next[NB][KS], k[2][KS];
+  uint32_t v[8][VC / 2];
+  // Loads of 16 keys go through a descriptor of their page's rows up to the length: what lies behind reads as 0 and is not fetched, and
+  // a step that does not exist has none.
+  __amdgpu_buffer_rsrc_t kd[2], vd[2];
+  int page[2];                             // of a step that is described later: a load of its own in front of the loads
+  auto look_up = [&](const Step& s) {
+    const scalar_ints table = scalar(a.table + (size_t)s.b * a.max_pages);
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) page[sub] = table[min(a.max_pages - 1, (s.t * kStep + 16 * sub) >> z.shift)];
+  };
+  auto describe = [&](const Step& s, bool there) {
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      const int key = s.t * kStep + 16 * sub, rows = __builtin_amdgcn_readfirstlane(there ? min(16, max(0, s.len - key)) : 0);
+      const int p = __builtin_amdgcn_readfirstlane(min(a.n_pages - 1, max(0, page[sub])));
+      const size_t at = ((((size_t)p * a.Hkv + s.hk) << z.shift) + (key & ((1 << z.shift) - 1))) * D;
+      kd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_pages + at), 0, rows * D * 2, 0x00020000);
+      vd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_pages + at), 0, rows * D * 2, 0x00020000);
+    }
+  };
+  auto load_q = [&](const Step& s, bool there) {
+    const uint16_t* qp = a.q + ((size_t)s.b * a.Hkv + s.hk) * z.G * D;
+    const __amdgpu_buffer_rsrc_t qd = __builtin_amdgcn_make_buffer_rsrc((void*)qp, 0, there ? z.G * D * 2 : 0, 0x00020000);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < KS; ++e)
+        q_next[nb][e] = __builtin_amdgcn_raw_buffer_load_b128(qd, (col + 16 * nb) * D * 2 + 64 * e + 16 * grp, 0, 0);
+  };
+  auto next_q = [&]() {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < KS; ++e) q[nb][e] = q_next[nb][e];
+  };
+  constexpr int kStream = 2;               // non-temporal: keys and values are read once
+  const int k_lane = col * D * 2 + 16 * grp, v_lane = 4 * grp * D * 2 + 2 * VC * col;
+  auto load_k = [&]() {
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int e = 0; e < KS; ++e) k[sub][e] = __builtin_amdgcn_raw_buffer_load_b128(kd[sub], k_lane + 64 * e, 0, kStream);
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const int from = v_lane + (r & 3) * D * 2;
+      if constexpr (VC == 4) {
+        const v2i x = __builtin_amdgcn_raw_buffer_load_b64(vd[r >> 2], from, 0, kStream);
+        v[r][0] = x[0], v[r][1] = x[1];
+      } else {
+#pragma unroll
+        for (int e = 0; e < VC / 8; ++e) {
+          const v4i x = __builtin_amdgcn_raw_buffer_load_b128(vd[r >> 2], from + 16 * e, 0, kStream);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) v[r][4 * e + d] = x[d];
+        }
+      }
+    }
+  };
 
-    v4i q[NB][KS];
+  v4f o[NB][VC];                           // o [D] of one head is spread over the four lanes of its column
+  float m[NB], l[NB];                      // maximum less 15; this lane's part of the sum
+  auto clear = [&]() {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      m[nb] = -__builtin_inff(), l[nb] = 0.f;
+#pragma unroll
+      for (int j = 0; j < VC; ++j) o[nb][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+
+  // A part of a row in LDS, a lane's registers in its column, and its addition to another
+  auto give = [&](float (*to)[64]) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float (*p)[64] = to + nb * (VC * 4 + 2);
+#pragma unroll
+      for (int j = 0; j < VC; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[4 * j + r][lane] = o[nb][j][r];
+      p[4 * VC][lane] = m[nb], p[4 * VC + 1][lane] = l[nb];
+    }
+  };
+  auto take = [&](float (*from)[64]) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float (*p)[64] = from + nb * (VC * 4 + 2);
+      const float other = p[4 * VC][lane], top = fmaxf(m[nb], other), k1 = fast_exp2(m[nb] - top), k2 = fast_exp2(other - top);
+      m[nb] = top;
+      l[nb] = l[nb] * k1 + p[4 * VC + 1][lane] * k2;
+#pragma unroll
+      for (int j = 0; j < VC; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[nb][j][r] = o[nb][j][r] * k1 + p[4 * j + r][lane] * k2;
+    }
+  };
+  // The state as the row's result, or as this share's part of it
+  auto put = [&](const Step& s, bool begins, bool ends) {
+    const size_t row = (size_t)s.b * a.Hkv + s.hk, slot = 2 * (size_t)blockIdx.x + (begins ? 1 : 0);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int head = col + 16 * nb;
+      const float sum = over_groups_sum(l[nb]), inv = 1.f / sum;
+      if (head >= z.G) continue;
+      if (begins && ends) {
+        const size_t to = row * z.G + head;
+        if (a.lse != nullptr && grp == 0) a.lse[to] = 0.6931471805599453f * (m[nb] + __builtin_log2f(sum));
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        q[nb][s] = head < z.G ? *reinterpret_cast<const v4i*>(a.q + (row * z.G + head) * D + 32 * s + 8 * grp) : v4i{0, 0, 0, 0};
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < VC; j += 4)
+            store_out4(a.out, a.out_dt, to * D + (4 * grp + r) * VC + j, o[nb][j][r] * inv, o[nb][j + 1][r] * inv, o[nb][j + 2][r] * inv, o[nb][j + 3][r] * inv);
+      } else {
+        const size_t to = slot * z.G + head;
+        if (grp == 0) z.w.part_ml[2 * to] = m[nb], z.w.part_ml[2 * to + 1] = sum;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < VC; j += 4)
+            *reinterpret_cast<v4f*>(z.w.part_o + to * D + (4 * grp + r) * VC + j) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]};
+      }
     }
-    State<NB, VC> st;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      st.m[nb] = -__builtin_inff(), st.l[nb] = 0.f;
-#pragma unroll
-      for (int j = 0; j < VC; ++j) st.o[nb][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
+  };
 
-    // element offset of the 16 keys from key on
-    auto place = [&](int key) {
-      const int page = min(a.n_pages - 1, max(0, table[min(a.max_pages - 1, key >> z.shift)]));
-      return ((((size_t)page * a.Hkv + hk) << z.shift) + (key & ((1 << z.shift) - 1))) * D;
-    };
-    for (int i = t + wave; i < t_end; i += kWaves) {
-      const int key0 = i * kStep;
-      v4i k[2][KS];
-      uint32_t v[8][VC / 2];
+  // ---- this wavefront's steps: every fourth where the share lies in one row, which keeps what the four read together, otherwise a quarter
+  // of the share, which leaves them one meeting whatever number of rows there is ----
+  const bool one_row = cur.t + (u_end - u) <= cur.steps;
+  const int stride = one_row ? kWaves : 1;
+  int skip = one_row ? wave : wave * each;
+  u += skip;
+  if (!one_row) u_end = min(u_end, u + each);
+  while (skip > 0 && u < u_end) {
+    const int room = cur.steps - cur.t;
+    if (skip < room) {
+      cur.t += skip;
+      break;
+    }
+    skip -= room;
+    cur.t = cur.steps - 1;
+    advance(cur);
+  }
+  bool kept = false;                       // the state is the first part of a row that the next wavefronts have more of
+  int begin = cur.t, first_u = u;          // this wavefront's first step of the row: in the row, and of all steps
+  if (wave > 0 && lane == 0) ended[wave] = u < u_end ? 0 : -1;
+  Step next = cur;
+  bool more = false;                       // next is a step of this wavefront
+  auto follow = [&]() {                    // next becomes the step behind, if there is one, and its pages are asked for
+    u += stride;
+    more = u < u_end;
+    if (one_row) next.t += more ? kWaves : 0;
+    else if (more) advance(next);
+    look_up(next);
+  };
+  bool busy = u < u_end;
+  if (busy) {
+    look_up(cur);
+    load_q(cur, true);
+    describe(cur, true);
+    load_k();
+    load_v();
+    clear();
+    next_q();
+    follow();
+  }
+  while (busy) {
+    float x[NB][8];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
-        const size_t at = place(key0 + 16 * sub);
-        const uint16_t* kp = a.k_pages + at + col * D + 8 * grp;
-        const uint16_t* vp = a.v_pages + at + 4 * grp * D + VC * col;
+        v4f s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < KS; ++s) k[sub][s] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(kp + 32 * s));
+        for (int e = 0; e < KS; ++e) s = Mma<T>::mma(k[sub][e], q[nb][e], s);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if constexpr (VC == 4) {
-            const v2i x = __builtin_nontemporal_load(reinterpret_cast<const v2i*>(vp + r * D));
-            v[4 * sub + r][0] = x[0], v[4 * sub + r][1] = x[1];
-          } else {
-#pragma unroll
-            for (int e = 0; e < VC / 8; ++e) {
-              const v4i x = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(vp + r * D + 8 * e));
-#pragma unroll
-              for (int d = 0; d < 4; ++d) v[4 * sub + r][4 * e + d] = x[d];
-            }
-          }
-        }
+        for (int r = 0; r < 4; ++r) x[nb][4 * sub + r] = s[r] * z.c;
       }
-      const bool tail = key0 + kStep > len;
-      v4i high[NB], low[NB];
+    const bool turns = more && next.t == 0;                      // a row begins with the next step
+    describe(next, more);
+    load_k();
+    load_q(next, turns);
+    const int behind = cur.len - cur.t * kStep;                  // keys of the row from this step on
+    auto masked = [&](int r) { return (r < 4 ? 0 : 12) + 4 * grp + r >= behind; };
+    v4i high[NB], low[NB];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float x[8];
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-          v4f s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int e = 0; e < KS; ++e) s = Mma<T>::mma(k[sub][e], q[nb][e], s);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[4 * sub + r] = s[r] * z.c;
-        }
-        if (tail) {
-#pragma unroll
-          for (int r = 0; r < 8; ++r)
-            if (key0 + (r < 4 ? 0 : 12) + 4 * grp + r >= len) x[r] = -__builtin_inff();
-        }
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        top = over_groups_max(top) - kShift;
-        if (__ballot(top > st.m[nb])) {
-          const float m = fmaxf(top, st.m[nb]), keep = fast_exp2(st.m[nb] - m);
-          st.m[nb] = m;
-          st.l[nb] *= keep;
-#pragma unroll
-          for (int j = 0; j < VC; ++j) st.o[nb][j] *= keep;
-        }
-        uint16_t hi[8], lo[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const float p = fast_exp2(x[r] - st.m[nb]);
-          st.l[nb] += p;
-          hi[r] = T::from_float(p);
-          lo[r] = T::from_float(p - T::to_float(hi[r]));
-        }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          high[nb][r] = (int)((uint32_t)hi[2 * r] | ((uint32_t)hi[2 * r + 1] << 16));
-          low[nb][r] = (int)((uint32_t)lo[2 * r] | ((uint32_t)lo[2 * r + 1] << 16));
-        }
-      }
-      if (tail) {                          // 0 times whatever lies past the length would not be 0
+    for (int nb = 0; nb < NB; ++nb) {
+      if (behind < kStep) {
 #pragma unroll
         for (int r = 0; r < 8; ++r)
-          if (key0 + (r < 4 ? 0 : 12) + 4 * grp + r >= len) {
+          if (masked(r)) x[nb][r] = -__builtin_inff();
+      }
+      const float (&y)[8] = x[nb];
+      const float top = over_groups_max(fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])))) - kShift;
+      if (__ballot(top > m[nb])) {
+        const float grown = fmaxf(top, m[nb]), keep = fast_exp2(m[nb] - grown);
+        m[nb] = grown;
+        l[nb] *= keep;
 #pragma unroll
-            for (int d = 0; d < VC / 2; ++d) v[r][d] = 0;
-          }
+        for (int j = 0; j < VC; ++j) o[nb][j] *= keep;
+      }
+      uint16_t hi[8], lo[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float p = fast_exp2(y[r] - m[nb]);
+        l[nb] += p;
+        hi[r] = T::from_float(p);
+        lo[r] = T::from_float(p - T::to_float(hi[r]));
       }
 #pragma unroll
-      for (int j = 0; j < VC; ++j) {
-        v4i x;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = (int)__builtin_amdgcn_perm(v[2 * r + 1][j / 2], v[2 * r][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          st.o[nb][j] = Mma<T>::mma(x, high[nb], st.o[nb][j]);
-          st.o[nb][j] = Mma<T>::mma(x, low[nb], st.o[nb][j]);
-        }
-      }
-    }
-
-    // ---- join the wavefronts: 2 into 0 and 3 into 1, then 1 into 0 ----
-    auto give = [&](float (*to)[64]) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float (*p)[64] = to + nb * (VC * 4 + 2);
-#pragma unroll
-        for (int j = 0; j < VC; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) p[4 * j + r][lane] = st.o[nb][j][r];
-        p[4 * VC][lane] = st.m[nb], p[4 * VC + 1][lane] = st.l[nb];
-      }
-    };
-    auto take = [&](float (*from)[64]) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float (*p)[64] = from + nb * (VC * 4 + 2);
-        const float m2 = p[4 * VC][lane], m = fmaxf(st.m[nb], m2);
-        const float k1 = st.m[nb] == m ? 1.f : fast_exp2(st.m[nb] - m), k2 = m2 == -__builtin_inff() ? 0.f : fast_exp2(m2 - m);
-        st.m[nb] = m;
-        st.l[nb] = st.l[nb] * k1 + p[4 * VC + 1][lane] * k2;
-#pragma unroll
-        for (int j = 0; j < VC; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) st.o[nb][j][r] = st.o[nb][j][r] * k1 + p[4 * j + r][lane] * k2;
-      }
-    };
-    if (wave >= 2) give(joined[wave - 2]);
-    __syncthreads();
-    if (wave < 2) take(joined[wave]);
-    if (wave == 1) give(joined[1]);
-    __syncthreads();
-    if (wave == 0) {
-      take(joined[1]);
-      const bool whole = t == 0 && t_end == steps;
-      const int slot = 2 * (int)blockIdx.x + (t == 0 ? 1 : 0);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int head = col + 16 * nb;
-        const float l = over_groups_sum(st.l[nb]), inv = 1.f / l;
-        if (head >= z.G) continue;
-        if (whole) {
-          const size_t at = row * z.G + head;
-          if (a.lse != nullptr && grp == 0) a.lse[at] = 0.6931471805599453f * (st.m[nb] + __builtin_log2f(l));
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < VC; j += 4)
-              store_out4(a.out, a.out_dt, at * D + (4 * grp + r) * VC + j, st.o[nb][j][r] * inv, st.o[nb][j + 1][r] * inv, st.o[nb][j + 2][r] * inv, st.o[nb][j + 3][r] * inv);
-        } else {
-          const size_t at = (size_t)slot * z.G + head;
-          if (grp == 0) z.w.part_ml[2 * at] = st.m[nb], z.w.part_ml[2 * at + 1] = l;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int j = 0; j < VC; j += 4)
-              *reinterpret_cast<v4f*>(z.w.part_o + at * D + (4 * grp + r) * VC + j) = v4f{st.o[nb][j][r], st.o[nb][j + 1][r], st.o[nb][j + 2][r], st.o[nb][j + 3][r]};
-        }
+      for (int r = 0; r < 4; ++r) {
+        high[nb][r] = (int)((uint32_t)hi[2 * r] | ((uint32_t)hi[2 * r + 1] << 16));
+        low[nb][r] = (int)((uint32_t)lo[2 * r] | ((uint32_t)lo[2 * r + 1] << 16));
       }
     }
-    u += t_end - t;
-    if (u >= u_end) return;
-    t = 0;
-    if (++hk == a.Hkv) {
-      hk = 0;
-      do len = length(seqlens[++b]); while (len == 0);       // u < u_end: there is a sequence with tokens behind
-      steps = steps_of(len);
+#pragma unroll
+    for (int j = 0; j < VC; ++j) {
+      v4i y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = (int)__builtin_amdgcn_perm(v[2 * r + 1][j / 2], v[2 * r][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        o[nb][j] = Mma<T>::mma(y, high[nb], o[nb][j]);
+        o[nb][j] = Mma<T>::mma(y, low[nb], o[nb][j]);
+      }
     }
-    __syncthreads();                       // wavefront 0 has read what the next segment overwrites
+    load_v();
+    if (!more || turns) {                  // the row ends, or what this wavefront has of it
+      const bool ends = cur.t + 1 == cur.steps;
+      if (begin > 0 && wave > 0) {         // an earlier wavefront's row
+        give(parts[wave]);
+        if (ends && lane == 0) ended[wave] = 1;
+      } else if (ends && !one_row) {
+        put(cur, begin == 0, true);
+      } else {
+        kept = true;
+      }
+      if (!more) break;
+      clear();
+      next_q();
+      begin = 0, first_u = u;
+    }
+    cur = next;
+    follow();
+  }
+  __syncthreads();
+  if (!kept) return;
+  bool ends = cur.t + 1 == cur.steps;
+  for (int w = wave + 1; w < kWaves && (one_row || !ends); ++w) {
+    if (ended[w] < 0) break;
+    take(parts[w]);
+    ends |= ended[w] > 0;
+  }
+  put(cur, begin == 0, ends);
+  // the state began with the row's first step, at each * kWaves * (shares so far) + what this share has of other rows; the rest of the
+  // row's steps fill the shares behind
+  if (begin == 0 && !ends && lane == 0) {
+    const int share = each * kWaves, here = min(share - (first_u - (int)blockIdx.x * share), cur.steps);
+    z.w.tail[blockIdx.x] = make_int2(cur.b * a.Hkv + cur.hk, 1 + (cur.steps - here + share - 1) / share);
   }
 }
 
-// One workgroup per (sequence, query head): joins the partials of a row that several shares have; rows without tokens become 0.
+// One workgroup per share and head of a group: joins the partials of the row that the share leaves unfinished.  Threads take four channels
+// of every kParts-th partial with a running maximum of their own, so that a partial's maximum, sum and channels are asked
+// for together.  Sequences without tokens become 0.
 template <int D>
-__global__ void __launch_bounds__(256) paged_merge_kernel(PagedDecodeArgs a, Launch z) {
-  constexpr int kQuads = D / 4, kParts = 256 / kQuads;      // float4 columns; partials side by side
-  __shared__ float scale_of[256];
-  __shared__ float top_of[4], sum_of[4];
+__global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedDecodeArgs a, Launch z) {
+  constexpr int kQuads = D / 4, kParts = kThreads / kQuads, kAhead = 4;
+  __shared__ float2 ml[kParts];
   __shared__ __align__(16) v4f sums[kParts][kQuads];
-  const int tid = threadIdx.x, b = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, hk = h / z.G;
-  const int len = min(a.max_pages << z.shift, max(0, a.seqlens[b])), steps = (len + kStep - 1) / kStep;
-  const size_t at = (size_t)b * a.Hq + h;
+  const int tid = threadIdx.x, first = blockIdx.x / z.G, g = blockIdx.x % z.G;
   const int quad = tid % kQuads, part = tid / kQuads;
-  if (len == 0) {
-    if (part == 0) store_out4(a.out, a.out_dt, at * D + 4 * quad, 0.f, 0.f, 0.f, 0.f);
-    if (a.lse != nullptr && tid == 0) a.lse[at] = -__builtin_inff();
-    return;
+  const int2 tail = z.w.tail[first];
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    if (a.seqlens[b] > 0) continue;
+    for (int i = tid; i < a.Hq * kQuads; i += kThreads) store_out4(a.out, a.out_dt, (size_t)b * a.Hq * D + 4 * (size_t)i, 0.f, 0.f, 0.f, 0.f);
+    if (a.lse != nullptr)
+      for (int h = tid; h < a.Hq; h += kThreads) a.lse[(size_t)b * a.Hq + h] = -__builtin_inff();
   }
-  const int share = z.w.share[0], u = z.w.row_start[(size_t)b * a.Hkv + hk];
-  const int first = u / share, n = (u + steps - 1) / share - first + 1;
-  if (n == 1) return;                                       // inside one share: written already
-  auto slot = [&](int i) { return (size_t)(2 * (first + i) + (i == 0 ? 1 : 0)) * z.G + (h - hk * z.G); };
-  // the largest maximum of all partials
-  float top = -__builtin_inff();
-  for (int i = tid; i < n; i += 256) top = fmaxf(top, z.w.part_ml[2 * slot(i)]);
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if ((tid & 63) == 0) top_of[tid >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(top_of[0], top_of[1]), fmaxf(top_of[2], top_of[3]));
+  const int n = tail.y;
+  if (tail.x < 0) return;
+  const size_t at = (size_t)tail.x * z.G + g;
   v4f o = {0.f, 0.f, 0.f, 0.f};
-  float l = 0.f;
-  for (int i0 = 0; i0 < n; i0 += 256) {
-    if (i0 > 0) __syncthreads();
-    if (i0 + tid < n) {
-      const size_t s = slot(i0 + tid);
-      const float k = fast_exp2(z.w.part_ml[2 * s] - top);
-      scale_of[tid] = k;
-      l += k * z.w.part_ml[2 * s + 1];
+  float m = -__builtin_inff(), l = 0.f;
+  for (int i0 = part; i0 < n; i0 += kParts * kAhead) {
+    v4f x[kAhead];
+    float2 y[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int w = min(n - 1, i0 + i * kParts);
+      const size_t s = (size_t)(2 * (first + w) + (w == 0 ? 1 : 0)) * z.G + g;
+      x[i] = *reinterpret_cast<const v4f*>(z.w.part_o + s * D + 4 * quad);
+      y[i] = *reinterpret_cast<const float2*>(z.w.part_ml + 2 * s);
+      if (i0 + i * kParts >= n) y[i] = make_float2(-__builtin_inff(), 0.f);
     }
-    __syncthreads();
-    const int count = min(256, n - i0);
-    for (int i = part; i < count; i += kParts) o += scale_of[i] * *reinterpret_cast<const v4f*>(z.w.part_o + slot(i0 + i) * D + 4 * quad);
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) top = fmaxf(top, y[i].x);
+    const float keep = fast_exp2(m - top);
+    m = top, l *= keep, o *= keep;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float k = fast_exp2(y[i].x - top);
+      l += k * y[i].y, o += k * x[i];
+    }
   }
-  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
-  if ((tid & 63) == 0) sum_of[tid >> 6] = l;
+  if (quad == 0) ml[part] = make_float2(m, l);
   sums[part][quad] = o;
   __syncthreads();
   if (part != 0) return;
-  l = (sum_of[0] + sum_of[1]) + (sum_of[2] + sum_of[3]);
-  for (int i = 1; i < kParts; ++i) o += sums[i][quad];
-  const float inv = 1.f / l;
+  float top = ml[0].x, sum = 0.f;
+#pragma unroll
+  for (int i = 1; i < kParts; ++i) top = fmaxf(top, ml[i].x);
+  o = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) {
+    const float k = fast_exp2(ml[i].x - top);
+    sum += k * ml[i].y, o += k * sums[i][quad];
+  }
+  const float inv = 1.f / sum;
   store_out4(a.out, a.out_dt, at * D + 4 * quad, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-  if (a.lse != nullptr && tid == 0) a.lse[at] = 0.6931471805599453f * (top + __builtin_log2f(l));
+  if (a.lse != nullptr && tid == 0) a.lse[at] = 0.6931471805599453f * (top + __builtin_log2f(sum));
 }
-
-int shares_of(int D, int G) { return kCus * resident(D, G > 16 ? 2 : 1); }
 
 template <typename T>
 void launch(const PagedDecodeArgs& a, const Launch& z, hipStream_t st) {
-  const dim3 grid(z.shares), merge((unsigned)((long)a.B * a.Hq)), block(kThreads);
+  const dim3 grid(kShares), merge(kShares * z.G), block(kThreads);
 #define THRIFT_PAGED(D_)                                                                     \
   if (z.G <= 16) paged_decode_kernel<T, D_, 1><<<grid, block, 0, st>>>(a, z);                \
   else paged_decode_kernel<T, D_, 2><<<grid, block, 0, st>>>(a, z);                          \
-  paged_merge_kernel<D_><<<merge, dim3(256), 0, st>>>(a, z)
+  paged_merge_kernel<D_><<<merge, block, 0, st>>>(a, z)
   if (a.D == 64) { THRIFT_PAGED(64); }
   else if (a.D == 128) { THRIFT_PAGED(128); }
   else { THRIFT_PAGED(256); }
 #undef THRIFT_PAGED
 }
 
-size_t aligned(size_t x) { return (x + 255) & ~(size_t)255; }
+constexpr size_t kTailBytes = kShares * sizeof(int2);
 
 }  // namespace
 
-size_t paged_decode_workspace(int B, int Hq, int Hkv, int, int, int D) {
-  const size_t G = Hq / Hkv, slots = 2 * (size_t)shares_of(D, (int)G);
-  return 256 + aligned((size_t)B * Hkv * sizeof(int)) + aligned(slots * G * D * sizeof(float)) + aligned(slots * G * 2 * sizeof(float));
-}
+size_t paged_decode_workspace(int Hq, int Hkv, int D) { return kTailBytes + 2 * (size_t)kShares * (Hq / Hkv) * (D + 2) * sizeof(float); }
 
 void launch_paged_decode(const PagedDecodeArgs& a, hipStream_t st) {
   Launch z;
   z.G = a.Hq / a.Hkv;
   z.shift = __builtin_ctz(a.page_size);
-  z.shares = shares_of(a.D, z.G);
   z.c = a.scale * 1.4426950408889634f;
   char* w = (char*)a.workspace;
-  z.w.share = (int*)w; w += 256;
-  z.w.row_start = (int*)w; w += aligned((size_t)a.B * a.Hkv * sizeof(int));
-  z.w.part_o = (float*)w; w += aligned(2 * (size_t)z.shares * z.G * a.D * sizeof(float));
-  z.w.part_ml = (float*)w;
+  z.w.tail = (int2*)w;
+  z.w.part_o = (float*)(w + kTailBytes);
+  z.w.part_ml = z.w.part_o + 2 * (size_t)kShares * z.G * a.D;
   if (a.dt == THRIFT_F16) launch<F16>(a, z, st);
   else launch<BF16>(a, z, st);
 }
