@@ -4,8 +4,8 @@
 // 16 x 16 matrix tiles:
 //   S = K Q^T      32 keys x 16 heads; operand K straight from memory, a lane reads 16 bytes of the row of its key
 //   P = 2^(S - m)  in fp32, with the running maximum m of the head; sums in fp32
-//   O^T += V^T P^T channels x heads.  A lane reads the channels D/16 c .. of the rows of its eight keys and pairs the rows' halves
-//                  up (one byte permute per two elements); matrix tile j holds channel j of every lane.  The eight keys are those whose
+//   O^T += V^T P^T channels x heads.  A lane reads eight channels (four of 64) of every 128 in the rows of its eight keys and pairs the
+//                  rows' halves up (one byte permute per two elements); matrix tile j holds channel j of every lane.  The eight keys are those whose
 //                  scores the lane holds, so that P goes from S to the next product without leaving the lane.
 // No tile passes through LDS.  P is split into two 16-bit pieces, high and low, for two products: rounding it once would cost an
 // output of 16 bits as much accuracy again as the output's own rounding.  P is scaled by 2^15, so that an fp16 piece is a normal
@@ -24,7 +24,10 @@ namespace thrift {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256;              // of the merge
+// Wavefronts of a share.  256 channels: two, whose 64 KiB on their way are as much as four of 128 channels have (4 x 8192-16384 tokens, 32/8
+// heads: 74.1 -> 70.2 us); 64 channels: eight with as much were slower than four (23.6 -> 25.1 us).
+constexpr int waves_of(int D) { return D == 256 ? 2 : 4; }
 constexpr int kStep = 32;                  // keys per step of a wavefront
 constexpr float kShift = 15.f;
 // One workgroup per CU: its four wavefronts have 64 KiB on their way, 16 MiB on the chip.  More of them ask for more than the memory takes at a
@@ -83,7 +86,8 @@ struct Step {
 };
 
 template <typename T, int D, int NB>
-__global__ void __launch_bounds__(kThreads, D * NB <= 128 ? 2 : 1) paged_decode_kernel(PagedDecodeArgs a, Launch z) {
+__global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged_decode_kernel(PagedDecodeArgs a, Launch z) {
+  constexpr int kWaves = waves_of(D);
   constexpr int KS = D / 32;               // 16-byte pieces of a key's row per lane
   constexpr int VC = D / 16;               // channels of a value's row per lane
   constexpr int NR = NB * (VC * 4 + 2);    // registers of a state
@@ -195,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, D * NB <= 128 ? 2 : 1) paged_decode_
       for (int e = 0; e < KS; ++e) q[nb][e] = q_next[nb][e];
   };
   constexpr int kStream = 2;               // non-temporal: keys and values are read once
-  const int k_lane = col * D * 2 + 16 * grp, v_lane = 4 * grp * D * 2 + 2 * VC * col;
+  const int k_lane = col * D * 2 + 16 * grp, v_lane = 4 * grp * D * 2 + 2 * min(VC, 8) * col;
   auto load_k = [&]() {
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub)
@@ -212,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, D * NB <= 128 ? 2 : 1) paged_decode_
       } else {
 #pragma unroll
         for (int e = 0; e < VC / 8; ++e) {
-          const v4i x = __builtin_amdgcn_raw_buffer_load_b128(vd[r >> 2], from + 16 * e, 0, kStream);
+          const v4i x = __builtin_amdgcn_raw_buffer_load_b128(vd[r >> 2], from + 256 * e, 0, kStream);
 #pragma unroll
           for (int d = 0; d < 4; ++d) v[r][4 * e + d] = x[d];
         }
@@ -220,7 +224,8 @@ __global__ void __launch_bounds__(kThreads, D * NB <= 128 ? 2 : 1) paged_decode_
     }
   };
 
-  v4f o[NB][VC];                           // o [D] of one head is spread over the four lanes of its column
+  v4f o[NB][VC];                           // o [D] of one head is spread over the four lanes of its column: element r of tile j is channel(r, j)
+  auto channel = [&](int r, int j) { return (j >> 3) * 128 + (4 * grp + r) * min(VC, 8) + (j & 7); };
   float m[NB], l[NB];                      // maximum less 15; this lane's part of the sum
   auto clear = [&]() {
 #pragma unroll
@@ -271,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, D * NB <= 128 ? 2 : 1) paged_decode_
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int j = 0; j < VC; j += 4)
-            store_out4(a.out, a.out_dt, to * D + (4 * grp + r) * VC + j, o[nb][j][r] * inv, o[nb][j + 1][r] * inv, o[nb][j + 2][r] * inv, o[nb][j + 3][r] * inv);
+            store_out4(a.out, a.out_dt, to * D + channel(r, j), o[nb][j][r] * inv, o[nb][j + 1][r] * inv, o[nb][j + 2][r] * inv, o[nb][j + 3][r] * inv);
       } else {
         const size_t to = slot * z.G + head;
         if (grp == 0) z.w.part_ml[2 * to] = m[nb], z.w.part_ml[2 * to + 1] = sum;
@@ -279,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, D * NB <= 128 ? 2 : 1) paged_decode_
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int j = 0; j < VC; j += 4)
-            *reinterpret_cast<v4f*>(z.w.part_o + to * D + (4 * grp + r) * VC + j) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]};
+            *reinterpret_cast<v4f*>(z.w.part_o + to * D + channel(r, j)) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]};
       }
     }
   };
@@ -486,8 +491,8 @@ template <typename T>
 void launch(const PagedDecodeArgs& a, const Launch& z, hipStream_t st) {
   const dim3 grid(kShares), merge(kShares * z.G), block(kThreads);
 #define THRIFT_PAGED(D_)                                                                     \
-  if (z.G <= 16) paged_decode_kernel<T, D_, 1><<<grid, block, 0, st>>>(a, z);                \
-  else paged_decode_kernel<T, D_, 2><<<grid, block, 0, st>>>(a, z);                          \
+  if (z.G <= 16) paged_decode_kernel<T, D_, 1><<<grid, dim3(64 * waves_of(D_)), 0, st>>>(a, z);                \
+  else paged_decode_kernel<T, D_, 2><<<grid, dim3(64 * waves_of(D_)), 0, st>>>(a, z);                          \
   paged_merge_kernel<D_><<<merge, block, 0, st>>>(a, z)
   if (a.D == 64) { THRIFT_PAGED(64); }
   else if (a.D == 128) { THRIFT_PAGED(128); }
