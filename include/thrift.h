@@ -446,7 +446,8 @@ thrift_status thrift_page_map(const int32_t* seqlens, const int32_t* new_lens, i
 /*
  * Returns the pages of finished sequences: for every b with drop[b] != 0 the ceil(seqlens[b] / page_size) pages of the sequence are put
  * on the stack in order (sequence, page) and its length becomes 0.  Table entries outside 0 .. n_pages - 1 are not put back, nor is what would pass
- * free_capacity.  block_table is read only.  seqlens_out [B], free_count_out [1]: arrays of their own.
+ * free_capacity.  block_table is read only.  seqlens_out [B], free_count_out [1]: arrays of their own.  Limits as thrift_page_map;
+ * B * max_pages below 2^31.
  */
 thrift_status thrift_page_release(const int32_t* seqlens, const int32_t* drop, int B, int page_size, int n_pages,
                                   const int32_t* block_table, int max_pages, int32_t* free_pages, int free_capacity, const int32_t* free_count,

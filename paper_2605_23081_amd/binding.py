@@ -528,9 +528,6 @@ def _heads(t: torch.Tensor, shape, dtype) -> None:
 
 
 def _rope(name: str, q, k, freqs, positions, layout: str, gain: float, q_out, k_out):
-    r = (_call or _native()).rope(int(name != "thrift_rope"), q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, _device(), _raw_stream())
-    if r is not None:
-        return _result(r, name)
     assert q.dtype in (torch.float16, torch.bfloat16), q.dtype
     B, Hq, N, D = q.shape
     _heads(q, q.shape, q.dtype)
@@ -562,12 +559,18 @@ def thrift_rope(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: s
                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q [B,Hq,N,D] and k [B,Hkv,N,D] (or None) with their first 2 * len(freqs) channels turned to positions ([B,N] or [N], default
     0 .. N-1): (q_out, k_out), contiguous unless given.  Inputs and outputs may be views (a fused projection's [B,N,H,D])."""
+    r = (_call or _native()).rope(0, q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, _device(), _raw_stream())
+    if r is not None:
+        return _result(r, "thrift_rope")
     return _rope("thrift_rope", q, k, freqs, positions, layout, gain, q_out, k_out)
 
 
 def thrift_rope_backward(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: str = "half", gain: float = 1.0,
                          q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """Gradients of thrift_rope's inputs from those of its outputs, q and k (or None); arguments as thrift_rope."""
+    r = (_call or _native()).rope(1, q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, _device(), _raw_stream())
+    if r is not None:
+        return _result(r, "thrift_rope_backward")
     return _rope("thrift_rope_backward", q, k, freqs, positions, layout, gain, q_out, k_out)
 
 

@@ -692,7 +692,7 @@ thrift_status thrift_page_release(const int32_t* seqlens, const int32_t* drop, i
                                   int32_t* seqlens_out, int32_t* free_count_out, void* stream) {
   if (!seqlens || !drop || !block_table || !free_pages || !free_count || !seqlens_out || !free_count_out) return THRIFT_ERR_NULL;
   if (B <= 0 || B > kMapMaxSeqs || !page_size_ok(page_size) || free_capacity <= 0 || !fits_int(n_pages, page_size) ||
-      !fits_int(max_pages, page_size) || seqlens_out == seqlens || free_count_out == free_count)
+      !fits_int(max_pages, page_size) || !fits_int(B, max_pages) || seqlens_out == seqlens || free_count_out == free_count)
     return THRIFT_ERR_SHAPE;
   if (thrift_status s = check_arch()) return s;
   PageReleaseArgs a;

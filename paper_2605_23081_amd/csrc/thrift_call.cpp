@@ -275,9 +275,19 @@ PyObject* page_map(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (B > 0x7ffffffe || width > 0x7fffffff || free->numel() > 0x7fffffff || table->scalar_type() != at::kInt || free->scalar_type() != at::kInt ||
       !is(*lens, at::kInt, {B}) || !is(*fresh, at::kInt, {B}) || !is(*count, at::kInt, {1}))
     Py_RETURN_NONE;
+  // five arrays of one allocation, 16 bytes aligned each
   Tensor out[5];
   const int64_t sizes[5] = {rows, rows, B + 1, B, 1};
-  for (int i = 0; i < 5; ++i) out[i] = at::empty({sizes[i]}, lens->options());
+  int64_t offset = 0;
+  for (const int64_t x : sizes) offset += (x + 3) / 4 * 4;
+  const Tensor space = at::empty({offset}, lens->options());
+  offset = 0;
+  for (int i = 0; i < 5; ++i) {
+    out[i] = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(space.storage()), space.key_set(), space.dtype());
+    out[i].unsafeGetTensorImpl()->set_storage_offset(offset);
+    out[i].unsafeGetTensorImpl()->set_sizes_contiguous({sizes[i]});
+    offset += (sizes[i] + 3) / 4 * 4;
+  }
   const auto p = [&](int i) { return out[i].data_ptr<int32_t>(); };
   thrift_status r;
   {

@@ -8,42 +8,42 @@ namespace thrift {
 namespace {
 
 constexpr int kMapThreads = 256;
-constexpr int kMapPerThread = kMapMaxSeqs / kMapThreads;
+constexpr int kMapRows = 4;                            // neighbouring rows of a thread
 
-// Exclusive prefix sums of at most kMapMaxSeqs counts over the workgroup, saturating at `cap`: counts and cap are not negative and below
-// 2^31, so that a sum of two fits 32 unsigned bits, and min(a + b, cap) is associative.  count(b) is asked for once;
-// prefix[0 .. B] is written.
-template <typename F>
-__device__ __forceinline__ void prefix_sums(int B, uint32_t cap, uint32_t* prefix, uint32_t* wave_sums, F count) {
+// Exclusive prefix sums of two counts per sequence over the workgroup, at most kMapMaxSeqs sequences.  The first saturates at `cap`: counts and
+// cap are below 2^31, so that a sum of two fits 32 unsigned bits, and min(a + b, cap) is associative.  The second may not pass
+// 2^31 (saturated there as well).  PER: sequences of a thread at most.  count(b) is asked for once; x[0 .. B] and y[0 .. B] are written.
+template <int PER, typename F>
+__device__ __forceinline__ void prefix_sums(int B, uint32_t cap, uint32_t* x, uint32_t* y, uint2* wave_sums, F count) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (B + kMapThreads - 1) / kMapThreads;
-  uint32_t mine[kMapPerThread], sum = 0;
+  const int per = PER == 1 ? 1 : (B + kMapThreads - 1) / kMapThreads;
+  auto add = [&](uint2 a, uint2 b) { return make_uint2(min(a.x + b.x, cap), min(a.y + b.y, 0x7fffffffu)); };
+  uint2 mine[PER], sum = make_uint2(0, 0);
 #pragma unroll
-  for (int i = 0; i < kMapPerThread; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const int b = tid * per + i;
-    mine[i] = (i < per && b < B) ? min(count(b), cap) : 0u;
-    sum = min(sum + mine[i], cap);
+    mine[i] = i < per && b < B ? count(b) : make_uint2(0, 0);
+    mine[i].x = min(mine[i].x, cap);
+    sum = add(sum, mine[i]);
   }
-  uint32_t incl = sum;
+  uint2 incl = sum;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const uint32_t other = __shfl_up(incl, d);
-    if (lane >= d) incl = min(incl + other, cap);
+    const uint2 other = make_uint2(__shfl_up(incl.x, d), __shfl_up(incl.y, d));
+    if (lane >= d) incl = add(incl, other);
   }
   if (lane == 63) wave_sums[wave] = incl;
   __syncthreads();
-  uint32_t before = __shfl_up(incl, 1);
-  if (lane == 0) before = 0;
-  uint32_t front = 0;
-  for (int w = 0; w < wave; ++w) front = min(front + wave_sums[w], cap);
-  before = min(before + front, cap);
+  uint2 before = make_uint2(__shfl_up(incl.x, 1), __shfl_up(incl.y, 1));
+  if (lane == 0) before = make_uint2(0, 0);
+  for (int w = 0; w < wave; ++w) before = add(before, wave_sums[w]);
 #pragma unroll
-  for (int i = 0; i < kMapPerThread; ++i) {
+  for (int i = 0; i < PER; ++i) {
     const int b = tid * per + i;
     if (i < per && b < B) {
-      prefix[b] = before;
-      before = min(before + mine[i], cap);
-      if (b == B - 1) prefix[B] = before;
+      x[b] = before.x, y[b] = before.y;
+      before = add(before, mine[i]);
+      if (b == B - 1) x[B] = before.x, y[B] = before.y;
     }
   }
   __syncthreads();
@@ -59,93 +59,165 @@ __device__ __forceinline__ int owner(const uint32_t* prefix, int B, uint32_t x) 
   return lo;
 }
 
-// Every workgroup forms the prefix sums of all sequences for itself (a few microseconds of one CU each, side by side, instead of a launch
-// in front) and then takes its share of the rows, of the new pages and of the sequences.
+// Every workgroup forms the prefix sums of all sequences for itself (side by side instead of a launch in front) and then takes its
+// share of the rows, of the new pages and of the sequences.  The pages are counted as if no row were cut off; where rows are, the
+// first sequence they are cut off from ends the count (`last_page`).  Bounded by its chain of latencies: lengths, sums, the
+// search for a row's sequence, its page.
+template <int PER>
 __global__ void __launch_bounds__(kMapThreads) page_map_kernel(PageMapArgs a) {
   __shared__ uint32_t row0[kMapMaxSeqs + 1];           // first row of every sequence
   __shared__ uint32_t page0[kMapMaxSeqs + 1];          // new pages of the sequences in front
-  __shared__ uint32_t wave_sums[kMapThreads / 64];
+  __shared__ uint32_t lens[kMapMaxSeqs];
+  __shared__ uint2 wave_sums[kMapThreads / 64];
+  __shared__ uint32_t cut_page;
   const int tid = threadIdx.x, P = a.page_size;
   const int shift = 31 - __builtin_clz(P);
-  const uint32_t capacity = (uint32_t)a.max_pages << shift;
+  const uint32_t capacity = (uint32_t)a.max_pages << shift, rows = (uint32_t)a.rows;
   const uint32_t avail = (uint32_t)min(a.free_capacity, max(0, a.free_count[0]));
-  auto length = [&](int b) { return min(capacity, (uint32_t)max(0, a.seqlens[b])); };
   auto pages = [&](uint32_t tokens) { return (tokens + P - 1) >> shift; };
-  prefix_sums(a.B, (uint32_t)a.rows, row0, wave_sums, [&](int b) { return (uint32_t)max(0, a.new_lens[b]); });
-  auto fitting = [&](int b, uint32_t len) { return min(row0[b + 1] - row0[b], capacity - len); };
-  auto wanted = [&](int b, uint32_t len) { return pages(len + fitting(b, len)) - pages(len); };
-  prefix_sums(a.B, 0x7fffffffu, page0, wave_sums, [&](int b) { return wanted(b, length(b)); });
-  // tokens of sequence b that have a place: page i of all new pages exists for i < avail
-  auto granted = [&](int b) { return min(page0[b + 1], avail) - min(page0[b], avail); };
-  auto placed = [&](int b, uint32_t len) { return min(fitting(b, len), ((pages(len) + granted(b)) << shift) - len); };
+  if (tid == 0) cut_page = 0xffffffffu;
+  prefix_sums<PER>(a.B, rows, row0, page0, wave_sums, [&](int b) {
+    const uint32_t len = min(capacity, (uint32_t)max(0, a.seqlens[b])), fresh = (uint32_t)max(0, a.new_lens[b]);
+    lens[b] = len;
+    return make_uint2(fresh, pages(len + min(fresh, capacity - len)) - pages(len));
+  });
+  auto fitting = [&](int b) { return min(row0[b + 1] - row0[b], capacity - lens[b]); };
+  if (row0[a.B] == rows) {                             // rows may have been cut off
+    for (int b = tid; b < a.B; b += kMapThreads)
+      if (row0[b] < rows && row0[b + 1] == rows) cut_page = page0[b] + pages(lens[b] + fitting(b)) - pages(lens[b]);
+    __syncthreads();
+  }
+  const uint32_t last_page = min(cut_page, avail);     // page i of all new pages exists for i < last_page
+  // tokens of sequence b that have a place
+  auto placed = [&](int b) {
+    const uint32_t granted = min(page0[b + 1], last_page) - min(page0[b], last_page);
+    return min(fitting(b), ((pages(lens[b]) + granted) << shift) - lens[b]);
+  };
   // page i of all new pages
   auto taken = [&](uint32_t i) { return a.free_pages[avail - 1 - i]; };
 
-  const uint32_t stride = gridDim.x * kMapThreads, first = blockIdx.x * kMapThreads + tid;
-  for (uint32_t r = first; r < (uint32_t)a.rows; r += stride) {
-    int slot = -1, position = 0;
-    if (r < row0[a.B]) {
-      const int b = owner(row0, a.B, r);
-      const uint32_t len = length(b), i = r - row0[b], p = len + i, j = p >> shift, old = pages(len);
-      position = (int)p;
-      if (i < placed(b, len)) {
-        // a page of this call comes from the stack: the table's entry is being written by another thread
-        const int page = j < old ? a.table[(size_t)b * a.max_pages + j] : taken(page0[b] + (j - old));
-        if (page >= 0 && page < a.n_pages) slot = (page << shift) + (int)(p & (P - 1));
+  const uint32_t threads = gridDim.x * kMapThreads, first = blockIdx.x * kMapThreads + tid;
+  const bool chunks = (((uintptr_t)a.slots | (uintptr_t)a.positions) & 15) == 0;
+  for (uint32_t r0 = first * kMapRows; r0 < rows; r0 += threads * kMapRows) {
+    int slot[kMapRows], position[kMapRows];
+    int b = r0 < row0[a.B] ? owner(row0, a.B, r0) : a.B;
+    uint32_t have = b < a.B ? placed(b) : 0;
+#pragma unroll
+    for (int e = 0; e < kMapRows; ++e) {
+      const uint32_t r = r0 + e;
+      slot[e] = -1, position[e] = 0;
+      if (b < a.B && r >= row0[b + 1]) {
+        do ++b; while (b < a.B && r >= row0[b + 1]);
+        have = b < a.B ? placed(b) : 0;
+      }
+      if (b < a.B) {
+        const uint32_t len = lens[b], i = r - row0[b], p = len + i, j = p >> shift, old = pages(len);
+        position[e] = (int)p;
+        if (i < have) {
+          // a page of this call comes from the stack: the table's entry is being written by another thread
+          const int page = j < old ? a.table[(size_t)b * a.max_pages + j] : taken(page0[b] + (j - old));
+          if (page >= 0 && page < a.n_pages) slot[e] = (page << shift) + (int)(p & (P - 1));
+        }
       }
     }
-    a.slots[r] = slot;
-    a.positions[r] = position;
-  }
-  const uint32_t total = min(page0[a.B], avail);
-  for (uint32_t i = first; i < total; i += stride) {
-    const int b = owner(page0, a.B, i);
-    a.table[(size_t)b * a.max_pages + pages(length(b)) + (i - page0[b])] = taken(i);
-  }
-  for (uint32_t b = first; b <= (uint32_t)a.B; b += stride) {
-    a.starts[b] = (int)row0[b];
-    if (b < (uint32_t)a.B) {
-      const uint32_t len = length(b);
-      a.seqlens_out[b] = (int)(len + placed(b, len));
+    if (chunks && r0 + kMapRows <= rows) {
+      *reinterpret_cast<int4*>(a.slots + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+      *reinterpret_cast<int4*>(a.positions + r0) = make_int4(position[0], position[1], position[2], position[3]);
     } else {
-      a.free_count_out[0] = (int)(avail - total);
+#pragma unroll
+      for (int e = 0; e < kMapRows; ++e)
+        if (r0 + e < rows) a.slots[r0 + e] = slot[e], a.positions[r0 + e] = position[e];
     }
+  }
+  const uint32_t total = min(page0[a.B], last_page);
+  for (uint32_t i = first; i < total; i += threads) {
+    const int b = owner(page0, a.B, i);
+    a.table[(size_t)b * a.max_pages + pages(lens[b]) + (i - page0[b])] = taken(i);
+  }
+  for (uint32_t b = first; b <= (uint32_t)a.B; b += threads) {
+    a.starts[b] = (int)row0[b];
+    if (b < (uint32_t)a.B) a.seqlens_out[b] = (int)(lens[b] + placed(b));
+    else a.free_count_out[0] = (int)(avail - total);
   }
 }
 
-__global__ void __launch_bounds__(kMapThreads) page_release_kernel(PageReleaseArgs a) {
-  __shared__ uint32_t page0[kMapMaxSeqs + 1];          // pages put back by the sequences in front
-  __shared__ uint32_t wave_sums[kMapThreads / 64];
+constexpr int kReleaseThreads = 1024;
+
+// One workgroup: most sequences stay, so those that end are listed first, in order; a wavefront then takes every 16th of them, once to
+// count its pages and once to put them on the stack behind those of the sequences in front.
+__global__ void __launch_bounds__(kReleaseThreads) page_release_kernel(PageReleaseArgs a) {
+  constexpr int kWaves = kReleaseThreads / 64;
+  __shared__ int ending[kMapMaxSeqs];
+  __shared__ uint32_t to_stack[kMapMaxSeqs];           // pages that go back, then their sums in front
+  __shared__ uint32_t wave_sums[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, P = a.page_size;
   const int shift = 31 - __builtin_clz(P);
   const uint32_t capacity = (uint32_t)a.max_pages << shift;
   const uint32_t have = (uint32_t)min(a.free_capacity, max(0, a.free_count[0]));
-  auto held = [&](int b) { return (min(capacity, (uint32_t)max(0, a.seqlens[b])) + P - 1) >> shift; };
-  auto valid = [&](int page) { return page >= 0 && page < a.n_pages; };
-  // pages whose entries name none are not put back: a sequence's count is that of its good entries
-  for (int b = wave; b < a.B; b += kMapThreads / 64) {
-    uint32_t n = 0;
-    if (a.drop[b] != 0)
-      for (uint32_t j = lane; j < held(b); j += 64) n += valid(a.table[(size_t)b * a.max_pages + j]);
-    for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
-    if (lane == 0) page0[b] = n;
+  const unsigned long long below = (1ull << lane) - 1;
+  // 16 wavefronts' counts to the sum in front of this one's, and of all
+  auto sums = [&](uint32_t mine, uint32_t& front, uint32_t& all) {
+    __syncthreads();
+    if (lane == 0) wave_sums[wave] = mine;
+    __syncthreads();
+    front = all = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) front += wave_sums[w];
+      all += wave_sums[w];
+    }
+  };
+  uint32_t n = 0, front, all;
+  for (int b0 = 0; b0 < a.B; b0 += kReleaseThreads) {
+    const int b = b0 + tid;
+    const bool drop = b < a.B && a.drop[b] != 0;
+    if (b < a.B) a.seqlens_out[b] = drop ? 0 : a.seqlens[b];
+    const unsigned long long who = __ballot(drop);
+    sums((uint32_t)__popcll(who), front, all);
+    if (drop) ending[n + front + __popcll(who & below)] = b;
+    n += all;
   }
   __syncthreads();
-  prefix_sums(a.B, 0x7fffffffu, page0, wave_sums, [&](int b) { return page0[b]; });
-  for (int b = wave; b < a.B; b += kMapThreads / 64) {
-    const bool drop = a.drop[b] != 0;
-    const uint32_t n = drop ? held(b) : 0u;
-    uint32_t at = have + page0[b];
-    for (uint32_t j0 = 0; j0 < n; j0 += 64) {
-      const int page = j0 + lane < n ? a.table[(size_t)b * a.max_pages + j0 + lane] : -1;
-      const unsigned long long good = __ballot(valid(page));
-      const uint32_t to = at + __popcll(good & ((1ull << lane) - 1));
-      if (valid(page) && to < (uint32_t)a.free_capacity) a.free_pages[to] = page;
+  auto held = [&](int b) { return (min(capacity, (uint32_t)max(0, a.seqlens[b])) + P - 1) >> shift; };
+  // entries that name no page are not put back
+  auto page_of = [&](int b, uint32_t j, uint32_t pages) {
+    const int page = j < pages ? a.table[(size_t)b * a.max_pages + j] : -1;
+    return page < a.n_pages ? page : -1;
+  };
+  for (uint32_t i = wave; i < n; i += kWaves) {
+    const int b = ending[i];
+    const uint32_t pages = held(b);
+    uint32_t good = 0;
+    for (uint32_t j0 = 0; j0 < pages; j0 += 64) good += __popcll(__ballot(page_of(b, j0 + lane, pages) >= 0));
+    if (lane == 0) to_stack[i] = good;
+  }
+  __syncthreads();
+  uint32_t total = 0;
+  for (uint32_t i0 = 0; i0 < n; i0 += kReleaseThreads) {
+    const uint32_t i = i0 + tid, mine = i < n ? to_stack[i] : 0u;
+    uint32_t incl = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t other = __shfl_up(incl, d);
+      if (lane >= d) incl += other;
+    }
+    sums(__shfl(incl, 63), front, all);
+    if (i < n) to_stack[i] = total + front + incl - mine;
+    total += all;
+  }
+  __syncthreads();
+  for (uint32_t i = wave; i < n; i += kWaves) {
+    const int b = ending[i];
+    const uint32_t pages = held(b);
+    uint32_t at = have + to_stack[i];
+    for (uint32_t j0 = 0; j0 < pages; j0 += 64) {
+      const int page = page_of(b, j0 + lane, pages);
+      const unsigned long long good = __ballot(page >= 0);
+      const uint32_t to = at + __popcll(good & below);
+      if (page >= 0 && to < (uint32_t)a.free_capacity) a.free_pages[to] = page;
       at += __popcll(good);
     }
-    if (lane == 0) a.seqlens_out[b] = drop ? 0 : a.seqlens[b];
   }
-  if (tid == 0) a.free_count_out[0] = (int)min((uint32_t)a.free_capacity, have + page0[a.B]);
+  if (tid == 0) a.free_count_out[0] = (int)min((uint32_t)a.free_capacity, have + total);
 }
 
 constexpr int kAppendRowThreads = 128;
@@ -182,7 +254,7 @@ __global__ void __launch_bounds__(kAppendRowThreads) paged_append_kernel(PagedAp
 }
 
 // The same in 16-byte chunks (thrift_rotary.h): the query heads of a row, then its key heads, then its value heads, which are copied.
-template <typename T, int LAYOUT>
+template <typename T, int LAYOUT, bool STREAM>
 __global__ void __launch_bounds__(kHeadThreads) paged_append_items_kernel(PagedAppendArgs a, HeadShape z) {
   __shared__ float2 table[kAngles];
   const int tid = threadIdx.x, half = a.rot / 2;
@@ -201,7 +273,7 @@ __global__ void __launch_bounds__(kHeadThreads) paged_append_items_kernel(PagedA
   int h = busy ? split * z.lanes + group : heads;
   auto load = [&](int i, v4i (&c)[2]) {
     const uint16_t* p = i < a.Hq ? q + i * a.qh : i < turned ? k + (i - a.Hq) * a.kh : v + (i - turned) * a.vh;
-    c[0] = *reinterpret_cast<const v4i*>(p + it.at[0]), c[1] = *reinterpret_cast<const v4i*>(p + it.at[1]);
+    c[0] = chunk_from<false>(p + it.at[0]), c[1] = chunk_from<false>(p + it.at[1]);
   };
   v4i c[2];
   if (h < heads) load(h, c);                 // on its way while the angles are formed
@@ -222,7 +294,7 @@ __global__ void __launch_bounds__(kHeadThreads) paged_append_items_kernel(PagedA
     v4i next[2];
     if (h < heads) load(h, next);
     if (!value) turn_item<T, LAYOUT>(it, c, cs);
-    *reinterpret_cast<v4i*>(p + it.at[0]) = c[0], *reinterpret_cast<v4i*>(p + it.at[1]) = c[1];
+    chunk_to<STREAM>(p + it.at[0], c[0]), chunk_to<STREAM>(p + it.at[1], c[1]);
     c[0] = next[0], c[1] = next[1];
   }
 }
@@ -236,20 +308,28 @@ void launch_append(const PagedAppendArgs& a, hipStream_t st) {
   }
   const HeadShape z = head_shape(a.T, a.Hq + 2 * a.Hkv, a.D, a.rot);
   const dim3 grid((unsigned)((a.T + z.tokens - 1) / z.tokens * z.splits)), block(kHeadThreads);
-  if (a.layout == THRIFT_ROPE_HALF) paged_append_items_kernel<T, THRIFT_ROPE_HALF><<<grid, block, 0, st>>>(a, z);
-  else paged_append_items_kernel<T, THRIFT_ROPE_INTERLEAVED><<<grid, block, 0, st>>>(a, z);
+  // Written past the caches where a store fills lines: 78.4 -> 71.8 us for 8192 rows of 64/8 heads of 128 channels, 167.7 -> 157.0 for 32768 of 32/8
+  const bool stream = a.D >= 128;
+#define THRIFT_APPEND(L_)                                                                    \
+  if (stream) paged_append_items_kernel<T, L_, true><<<grid, block, 0, st>>>(a, z);          \
+  else paged_append_items_kernel<T, L_, false><<<grid, block, 0, st>>>(a, z)
+  if (a.layout == THRIFT_ROPE_HALF) { THRIFT_APPEND(THRIFT_ROPE_HALF); }
+  else { THRIFT_APPEND(THRIFT_ROPE_INTERLEAVED); }
+#undef THRIFT_APPEND
 }
 
 }  // namespace
 
 void launch_page_map(const PageMapArgs& a, hipStream_t st) {
-  const long items = a.rows > a.B ? a.rows : a.B;
+  const long items = a.rows / kMapRows > a.B ? a.rows / kMapRows : a.B;
   const long blocks = (items + kMapThreads - 1) / kMapThreads;
-  page_map_kernel<<<dim3((unsigned)(blocks < 256 ? blocks : 256)), dim3(kMapThreads), 0, st>>>(a);
+  const dim3 grid((unsigned)(blocks < 256 ? blocks : 256)), block(kMapThreads);
+  if (a.B <= kMapThreads) page_map_kernel<1><<<grid, block, 0, st>>>(a);
+  else page_map_kernel<kMapMaxSeqs / kMapThreads><<<grid, block, 0, st>>>(a);
 }
 
 void launch_page_release(const PageReleaseArgs& a, hipStream_t st) {
-  page_release_kernel<<<dim3(1), dim3(kMapThreads), 0, st>>>(a);
+  page_release_kernel<<<dim3(1), dim3(kReleaseThreads), 0, st>>>(a);
 }
 
 void launch_paged_append(const PagedAppendArgs& a, thrift_dtype dt, hipStream_t st) {

@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs a) {
   }
 }
 
-template <typename T, int LAYOUT>
+template <typename T, int LAYOUT, bool STREAM>
 __global__ void __launch_bounds__(kHeadThreads) rope_items_kernel(RopeArgs a, HeadShape z) {
   __shared__ float2 table[kAngles];
   const int tid = threadIdx.x, half = a.rot / 2, all = a.B * a.N;
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kHeadThreads) rope_items_kernel(RopeArgs a, He
   auto load = [&](int head, v4i (&c)[2]) {
     const int s = head >= a.side[0].heads, i = head - (s ? a.side[0].heads : 0);
     const uint16_t* p = x[s] + i * a.side[s].xh;
-    c[0] = *reinterpret_cast<const v4i*>(p + it.at[0]), c[1] = *reinterpret_cast<const v4i*>(p + it.at[1]);
+    c[0] = chunk_from<STREAM>(p + it.at[0]), c[1] = chunk_from<STREAM>(p + it.at[1]);
   };
   v4i c[2];
   if (h < heads) load(h, c);                 // on its way while the angles are formed
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(kHeadThreads) rope_items_kernel(RopeArgs a, He
     v4i next[2];
     if (h < heads) load(h, next);
     turn_item<T, LAYOUT>(it, c, cs);
-    *reinterpret_cast<v4i*>(p + it.at[0]) = c[0], *reinterpret_cast<v4i*>(p + it.at[1]) = c[1];
+    chunk_to<STREAM>(p + it.at[0], c[0]), chunk_to<STREAM>(p + it.at[1], c[1]);
     c[0] = next[0], c[1] = next[1];
   }
 }
@@ -100,8 +100,16 @@ void launch(const RopeArgs& a, hipStream_t st) {
   }
   const HeadShape z = head_shape(tokens, a.side[0].heads + a.side[1].heads, a.D, a.rot);
   const dim3 grid((unsigned)((tokens + z.tokens - 1) / z.tokens * z.splits)), block(kHeadThreads);
-  if (a.layout == THRIFT_ROPE_HALF) rope_items_kernel<T, THRIFT_ROPE_HALF><<<grid, block, 0, st>>>(a, z);
-  else rope_items_kernel<T, THRIFT_ROPE_INTERLEAVED><<<grid, block, 0, st>>>(a, z);
+  // Past the caches where they cannot hold inputs and results (256 MiB; twice that here, up to which the two were equal or the cached
+  // form faster: 44 and 49 us for 268 MB, 65 and 65 for 336, 142 and 131 for 671, 538 and 499 for 2.7 GB) and where a store fills lines (heads of
+  // 64 channels: 88 and 98 us for 409 MB).
+  const bool stream = 4L * tokens * (a.side[0].heads + a.side[1].heads) * a.D > (512L << 20) && a.D >= 128;
+#define THRIFT_ROPE(L_)                                                              \
+  if (stream) rope_items_kernel<T, L_, true><<<grid, block, 0, st>>>(a, z);          \
+  else rope_items_kernel<T, L_, false><<<grid, block, 0, st>>>(a, z)
+  if (a.layout == THRIFT_ROPE_HALF) { THRIFT_ROPE(THRIFT_ROPE_HALF); }
+  else { THRIFT_ROPE(THRIFT_ROPE_INTERLEAVED); }
+#undef THRIFT_ROPE
 }
 
 }  // namespace

@@ -89,6 +89,17 @@ struct Item {
   }
 };
 
+// 16 bytes, past the caches where STREAM
+template <bool STREAM>
+__device__ __forceinline__ v4i chunk_from(const uint16_t* p) {
+  return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p)) : *reinterpret_cast<const v4i*>(p);
+}
+template <bool STREAM>
+__device__ __forceinline__ void chunk_to(uint16_t* p, v4i x) {
+  if (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<v4i*>(p));
+  else *reinterpret_cast<v4i*>(p) = x;
+}
+
 template <typename T>
 __device__ __forceinline__ void turn_pair(uint32_t x0, uint32_t x1, float2 cs, uint32_t& y0, uint32_t& y1) {
   float a, b;
