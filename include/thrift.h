@@ -413,7 +413,8 @@ thrift_status thrift_rope(const void* q, const int64_t* q_strides, void* q_out, 
                           int B, int N, int D, void* stream);
 
 /* Gradient of thrift_rope with respect to its inputs: the transposed rotation of the gradients of its outputs (the angle's sign
- * turned, the same gain).  q, k: gradients of q_out, k_out; q_out, k_out: gradients of q, k.  Arguments as thrift_rope. */
+ * turned, the same gain).  q, k: gradients of q_out, k_out; q_out, k_out: gradients of q, k, one per element (of an input that was
+ * repeated, the caller adds them up).  Arguments as thrift_rope. */
 thrift_status thrift_rope_backward(const void* q, const int64_t* q_strides, void* q_out, const int64_t* q_out_strides, int Hq,
                                    const void* k, const int64_t* k_strides, void* k_out, const int64_t* k_out_strides, int Hkv, thrift_dtype dt,
                                    const int32_t* positions, int64_t positions_stride, const double* freqs, int rot, int layout, float gain,
@@ -483,6 +484,7 @@ size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int 
  *     k_pages and v_pages (clamped to 0 .. n_pages - 1).
  *   softmax_scale <= 0 selects 1/sqrt(D)
  *   out [B,Hq,D] in out_dt; lse (nullable) [B,Hq] fp32: log-sum-exp of the scaled scores, -inf for length 0
+ *   q, k_pages, v_pages and out are 16-byte aligned, otherwise THRIFT_ERR_SHAPE
  *   workspace: thrift_paged_decode_workspace(...) bytes, 16-byte aligned; the next call on the same stream may use it again
  */
 thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,

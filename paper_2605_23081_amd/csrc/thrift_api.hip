@@ -740,6 +740,7 @@ thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_
   if (!q || !k_pages || !v_pages || !block_table || !seqlens || !out) return THRIFT_ERR_NULL;
   if (!is16(dt) || !is_out(out_dt)) return THRIFT_ERR_DTYPE;
   if (!paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) || !fits_int(n_pages, page_size)) return THRIFT_ERR_SHAPE;
+  if ((((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)out) & 15) != 0) return THRIFT_ERR_SHAPE;
   const size_t need = paged_decode_workspace(Hq, Hkv, D);
   if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15) != 0) return THRIFT_ERR_WORKSPACE;
   if (thrift_status s = check_arch()) return s;

@@ -103,10 +103,10 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
   int u = 0, u_end = 0, each = 0, window = 0, lens;         // lens: length of sequence window + lane
   Step cur;
   {
-    int n = a.B, base = 0, b = 0;
+    int n = a.B, per, base = 0, b = 0;
     bool first = true;
     do {                                   // 64 parts of what is left; the part with step u; once more inside it
-      const int per = (n + 63) / 64;
+      per = (n + 63) / 64;
       int sum = 0;
       for (int i = 0; i < per; ++i) {
         const int at = lane * per + i;
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
       window = b;
       b += at * per;
       n = min(per, n - at * per);
-    } while (n > 1);
+    } while (per > 1);                     // the last round has a sequence per lane: its lengths are kept
     // wavefront-uniform, and known to be: descriptors of loads are scalar
     u = __builtin_amdgcn_readfirstlane(u), u_end = __builtin_amdgcn_readfirstlane(u_end);
     window = __builtin_amdgcn_readfirstlane(window), base = __builtin_amdgcn_readfirstlane(base);

@@ -275,6 +275,38 @@ def test_ragged_and_long_sequences(T, B, Hq, Hkv, top, dtype):
     _check_attention(T, _randn(B, Hq, 128, dtype=dtype, seed=4), kp, vp, table, lens)
 
 
+def _few_lengths(B, kind):
+    if kind == "one far behind":                          # nothing in front of it
+        return [0] * (B - 2) + [40, 0]
+    if kind == "the last":
+        return [0] * (B - 1) + [41]
+    if kind == "gaps":                                    # some sequences with tokens, hundreds without between them
+        return [(33 if b % 700 in (5, 6) else 0) for b in range(B)]
+    return [(b * 7) % 41 for b in range(B)]               # all kinds of short ones
+
+
+@pytest.mark.parametrize("B", [64, 65, 129, 4096, 4097, 9000])
+@pytest.mark.parametrize("kind", ["one far behind", "the last", "gaps", "short"])
+def test_many_sequences(T, B, kind):
+    lens = _few_lengths(B, kind)
+    print(f"many sequences B={B} {kind}", flush=True)
+    page, Hkv, D = 16, 1, 64
+    k, v = _randn(8, Hkv, page, D, dtype=torch.float16), _randn(8, Hkv, page, D, dtype=torch.float16, seed=1)
+    table = (torch.arange(B * 3, device="cuda").view(B, 3) * 5 % 8).to(I32)
+    q = _randn(B, 2, D, dtype=torch.float16, seed=2)
+    got, lse = T.thrift_paged_decode(q, k, v, table, _ints(lens), out_dtype=torch.float32, return_lse=True)
+    n = torch.tensor(lens, device="cuda")
+    keys, values = (p[table.long()].transpose(1, 2).reshape(B, 3 * page, D).double() for p in (k, v))
+    s = torch.bmm(q.double(), keys.transpose(1, 2).contiguous()) / math.sqrt(D)
+    s = s.masked_fill(torch.arange(3 * page, device="cuda") >= n.view(B, 1, 1), -math.inf)
+    live = n > 0
+    want = torch.bmm(torch.softmax(s[live], -1), values[live])
+    # as in attention64: scores of 64 products below 30, 40 keys
+    assert bool(((got[live].double() - want).abs() <= 2 ** -15 * values.abs().amax()).all())
+    assert bool(((lse[live].double() - torch.logsumexp(s[live], -1)).abs() <= 2 ** -15).all())
+    assert bool((got[~live] == 0).all()) and bool((lse[~live] == -math.inf).all())
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("gain", [0.01, 30.0])
 def test_flat_and_peaked_scores(T, dtype, gain):

@@ -108,9 +108,11 @@ def test_page_calls_refuse_before_a_launch():
     for bad in (dict(B=0), dict(Hq=0), dict(Hkv=0), dict(Hq=5), dict(Hq=66), dict(D=96), dict(D=512), dict(ps=8), dict(ps=20), dict(mp=0), dict(n=0),
                 dict(n=1 << 28), dict(mp=1 << 28), dict(B=1 << 20, Hq=32, Hkv=8)):
         assert decode(**bad) == SHAPE, bad
+    for bad in ("q", "kp", "vp", "out"):
+        assert decode(**{bad: C.c_void_p(0x1008)}) == SHAPE, bad
     need = L.thrift_paged_decode_workspace(2, 4, 2, 8, 16, 128)
-    if need:
-        assert decode(ws=None) == WORKSPACE and decode(size=need - 1) == WORKSPACE and decode(ws=C.c_void_p(0x1008)) == WORKSPACE
+    assert need > 0
+    assert decode(ws=None) == WORKSPACE and decode(size=need - 1) == WORKSPACE and decode(ws=C.c_void_p(0x1008)) == WORKSPACE
     assert L.thrift_paged_decode_workspace(2, 5, 2, 8, 16, 128) == 0 and L.thrift_paged_decode_workspace(2, 4, 2, 8, 16, 96) == 0
     if not torch.cuda.is_available():
         assert page_map() == ARCH and release() == ARCH and append() == ARCH and append(q=None, qo=None, Hq=0) == ARCH and decode() == ARCH
