@@ -29,7 +29,7 @@ constexpr int kThreads = 256;              // of the merge
 // heads: 74.1 -> 70.2 us); 64 channels: eight with as much were slower than four (23.6 -> 25.1 us).
 constexpr int waves_of(int D) { return D == 256 ? 2 : 4; }
 constexpr int kStep = 32;                  // keys per step of a wavefront
-constexpr float kShift = 15.f;
+constexpr float kShift = 15.f, kLn2 = 0.6931471805599453f;
 // One workgroup per CU: its four wavefronts have 64 KiB on their way, 16 MiB on the chip.  More of them ask for more than the memory takes at a
 // time, and what waits in front of it is served unevenly.
 constexpr int kShares = kCus;
@@ -85,19 +85,211 @@ struct Step {
   int b, hk, t, len, steps;                // sequence, KV head, number in the row; the sequence's length and steps
 };
 
+__device__ __forceinline__ int length_of(const PagedDecodeArgs& a, const Launch& z, int n) { return min(a.max_pages << z.shift, max(0, n)); }
+__device__ __forceinline__ int steps_of(int len) { return (len + kStep - 1) / kStep; }
+
+// What a wavefront holds of a row, and its steps
+template <typename T, int D, int NB>
+struct Walk {
+  static constexpr int KS = D / 32;        // 16-byte pieces of a key's row per lane
+  static constexpr int VC = D / 16;        // channels of a value's row per lane
+  static constexpr int NR = NB * (VC * 4 + 2);                   // registers of a state
+  static constexpr int kStream = 2;        // non-temporal: keys and values are read once
+  int lane, col, grp;
+  v4i q[NB][KS], q_next[NB][KS], k[2][KS];
+  uint32_t v[8][VC / 2];
+  v4f o[NB][VC];                           // o [D] of one head is spread over the four lanes of its column: element r of tile j is channel(r, j)
+  float m[NB], l[NB];                      // maximum less 15; this lane's part of the sum
+  // Loads of 16 keys go through a descriptor of their page's rows up to the length: what lies behind reads as 0 and is not fetched, and
+  // a step that does not exist has none.
+  __amdgpu_buffer_rsrc_t kd[2], vd[2];
+  int page[2];                             // of a step that is described later: a load of its own in front of the loads
+
+  __device__ __forceinline__ Walk() : lane(threadIdx.x & 63), col(lane & 15), grp(lane >> 4) {}
+  __device__ __forceinline__ int channel(int r, int j) const { return (j >> 3) * 128 + (4 * grp + r) * min(VC, 8) + (j & 7); }
+
+  __device__ __forceinline__ void look_up(const PagedDecodeArgs& a, const Launch& z, const Step& s) {
+    const scalar_ints table = scalar(a.table + (size_t)s.b * a.max_pages);
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) page[sub] = table[min(a.max_pages - 1, (s.t * kStep + 16 * sub) >> z.shift)];
+  }
+  __device__ __forceinline__ void describe(const PagedDecodeArgs& a, const Launch& z, const Step& s, bool there) {
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      const int key = s.t * kStep + 16 * sub, rows = __builtin_amdgcn_readfirstlane(there ? min(16, max(0, s.len - key)) : 0);
+      const int p = __builtin_amdgcn_readfirstlane(min(a.n_pages - 1, max(0, page[sub])));
+      const size_t at = ((((size_t)p * a.Hkv + s.hk) << z.shift) + (key & ((1 << z.shift) - 1))) * D;
+      kd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_pages + at), 0, rows * D * 2, 0x00020000);
+      vd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_pages + at), 0, rows * D * 2, 0x00020000);
+    }
+  }
+  __device__ __forceinline__ void load_q(const PagedDecodeArgs& a, const Launch& z, const Step& s, bool there) {
+    const uint16_t* qp = a.q + ((size_t)s.b * a.Hkv + s.hk) * z.G * D;
+    const __amdgpu_buffer_rsrc_t qd = __builtin_amdgcn_make_buffer_rsrc((void*)qp, 0, there ? z.G * D * 2 : 0, 0x00020000);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < KS; ++e)
+        q_next[nb][e] = __builtin_amdgcn_raw_buffer_load_b128(qd, (col + 16 * nb) * D * 2 + 64 * e + 16 * grp, 0, 0);
+  }
+  __device__ __forceinline__ void next_q() {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < KS; ++e) q[nb][e] = q_next[nb][e];
+  }
+  __device__ __forceinline__ void load_k() {
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+      for (int e = 0; e < KS; ++e) k[sub][e] = __builtin_amdgcn_raw_buffer_load_b128(kd[sub], col * D * 2 + 16 * grp + 64 * e, 0, kStream);
+  }
+  __device__ __forceinline__ void load_v() {
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const int from = 4 * grp * D * 2 + 2 * min(VC, 8) * col + (r & 3) * D * 2;
+      if constexpr (VC == 4) {
+        const v2i x = __builtin_amdgcn_raw_buffer_load_b64(vd[r >> 2], from, 0, kStream);
+        v[r][0] = x[0], v[r][1] = x[1];
+      } else {
+#pragma unroll
+        for (int e = 0; e < VC / 8; ++e) {
+          const v4i x = __builtin_amdgcn_raw_buffer_load_b128(vd[r >> 2], from + 256 * e, 0, kStream);
+#pragma unroll
+          for (int d = 0; d < 4; ++d) v[r][4 * e + d] = x[d];
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      m[nb] = -__FLT_MAX__, l[nb] = 0.f;   // a number: scores of -inf then have weight 0
+#pragma unroll
+      for (int j = 0; j < VC; ++j) o[nb][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // One step, of which the row has `behind` keys from its first on; `ask` when the keys' registers are free
+  template <typename F>
+  __device__ __forceinline__ void step(float c, int behind, F ask) {
+    float x[NB][8];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        v4f s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < KS; ++e) s = Mma<T>::mma(k[sub][e], q[nb][e], s);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[nb][4 * sub + r] = s[r] * c;
+      }
+    ask();
+    v4i high[NB], low[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if (behind < kStep) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if ((r < 4 ? 0 : 12) + 4 * grp + r >= behind) x[nb][r] = -__builtin_inff();
+      }
+      const float (&y)[8] = x[nb];
+      const float top = over_groups_max(fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])))) - kShift;
+      if (__ballot(top > m[nb])) {
+        const float grown = fmaxf(top, m[nb]), keep = fast_exp2(m[nb] - grown);
+        m[nb] = grown;
+        l[nb] *= keep;
+#pragma unroll
+        for (int j = 0; j < VC; ++j) o[nb][j] *= keep;
+      }
+      uint16_t hi[8], lo[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float p = fast_exp2(y[r] - m[nb]);
+        l[nb] += p;
+        hi[r] = T::from_float(p);
+        lo[r] = T::from_float(p - T::to_float(hi[r]));
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        high[nb][r] = (int)((uint32_t)hi[2 * r] | ((uint32_t)hi[2 * r + 1] << 16));
+        low[nb][r] = (int)((uint32_t)lo[2 * r] | ((uint32_t)lo[2 * r + 1] << 16));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < VC; ++j) {
+      v4i y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = (int)__builtin_amdgcn_perm(v[2 * r + 1][j / 2], v[2 * r][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        o[nb][j] = Mma<T>::mma(y, high[nb], o[nb][j]);
+        o[nb][j] = Mma<T>::mma(y, low[nb], o[nb][j]);
+      }
+    }
+  }
+
+  // The state in LDS, a lane's registers in its column, and the addition of another
+  __device__ __forceinline__ void give(float (*to)[64]) const {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float (*p)[64] = to + nb * (VC * 4 + 2);
+#pragma unroll
+      for (int j = 0; j < VC; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[4 * j + r][lane] = o[nb][j][r];
+      p[4 * VC][lane] = m[nb], p[4 * VC + 1][lane] = l[nb];
+    }
+  }
+  __device__ __forceinline__ void take(float (*from)[64]) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      float (*p)[64] = from + nb * (VC * 4 + 2);
+      const float other = p[4 * VC][lane], top = fmaxf(m[nb], other), k1 = fast_exp2(m[nb] - top), k2 = fast_exp2(other - top);
+      m[nb] = top;
+      l[nb] = l[nb] * k1 + p[4 * VC + 1][lane] * k2;
+#pragma unroll
+      for (int j = 0; j < VC; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[nb][j][r] = o[nb][j][r] * k1 + p[4 * j + r][lane] * k2;
+    }
+  }
+  // The state as the row's result, or as a part of it in `slot`
+  __device__ __forceinline__ void put(const PagedDecodeArgs& a, const Launch& z, const Step& s, bool whole, size_t slot) const {
+    const size_t row = (size_t)s.b * a.Hkv + s.hk;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int head = col + 16 * nb;
+      const float sum = over_groups_sum(l[nb]), inv = 1.f / sum;
+      if (head >= z.G) continue;
+      if (whole) {
+        const size_t to = row * z.G + head;
+        if (a.lse != nullptr && grp == 0) a.lse[to] = kLn2 * (m[nb] + __builtin_log2f(sum));
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < VC; j += 4)
+            store_out4(a.out, a.out_dt, to * D + channel(r, j), o[nb][j][r] * inv, o[nb][j + 1][r] * inv, o[nb][j + 2][r] * inv, o[nb][j + 3][r] * inv);
+      } else {
+        const size_t to = slot * z.G + head;
+        if (grp == 0) z.w.part_ml[2 * to] = m[nb], z.w.part_ml[2 * to + 1] = sum;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int j = 0; j < VC; j += 4)
+            *reinterpret_cast<v4f*>(z.w.part_o + to * D + channel(r, j)) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]};
+      }
+    }
+  }
+};
+
 template <typename T, int D, int NB>
 __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged_decode_kernel(PagedDecodeArgs a, Launch z) {
   constexpr int kWaves = waves_of(D);
-  constexpr int KS = D / 32;               // 16-byte pieces of a key's row per lane
-  constexpr int VC = D / 16;               // channels of a value's row per lane
-  constexpr int NR = NB * (VC * 4 + 2);    // registers of a state
-  __shared__ float parts[kWaves][NR][64];  // a wavefront's part of a row that an earlier one has begun
+  using W = Walk<T, D, NB>;
+  __shared__ float parts[kWaves][W::NR][64];                     // a wavefront's part of a row that an earlier one has begun
   __shared__ int ended[kWaves];            // whether the row ends with that part
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 15, grp = lane >> 4;
-  const int capacity = a.max_pages << z.shift;
-  auto length = [&](int n) { return min(capacity, max(0, n)); };
-  auto steps_of = [&](int len) { return (len + kStep - 1) / kStep; };
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
 
   // ---- this workgroup's share, steps u .. u_end - 1, and the first one's place ----
   int u = 0, u_end = 0, each = 0, window = 0, lens;         // lens: length of sequence window + lane
@@ -110,7 +302,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
       int sum = 0;
       for (int i = 0; i < per; ++i) {
         const int at = lane * per + i;
-        lens = b + at < a.B ? length(a.seqlens[b + at]) : 0;     // the last round's reach past its part: the sequences that follow
+        lens = b + at < a.B ? length_of(a, z, a.seqlens[b + at]) : 0;     // the last round's reach past its part: the sequences that follow
         if (at < n) sum += a.Hkv * steps_of(lens);
       }
       int incl = sum;
@@ -157,138 +349,12 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
         break;
       }
       window += 64, s.b = window - 1;
-      lens = window + lane < a.B ? length(a.seqlens[window + lane]) : 0;
+      lens = window + lane < a.B ? length_of(a, z, a.seqlens[window + lane]) : 0;
     }
     s.steps = steps_of(s.len);
   };
 
-  v4i q[NB][KS], q_next[NB][KS], k[2][KS];
-  uint32_t v[8][VC / 2];
-  // Loads of 16 keys go through a descriptor of their page's rows up to the length: what lies behind reads as 0 and is not fetched, and
-  // a step that does not exist has none.
-  __amdgpu_buffer_rsrc_t kd[2], vd[2];
-  int page[2];                             // of a step that is described later: a load of its own in front of the loads
-  auto look_up = [&](const Step& s) {
-    const scalar_ints table = scalar(a.table + (size_t)s.b * a.max_pages);
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) page[sub] = table[min(a.max_pages - 1, (s.t * kStep + 16 * sub) >> z.shift)];
-  };
-  auto describe = [&](const Step& s, bool there) {
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
-      const int key = s.t * kStep + 16 * sub, rows = __builtin_amdgcn_readfirstlane(there ? min(16, max(0, s.len - key)) : 0);
-      const int p = __builtin_amdgcn_readfirstlane(min(a.n_pages - 1, max(0, page[sub])));
-      const size_t at = ((((size_t)p * a.Hkv + s.hk) << z.shift) + (key & ((1 << z.shift) - 1))) * D;
-      kd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_pages + at), 0, rows * D * 2, 0x00020000);
-      vd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_pages + at), 0, rows * D * 2, 0x00020000);
-    }
-  };
-  auto load_q = [&](const Step& s, bool there) {
-    const uint16_t* qp = a.q + ((size_t)s.b * a.Hkv + s.hk) * z.G * D;
-    const __amdgpu_buffer_rsrc_t qd = __builtin_amdgcn_make_buffer_rsrc((void*)qp, 0, there ? z.G * D * 2 : 0, 0x00020000);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int e = 0; e < KS; ++e)
-        q_next[nb][e] = __builtin_amdgcn_raw_buffer_load_b128(qd, (col + 16 * nb) * D * 2 + 64 * e + 16 * grp, 0, 0);
-  };
-  auto next_q = [&]() {
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int e = 0; e < KS; ++e) q[nb][e] = q_next[nb][e];
-  };
-  constexpr int kStream = 2;               // non-temporal: keys and values are read once
-  const int k_lane = col * D * 2 + 16 * grp, v_lane = 4 * grp * D * 2 + 2 * min(VC, 8) * col;
-  auto load_k = [&]() {
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-      for (int e = 0; e < KS; ++e) k[sub][e] = __builtin_amdgcn_raw_buffer_load_b128(kd[sub], k_lane + 64 * e, 0, kStream);
-  };
-  auto load_v = [&]() {
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const int from = v_lane + (r & 3) * D * 2;
-      if constexpr (VC == 4) {
-        const v2i x = __builtin_amdgcn_raw_buffer_load_b64(vd[r >> 2], from, 0, kStream);
-        v[r][0] = x[0], v[r][1] = x[1];
-      } else {
-#pragma unroll
-        for (int e = 0; e < VC / 8; ++e) {
-          const v4i x = __builtin_amdgcn_raw_buffer_load_b128(vd[r >> 2], from + 256 * e, 0, kStream);
-#pragma unroll
-          for (int d = 0; d < 4; ++d) v[r][4 * e + d] = x[d];
-        }
-      }
-    }
-  };
-
-  v4f o[NB][VC];                           // o [D] of one head is spread over the four lanes of its column: element r of tile j is channel(r, j)
-  auto channel = [&](int r, int j) { return (j >> 3) * 128 + (4 * grp + r) * min(VC, 8) + (j & 7); };
-  float m[NB], l[NB];                      // maximum less 15; this lane's part of the sum
-  auto clear = [&]() {
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      m[nb] = -__builtin_inff(), l[nb] = 0.f;
-#pragma unroll
-      for (int j = 0; j < VC; ++j) o[nb][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
-  };
-
-  // A part of a row in LDS, a lane's registers in its column, and its addition to another
-  auto give = [&](float (*to)[64]) {
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      float (*p)[64] = to + nb * (VC * 4 + 2);
-#pragma unroll
-      for (int j = 0; j < VC; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) p[4 * j + r][lane] = o[nb][j][r];
-      p[4 * VC][lane] = m[nb], p[4 * VC + 1][lane] = l[nb];
-    }
-  };
-  auto take = [&](float (*from)[64]) {
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      float (*p)[64] = from + nb * (VC * 4 + 2);
-      const float other = p[4 * VC][lane], top = fmaxf(m[nb], other), k1 = fast_exp2(m[nb] - top), k2 = fast_exp2(other - top);
-      m[nb] = top;
-      l[nb] = l[nb] * k1 + p[4 * VC + 1][lane] * k2;
-#pragma unroll
-      for (int j = 0; j < VC; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) o[nb][j][r] = o[nb][j][r] * k1 + p[4 * j + r][lane] * k2;
-    }
-  };
-  // The state as the row's result, or as this share's part of it
-  auto put = [&](const Step& s, bool begins, bool ends) {
-    const size_t row = (size_t)s.b * a.Hkv + s.hk, slot = 2 * (size_t)blockIdx.x + (begins ? 1 : 0);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const int head = col + 16 * nb;
-      const float sum = over_groups_sum(l[nb]), inv = 1.f / sum;
-      if (head >= z.G) continue;
-      if (begins && ends) {
-        const size_t to = row * z.G + head;
-        if (a.lse != nullptr && grp == 0) a.lse[to] = 0.6931471805599453f * (m[nb] + __builtin_log2f(sum));
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int j = 0; j < VC; j += 4)
-            store_out4(a.out, a.out_dt, to * D + channel(r, j), o[nb][j][r] * inv, o[nb][j + 1][r] * inv, o[nb][j + 2][r] * inv, o[nb][j + 3][r] * inv);
-      } else {
-        const size_t to = slot * z.G + head;
-        if (grp == 0) z.w.part_ml[2 * to] = m[nb], z.w.part_ml[2 * to + 1] = sum;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int j = 0; j < VC; j += 4)
-            *reinterpret_cast<v4f*>(z.w.part_o + to * D + channel(r, j)) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]};
-      }
-    }
-  };
-
+  W w;
   // ---- this wavefront's steps: every fourth where the share lies in one row, which keeps what the four read together, otherwise a quarter
   // of the share, which leaves them one meeting whatever number of rows there is ----
   const bool one_row = cur.t + (u_end - u) <= cur.steps;
@@ -316,93 +382,40 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
     more = u < u_end;
     if (one_row) next.t += more ? kWaves : 0;
     else if (more) advance(next);
-    look_up(next);
+    w.look_up(a, z, next);
   };
   bool busy = u < u_end;
   if (busy) {
-    look_up(cur);
-    load_q(cur, true);
-    describe(cur, true);
-    load_k();
-    load_v();
-    clear();
-    next_q();
+    w.look_up(a, z, cur);
+    w.load_q(a, z, cur, true);
+    w.describe(a, z, cur, true);
+    w.load_k();
+    w.load_v();
+    w.clear();
+    w.next_q();
     follow();
   }
   while (busy) {
-    float x[NB][8];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
-        v4f s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < KS; ++e) s = Mma<T>::mma(k[sub][e], q[nb][e], s);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[nb][4 * sub + r] = s[r] * z.c;
-      }
     const bool turns = more && next.t == 0;                      // a row begins with the next step
-    describe(next, more);
-    load_k();
-    load_q(next, turns);
-    const int behind = cur.len - cur.t * kStep;                  // keys of the row from this step on
-    auto masked = [&](int r) { return (r < 4 ? 0 : 12) + 4 * grp + r >= behind; };
-    v4i high[NB], low[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      if (behind < kStep) {
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (masked(r)) x[nb][r] = -__builtin_inff();
-      }
-      const float (&y)[8] = x[nb];
-      const float top = over_groups_max(fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])))) - kShift;
-      if (__ballot(top > m[nb])) {
-        const float grown = fmaxf(top, m[nb]), keep = fast_exp2(m[nb] - grown);
-        m[nb] = grown;
-        l[nb] *= keep;
-#pragma unroll
-        for (int j = 0; j < VC; ++j) o[nb][j] *= keep;
-      }
-      uint16_t hi[8], lo[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const float p = fast_exp2(y[r] - m[nb]);
-        l[nb] += p;
-        hi[r] = T::from_float(p);
-        lo[r] = T::from_float(p - T::to_float(hi[r]));
-      }
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        high[nb][r] = (int)((uint32_t)hi[2 * r] | ((uint32_t)hi[2 * r + 1] << 16));
-        low[nb][r] = (int)((uint32_t)lo[2 * r] | ((uint32_t)lo[2 * r + 1] << 16));
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < VC; ++j) {
-      v4i y;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = (int)__builtin_amdgcn_perm(v[2 * r + 1][j / 2], v[2 * r][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        o[nb][j] = Mma<T>::mma(y, high[nb], o[nb][j]);
-        o[nb][j] = Mma<T>::mma(y, low[nb], o[nb][j]);
-      }
-    }
-    load_v();
+    w.step(z.c, cur.len - cur.t * kStep, [&]() {
+      w.describe(a, z, next, more);
+      w.load_k();
+      w.load_q(a, z, next, turns);
+    });
+    w.load_v();
     if (!more || turns) {                  // the row ends, or what this wavefront has of it
       const bool ends = cur.t + 1 == cur.steps;
       if (begin > 0 && wave > 0) {         // an earlier wavefront's row
-        give(parts[wave]);
+        w.give(parts[wave]);
         if (ends && lane == 0) ended[wave] = 1;
       } else if (ends && !one_row) {
-        put(cur, begin == 0, true);
+        w.put(a, z, cur, begin == 0, 2 * (size_t)blockIdx.x);
       } else {
         kept = true;
       }
       if (!more) break;
-      clear();
-      next_q();
+      w.clear();
+      w.next_q();
       begin = 0, first_u = u;
     }
     cur = next;
@@ -411,17 +424,96 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
   __syncthreads();
   if (!kept) return;
   bool ends = cur.t + 1 == cur.steps;
-  for (int w = wave + 1; w < kWaves && (one_row || !ends); ++w) {
-    if (ended[w] < 0) break;
-    take(parts[w]);
-    ends |= ended[w] > 0;
+  for (int i = wave + 1; i < kWaves && (one_row || !ends); ++i) {
+    if (ended[i] < 0) break;
+    w.take(parts[i]);
+    ends |= ended[i] > 0;
   }
-  put(cur, begin == 0, ends);
+  w.put(a, z, cur, begin == 0 && ends, 2 * (size_t)blockIdx.x + (begin == 0 ? 1 : 0));
   // the state began with the row's first step, at each * kWaves * (shares so far) + what this share has of other rows; the rest of the
   // row's steps fill the shares behind
   if (begin == 0 && !ends && lane == 0) {
     const int share = each * kWaves, here = min(share - (first_u - (int)blockIdx.x * share), cur.steps);
     z.w.tail[blockIdx.x] = make_int2(cur.b * a.Hkv + cur.hk, 1 + (cur.steps - here + share - 1) / share);
+  }
+}
+
+// One workgroup per row, for short caches: what it reads first (length, pages, query) does not depend on each other, and there is nothing to
+// join afterwards.  Wavefronts take every fourth step (eight instead of four gained nothing); at the end each joins some channels of all
+// of them.
+constexpr int kRowWaves = 4;
+template <typename T, int D>
+__global__ void __launch_bounds__(64 * kRowWaves, 1) paged_decode_rows_kernel(PagedDecodeArgs a, Launch z) {
+  using Rows = Walk<T, D, 1>;
+  constexpr int W = kRowWaves;
+  constexpr int VC = Rows::VC;
+  __shared__ float parts[W][Rows::NR][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Step cur;
+  cur.b = blockIdx.x / a.Hkv, cur.hk = blockIdx.x - cur.b * a.Hkv, cur.t = wave;
+  const int n = scalar(a.seqlens)[cur.b];
+  Rows w;
+  w.look_up(a, z, cur);
+  w.load_q(a, z, cur, true);
+  cur.len = length_of(a, z, n), cur.steps = steps_of(cur.len);
+  const size_t row0 = (size_t)blockIdx.x * z.G;                  // the group's first row of out
+  if (cur.len == 0) {
+    for (int i = threadIdx.x; i < z.G * D / 4; i += 64 * W) store_out4(a.out, a.out_dt, row0 * D + 4 * (size_t)i, 0.f, 0.f, 0.f, 0.f);
+    if (a.lse != nullptr && (int)threadIdx.x < z.G) a.lse[row0 + threadIdx.x] = -__builtin_inff();
+    return;
+  }
+  const int active = min(W, cur.steps);                          // wavefronts with a step
+  if (wave < active) {
+    w.describe(a, z, cur, true);
+    w.load_k();
+    w.load_v();
+    w.clear();
+    w.next_q();
+    while (true) {
+      Step next = cur;
+      next.t += W;
+      const bool more = next.t < cur.steps;
+      w.look_up(a, z, next);
+      w.step(z.c, cur.len - cur.t * kStep, [&]() {
+        w.describe(a, z, next, more);
+        w.load_k();
+      });
+      if (!more) break;
+      w.load_v();
+      cur.t = next.t;
+    }
+    w.give(parts[wave]);
+  }
+  __syncthreads();
+  // four channels of every lane's head at a time
+  if (w.col >= z.G) return;
+  float top = -__FLT_MAX__, l = 0.f, weight[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    weight[i] = i < active ? parts[i][4 * VC][lane] : -__FLT_MAX__;
+    top = fmaxf(top, weight[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    weight[i] = i < active ? fast_exp2(weight[i] - top) : 0.f;
+    if (i < active) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) l += weight[i] * parts[i][4 * VC + 1][w.col + 16 * g];
+    }
+  }
+  const float inv = 1.f / l;
+  const size_t to = row0 + w.col;
+  if (a.lse != nullptr && threadIdx.x == w.col) a.lse[to] = kLn2 * (top + __builtin_log2f(l));
+  for (int u = wave; u < VC; u += W) {
+    const int r = u & 3, j = 4 * (u >> 2);
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      if (i < active) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += weight[i] * parts[i][4 * (j + e) + r][lane];
+      }
+    store_out4(a.out, a.out_dt, to * D + w.channel(r, j), x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
   }
 }
 
@@ -484,11 +576,28 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedDecodeArgs a
   }
   const float inv = 1.f / sum;
   store_out4(a.out, a.out_dt, at * D + 4 * quad, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
-  if (a.lse != nullptr && tid == 0) a.lse[at] = 0.6931471805599453f * (top + __builtin_log2f(sum));
+  if (a.lse != nullptr && tid == 0) a.lse[at] = kLn2 * (top + __builtin_log2f(sum));
+}
+
+// A CU takes about 40 GB/s from memory, so that a row of its own costs it 6.4 us for 256 KiB of keys and values; where the block table has room for no
+// more, that is less than the search for a share and the second launch.  Shares / rows, us, 32/8 heads of 128 channels: 10.3 / 7.1 for 1 x 256,
+// 10.7 / 6.9 for 16 x 50-100, 12.8 / 10.7 for 16 x 250-500, 54.3 / 54.6 for 256 x 125-500; beyond: 10.3 / 12.5 for 1 x 1000, 15.2 / 17.8 for
+// 16 x 500-1000.  64 channels: 14.0 / 11.5 for 64 x 125-500; 256 channels: 12.5 / 16.2 for 4 x 250-500, 16/16 heads.
+// With more than four rows per CU the shares are as fast (33.8 / 33.7 for 256 x 63-250) or faster (160 / 226 for 4096 x 15-60).
+constexpr long kRowBytes = 256 << 10, kRowMost = 4 * kCus;
+bool by_rows(const PagedDecodeArgs& a, const Launch& z) {
+  return z.G <= 16 && ((long)a.max_pages << z.shift) * a.D * 4 <= kRowBytes && (long)a.B * a.Hkv <= kRowMost;
 }
 
 template <typename T>
 void launch(const PagedDecodeArgs& a, const Launch& z, hipStream_t st) {
+  if (by_rows(a, z)) {
+    const dim3 rows((unsigned)((long)a.B * a.Hkv)), block(64 * kRowWaves);
+    if (a.D == 64) paged_decode_rows_kernel<T, 64><<<rows, block, 0, st>>>(a, z);
+    else if (a.D == 128) paged_decode_rows_kernel<T, 128><<<rows, block, 0, st>>>(a, z);
+    else paged_decode_rows_kernel<T, 256><<<rows, block, 0, st>>>(a, z);
+    return;
+  }
   const dim3 grid(kShares), merge(kShares * z.G), block(kThreads);
 #define THRIFT_PAGED(D_)                                                                     \
   if (z.G <= 16) paged_decode_kernel<T, D_, 1><<<grid, dim3(64 * waves_of(D_)), 0, st>>>(a, z);                \
