@@ -6,7 +6,7 @@ import random
 import pytest
 import torch
 
-from tests.paged_util import LAYOUTS, attention64, check_rounded, rope64
+from tests.paged_util import LAYOUTS, attention64, check_rounded, rope64, tokens
 
 pytestmark = pytest.mark.gpu
 DTYPES = (torch.float16, torch.bfloat16)
@@ -245,10 +245,11 @@ LENS = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 255, 256, 
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("Hq,Hkv", [(4, 4), (8, 2), (32, 4), (7, 1), (32, 1), (3, 3), (40, 2), (17, 1)])
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_attention_against_64_bits(T, D, Hq, Hkv, dtype):
+@pytest.mark.parametrize("room", [300, 1300])                  # of the block table: a workgroup per row, or shares
+def test_attention_against_64_bits(T, D, Hq, Hkv, dtype, room):
     for page in (16, 64, 256):
-        print(f"paged D={D} Hq={Hq} Hkv={Hkv} page={page} {dtype}", flush=True)
-        width = -(-300 // page)
+        print(f"paged D={D} Hq={Hq} Hkv={Hkv} page={page} room={room} {dtype}", flush=True)
+        width = -(-room // page)
         kp, vp, table = _cache(len(LENS), Hkv, D, page, width, dtype, LENS, seed=page)
         q = _randn(len(LENS), Hq, D, dtype=dtype, seed=9)
         _check_attention(T, q, kp, vp, table, LENS)
@@ -256,9 +257,10 @@ def test_attention_against_64_bits(T, D, Hq, Hkv, dtype):
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("garbage", [float("nan"), float("inf"), -65504.0])
-def test_what_lies_past_the_length_reaches_no_result(T, page, garbage):
-    for lens in ([1], [page + 1, 5 * page - 1], [0, 0, 0], [3 * page, 10 ** 9, -1]):
-        kp, vp, table = _cache(len(lens), 2, 128, page, 5, torch.float16, lens, seed=page, garbage=garbage)
+@pytest.mark.parametrize("width", [2, 40])
+def test_what_lies_past_the_length_reaches_no_result(T, page, garbage, width):
+    for lens in ([1], [page + 1, width * page - 1], [0, 0, 0], [2 * page, 10 ** 9, -1]):
+        kp, vp, table = _cache(len(lens), 2, 128, page, width, torch.float16, lens, seed=page, garbage=garbage)
         q = _randn(len(lens), 8, 128, dtype=torch.float16, seed=3)
         print(f"past the length page={page} lens={lens} garbage={garbage}", flush=True)
         _check_attention(T, q, kp, vp, table, lens)
@@ -309,9 +311,9 @@ def test_many_sequences(T, B, kind):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("gain", [0.01, 30.0])
-def test_flat_and_peaked_scores(T, dtype, gain):
-    lens = [700, 64, 1, 333]
-    kp, vp, table = _cache(4, 2, 128, 32, 24, dtype, lens, seed=6)
+@pytest.mark.parametrize("lens", [[700, 64, 1, 333], [500, 64, 1, 333]])
+def test_flat_and_peaked_scores(T, dtype, gain, lens):
+    kp, vp, table = _cache(4, 2, 128, 32, -(-lens[0] // 32), dtype, lens, seed=6)
     q = (_randn(4, 8, 128, dtype=torch.float32, seed=7) * gain).to(dtype)
     _check_attention(T, q, kp, vp, table, lens)
     _check_attention(T, q, kp, vp, table, lens, scale=0.3)
@@ -325,6 +327,22 @@ def test_flat_and_peaked_scores(T, dtype, gain):
             live = torch.arange(len(held) * 32, device="cuda").view(-1, 1, 32, 1) < n
             kp2[held] = torch.where(live, kp2[held], float("nan"))
         _check_attention(T, q.abs(), kp2, vp, table, lens)
+
+
+@pytest.mark.parametrize("width", [6, 60])
+def test_scores_of_minus_infinity_weigh_nothing(T, width):
+    """Keys whose product with the query overflows downwards, a whole step of them first."""
+    kp, vp, table = _cache(1, 1, 128, 16, width, torch.bfloat16, [90], seed=8)
+    q = torch.ones(1, 2, 128, dtype=torch.bfloat16, device="cuda")
+    for j in range(4):
+        kp[table[0, j].long()] = -3e37
+    out, lse = T.thrift_paged_decode(q, kp, vp, table, _ints([90]), out_dtype=torch.float32, return_lse=True)
+    k, v = (tokens(p, table[0], 90)[0, 64:].double() for p in (kp, vp))
+    s = (q[0].double() @ k.t().contiguous()) / math.sqrt(128)
+    want = torch.softmax(s, -1) @ v
+    # fp32 sums of 128 products of about 1 (attention64 gives 2^-15 of the values)
+    assert bool(((out[0].double() - want).abs() <= 2 ** -14 * v.abs().amax()).all())
+    assert bool(((lse[0].double() - torch.logsumexp(s, -1)).abs() <= 2 ** -14).all())
 
 
 def test_the_same_page_twice(T):
