@@ -416,6 +416,63 @@ def test_streams_workspaces_and_replays(T):
 
 # ---- all together ----
 
+def test_a_captured_step_replayed(T):
+    """Map, append and attention of one token per request captured once; every replay moves the pool on as an eager step on a copy of
+    it does, with eager work in between, until pages run out."""
+    B, Hq, Hkv, D, page, dtype = 5, 8, 2, 128, 16, torch.float16
+    freqs, gain = T.rope_frequencies(D, 1e4, device="cuda")
+
+    class Server:
+        def __init__(self):
+            self.table = T.PageTable(B, 80, page, 21, "cuda")             # 21 pages: a few steps in, some request gets none
+            self.cache = T.PagedKVCache(self.table, Hkv, D, dtype)
+            self.x = torch.empty(B, Hq + 2 * Hkv, D, dtype=dtype, device="cuda")
+            self.new = torch.ones(B, dtype=I32, device="cuda")
+            self.seqlens, self.count = _ints([30, 0, 47, 79, 111]), _ints([0])
+            held = [2, 0, 3, 5, 7]
+            pages = list(range(20, -1, -1))
+            for b, n in enumerate(held):
+                self.table.block_table[b, :n] = _ints([pages.pop() for _ in range(n)])
+            self.table.free_pages[:len(pages)] = _ints(pages)
+            self.count.fill_(len(pages))
+            for i, p in enumerate((self.cache.k_pages, self.cache.v_pages)):
+                p.copy_(_randn(*p.shape, dtype=dtype, seed=40 + i))
+
+        def step(self):
+            t = self.table
+            t.seqlens, t.free_count = self.seqlens, self.count
+            m = t.map(self.new, B + 3)
+            x = torch.cat([self.x, torch.zeros(3, Hq + 2 * Hkv, D, dtype=dtype, device="cuda")])
+            q = self.cache.append(x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], m, x[:, :Hq], freqs, "half", gain, q_out=torch.zeros(B + 3, Hq, D, dtype=dtype, device="cuda"))
+            out, lse = self.cache.decode(q[:B], return_lse=True)
+            self.seqlens.copy_(m.seqlens)
+            self.count.copy_(m.free_count)
+            return [out, lse, m.slots, m.positions, m.starts]
+
+        def state(self):
+            return [self.seqlens, self.count, self.table.block_table, self.cache.k_pages, self.cache.v_pages]
+
+    eager, captured = Server(), Server()
+    eager.x.copy_(_randn(*eager.x.shape, dtype=dtype, seed=1)), captured.x.copy_(eager.x)
+    eager.step(), captured.step()                                         # (the capture's warm-up)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        results = captured.step()
+    refused = 0
+    for i in range(24):
+        x = _randn(*eager.x.shape, dtype=dtype, seed=100 + i)
+        eager.x.copy_(x), captured.x.copy_(x)
+        want = eager.step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(results + captured.state(), want + eager.state()):
+            assert torch.equal(a, b), i
+        refused += int((want[2][:B] < 0).sum())
+    assert refused > 0 and int(eager.count) == 0
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("layout", LAYOUTS)
 def test_a_servers_steps(T, dtype, layout):
