@@ -422,7 +422,8 @@ thrift_status thrift_rope_backward(const void* q, const int64_t* q_strides, void
 
 /*
  * Pages of a paged cache.  A page holds page_size consecutive tokens of one sequence (page_size: 16, 32, 64, 128 or 256); the pages of
- * sequence b are block_table[b][0 .. ceil(length / page_size) - 1].  Slot s is token s % page_size of page s / page_size.  Free
+ * sequence b are block_table[b][0 .. ceil(length / page_size) - 1], each held by one sequence only (attention may read tables that share
+ * pages; who is given tokens and whose pages are put back is then the caller's business).  Slot s is token s % page_size of page s / page_size.  Free
  * pages lie on a stack: free_pages[0 .. free_count[0] - 1], the next one to be taken last.
  *
  * thrift_page_map gives the new tokens of a step their places, from the lengths on the device alone.  The new tokens of all sequences
@@ -462,7 +463,7 @@ thrift_status thrift_page_release(const int32_t* seqlens, const int32_t* drop, i
  *   slots [T]: from thrift_page_map.  A row whose slot lies outside 0 .. n_pages * page_size - 1 is skipped: its keys and values go
  *     nowhere and its q_out row is left as it was.  No slot may occur twice.
  *   positions [T], freqs, rot, layout, gain as thrift_rope; rot == 0: nothing is rotated (positions and freqs unused, q copied)
- *   k_pages, v_pages [n_pages,Hkv,page_size,D] 16-bit (dt)
+ *   k_pages, v_pages [n_pages,Hkv,page_size,D] 16-bit (dt); the inputs and q_out must not overlap them
  * D even, <= 1024; T below 2^23.
  */
 thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
@@ -479,12 +480,12 @@ size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int 
  *   q [B,Hq,D] 16-bit (dt); k_pages, v_pages [n_pages,Hkv,page_size,D]; block_table [B,max_pages]; D 64, 128 or 256; Hq a multiple
  *     of Hkv, at most 32 heads per KV head; B * Hq below 2^23, B * Hkv * max_pages * page_size below 2^35
  *   seqlens [B]: cached tokens, clamped to 0 .. max_pages * page_size.  What pages hold past the length reaches no result, whatever
- *     it is.  A sequence of length 0 gives zeros.
+ *     it is.  A sequence of length 0 gives zeros.  Within the length, values are finite (an infinite one gives NaN in its channel).
  *   block_table entries within the length must name pages; others give unspecified numbers but are never followed outside
  *     k_pages and v_pages (clamped to 0 .. n_pages - 1).
  *   softmax_scale <= 0 selects 1/sqrt(D)
  *   out [B,Hq,D] in out_dt; lse (nullable) [B,Hq] fp32: log-sum-exp of the scaled scores, -inf for length 0
- *   q, k_pages, v_pages and out are 16-byte aligned, otherwise THRIFT_ERR_SHAPE
+ *   q, k_pages, v_pages and out are 16-byte aligned, otherwise THRIFT_ERR_SHAPE; out and lse overlap no input
  *   workspace: thrift_paged_decode_workspace(...) bytes, 16-byte aligned; the next call on the same stream may use it again
  */
 thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,

@@ -570,3 +570,17 @@ def test_the_module_leaves_other_arguments_to_the_general_path(T):
     assert m.paged_decode(k, pages, pages, table, lens, 0.0, None, None, 0, torch.empty(16, dtype=torch.uint8, device="cuda"), 0, 0) == 5
     assert m.page_map(lens, lens, table, slots, lens[:1], 16, 4, 3, 1, 0) is None and m.page_map(lens, lens, table, slots, lens, 16, 4, 3, 0, 0) is None
     assert m.page_map(lens, lens, table, slots, lens[:1], 17, 4, 3, 0, 0) == 2 and len(m.page_map(lens, lens, table, slots, lens[:1], 16, 4, 3, 0, 0)) == 5
+
+
+def test_the_steps_that_the_readme_shows(T):
+    import os
+    readme = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code = readme.split("```python\n")[1].split("```")[0]
+    B, Hq, Hkv, D, rows = 3, 8, 2, 128, 3
+    names = dict(T=T, torch=torch, B=B, max_pages=8, page_size=16, n_pages=30, Hkv=Hkv, D=D, rows=rows, new_lens=torch.ones(B, dtype=I32, device="cuda"),
+                 q=_randn(rows, Hq, D, dtype=torch.bfloat16), k=_randn(rows, Hkv, D, dtype=torch.bfloat16), v=_randn(rows, Hkv, D, dtype=torch.bfloat16, seed=1),
+                 ended=_ints([0, 1, 0]))
+    exec(code, names)
+    # the first token of every request attends to itself alone
+    assert torch.equal(names["out"], names["v"].repeat_interleave(Hq // Hkv, 1))
+    assert names["table"].seqlens.tolist() == [1, 0, 1] and names["table"].free_count.tolist() == [28]
