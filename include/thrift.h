@@ -471,7 +471,7 @@ thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void*
                                   const int32_t* positions, const double* freqs, int rot, int layout, float gain,
                                   void* k_pages, void* v_pages, int n_pages, int page_size, int D, void* stream);
 
-/* Host: bytes of workspace thrift_paged_decode needs (0 for sizes that it refuses). */
+/* Host: bytes of workspace thrift_paged_decode needs.  0: none (short caches; workspace may be NULL), and for sizes that it refuses. */
 size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D);
 
 /*

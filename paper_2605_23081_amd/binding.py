@@ -125,11 +125,13 @@ def _raw_stream() -> int:
         return 0
 
 
-def _device() -> int:
+def _here_now() -> Tuple[int, int]:
+    """The current device and its current stream."""
     try:
-        return torch._C._cuda_getDevice()
+        device = torch._C._cuda_getDevice()
+        return device, torch._C._cuda_getCurrentRawStream(device)
     except RuntimeError:
-        return -1
+        return -1, 0
 
 
 def _result(r, where: str):
@@ -559,7 +561,7 @@ def thrift_rope(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: s
                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q [B,Hq,N,D] and k [B,Hkv,N,D] (or None) with their first 2 * len(freqs) channels turned to positions ([B,N] or [N], default
     0 .. N-1): (q_out, k_out), contiguous unless given.  Inputs and outputs may be views (a fused projection's [B,N,H,D])."""
-    r = (_call or _native()).rope(0, q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, _device(), _raw_stream())
+    r = (_call or _native()).rope(0, q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, *_here_now())
     if r is not None:
         return _result(r, "thrift_rope")
     return _rope("thrift_rope", q, k, freqs, positions, layout, gain, q_out, k_out)
@@ -568,7 +570,7 @@ def thrift_rope(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: s
 def thrift_rope_backward(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: str = "half", gain: float = 1.0,
                          q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """Gradients of thrift_rope's inputs from those of its outputs, q and k (or None); arguments as thrift_rope."""
-    r = (_call or _native()).rope(1, q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, _device(), _raw_stream())
+    r = (_call or _native()).rope(1, q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, *_here_now())
     if r is not None:
         return _result(r, "thrift_rope_backward")
     return _rope("thrift_rope_backward", q, k, freqs, positions, layout, gain, q_out, k_out)
@@ -597,7 +599,7 @@ def _pool(seqlens, block_table, free_pages, free_count) -> Tuple[int, int]:
 
 def thrift_page_map(seqlens, new_lens, block_table, free_pages, free_count, page_size: int, n_pages: int, rows: int) -> PageMap:
     """Pages, block-table entries (written into block_table), slots and positions of new_lens [B] new tokens per sequence."""
-    r = (_call or _native()).page_map(seqlens, new_lens, block_table, free_pages, free_count, page_size, n_pages, rows, _device(), _raw_stream())
+    r = (_call or _native()).page_map(seqlens, new_lens, block_table, free_pages, free_count, page_size, n_pages, rows, *_here_now())
     if r is not None:
         return PageMap._make(_result(r, "thrift_page_map"))
     B, max_pages = _pool(seqlens, block_table, free_pages, free_count)
@@ -635,7 +637,7 @@ def thrift_paged_append(k, v, slots, k_pages, v_pages, q: Optional[torch.Tensor]
                         gain: float = 1.0) -> Optional[torch.Tensor]:
     """k, v [T,Hkv,D] into the pages [n_pages,Hkv,page_size,D] at slots [T]; with freqs, k and q [T,Hq,D] are rotated to
     positions [T].  Returns q_out (contiguous; rows of skipped tokens are left as they were)."""
-    r = (_call or _native()).paged_append(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs, ROPE_LAYOUTS[layout], gain, _device(), _raw_stream())
+    r = (_call or _native()).paged_append(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs, ROPE_LAYOUTS[layout], gain, *_here_now())
     if r is not None:
         return None if r is True else _result(r, "thrift_paged_append")
     _pages(k_pages, v_pages)
@@ -674,7 +676,7 @@ def thrift_paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale
     """Attention of q [B,Hq,D] over the first seqlens [B] tokens of each sequence's pages: out, or (out, lse) with return_lse."""
     if out is not None or out_dtype is None:
         r = (_call or _native()).paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale, out, lse, int(bool(return_lse)), workspace,
-                                              _device(), _raw_stream())
+                                              *_here_now())
         if r is not None:
             return _result(r, "thrift_paged_decode")
     _pages(k_pages, v_pages)
@@ -692,7 +694,7 @@ def thrift_paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale
     assert lse is None or tuple(_dev(lse, torch.float32).shape) == (B, Hq)
     if workspace is None:
         need = paged_decode_workspace_bytes(B, Hq, Hkv, max_pages, page_size, D)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
     _dev(workspace, torch.uint8)
     _here(q, k_pages, v_pages, block_table, seqlens, out, lse, workspace)
     _check(lib().thrift_paged_decode(_ptr(q), _DT[q.dtype], _ptr(k_pages), _ptr(v_pages), n_pages, _ptr(block_table), max_pages, _ptr(seqlens),

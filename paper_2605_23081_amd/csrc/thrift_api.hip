@@ -730,7 +730,7 @@ static bool paged_decode_ok(int B, int Hq, int Hkv, int max_pages, int page_size
 }
 
 size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
-  return paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) ? paged_decode_workspace(Hq, Hkv, D) : 0;
+  return paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) ? paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D) : 0;
 }
 
 thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,
@@ -741,8 +741,8 @@ thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_
   if (!is16(dt) || !is_out(out_dt)) return THRIFT_ERR_DTYPE;
   if (!paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) || !fits_int(n_pages, page_size)) return THRIFT_ERR_SHAPE;
   if ((((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)out) & 15) != 0) return THRIFT_ERR_SHAPE;
-  const size_t need = paged_decode_workspace(Hq, Hkv, D);
-  if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15) != 0) return THRIFT_ERR_WORKSPACE;
+  const size_t need = paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D);
+  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15) != 0)) return THRIFT_ERR_WORKSPACE;
   if (thrift_status s = check_arch()) return s;
   PagedDecodeArgs a;
   a.q = (const uint16_t*)q; a.k_pages = (const uint16_t*)k_pages; a.v_pages = (const uint16_t*)v_pages; a.table = block_table;

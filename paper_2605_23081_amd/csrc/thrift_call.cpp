@@ -365,13 +365,14 @@ PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!dtype_out(out, &odt)) Py_RETURN_NONE;
   const Tensor lse = lse_given ? *lse_given : return_lse ? at::empty({B, Hq}, q->options().dtype(at::kFloat)) : Tensor();
   const int Hkv = (int)kp->size(1), page = (int)kp->size(2);
-  const Tensor ws = ws_given ? *ws_given : bytes_like(*q, thrift_paged_decode_workspace((int)B, (int)Hq, Hkv, (int)width, page, (int)D));
+  const size_t need = ws_given ? 0 : thrift_paged_decode_workspace((int)B, (int)Hq, Hkv, (int)width, page, (int)D);
+  const Tensor ws = ws_given ? *ws_given : need > 0 ? bytes_like(*q, need) : Tensor();
   thrift_status r;
   {
     const Unlocked unlocked;
     r = thrift_paged_decode(ptr(q), dt, ptr(kp), ptr(vp), (int)kp->size(0), ptr_as<int32_t>(table), (int)width, ptr_as<int32_t>(lens),
                                                 (int)B, (int)Hq, Hkv, (int)D, page, (float)scale, out.data_ptr(), odt,
-                                                lse.defined() ? lse.data_ptr<float>() : nullptr, ws.data_ptr(), (size_t)ws.numel(), stream);
+                                                lse.defined() ? lse.data_ptr<float>() : nullptr, ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? (size_t)ws.numel() : 0, stream);
   }
   if (r != THRIFT_OK || !return_lse) return answer(r, out);
   PyObject* both = PyTuple_New(2);

@@ -81,7 +81,7 @@ struct PagedDecodeArgs {
   float scale;                // softmax scale (already defaulted)
   thrift_dtype dt, out_dt;
 };
-size_t paged_decode_workspace(int Hq, int Hkv, int D);
+size_t paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D);   // 0: none is needed
 void launch_paged_decode(const PagedDecodeArgs& a, hipStream_t st);
 
 }  // namespace thrift

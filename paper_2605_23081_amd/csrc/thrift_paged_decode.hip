@@ -590,13 +590,13 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedDecodeArgs a
 // 16 x 500-1000.  64 channels: 14.0 / 11.5 for 64 x 125-500; 256 channels: 12.5 / 16.2 for 4 x 250-500, 16/16 heads.
 // With more than four rows per CU the shares are as fast (33.8 / 33.7 for 256 x 63-250) or faster (160 / 226 for 4096 x 15-60).
 constexpr long kRowBytes = 256 << 10, kRowMost = 4 * kCus;
-bool by_rows(const PagedDecodeArgs& a, const Launch& z) {
-  return z.G <= 16 && ((long)a.max_pages << z.shift) * a.D * 4 <= kRowBytes && (long)a.B * a.Hkv <= kRowMost;
+bool by_rows(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
+  return Hq / Hkv <= 16 && (long)max_pages * page_size * D * 4 <= kRowBytes && (long)B * Hkv <= kRowMost;
 }
 
 template <typename T>
 void launch(const PagedDecodeArgs& a, const Launch& z, hipStream_t st) {
-  if (by_rows(a, z)) {
+  if (by_rows(a.B, a.Hq, a.Hkv, a.max_pages, a.page_size, a.D)) {
     const dim3 rows((unsigned)((long)a.B * a.Hkv)), block(64 * kRowWaves);
     if (a.D == 64) paged_decode_rows_kernel<T, 64><<<rows, block, 0, st>>>(a, z);
     else if (a.D == 128) paged_decode_rows_kernel<T, 128><<<rows, block, 0, st>>>(a, z);
@@ -618,7 +618,10 @@ constexpr size_t kTailBytes = kShares * sizeof(int2);
 
 }  // namespace
 
-size_t paged_decode_workspace(int Hq, int Hkv, int D) { return kTailBytes + 2 * (size_t)kShares * (Hq / Hkv) * (D + 2) * sizeof(float); }
+size_t paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
+  if (by_rows(B, Hq, Hkv, max_pages, page_size, D)) return 0;
+  return kTailBytes + 2 * (size_t)kShares * (Hq / Hkv) * (D + 2) * sizeof(float);
+}
 
 void launch_paged_decode(const PagedDecodeArgs& a, hipStream_t st) {
   Launch z;

@@ -30,8 +30,9 @@ int main() {
       EXPECT(thrift_paged_append(p, far, p, a, p, far, p, far, b, THRIFT_F16, a, i, i, f, 128, 0, 1.f, p, p, b, 24, 128, nullptr), THRIFT_ERR_SHAPE);
       EXPECT(thrift_paged_decode(p, THRIFT_F16, p, p, a, i, b, i, a, b, a, 96, 16, 0.f, p, THRIFT_F16, nullptr, p, 0, nullptr), THRIFT_ERR_SHAPE);
       for (int c : sizes) {
+        // sizes that are taken need a workspace (one byte less is refused) or none; then 17 is no page size
         const size_t need = thrift_paged_decode_workspace(a, b, c, a, 16, 128);
-        const int s = (int)thrift_paged_decode(p, THRIFT_BF16, p, p, 8, i, a, i, a, b, c, 128, 16, 0.f, p, THRIFT_F32, nullptr, p, need ? need - 1 : 0, nullptr);
+        const int s = (int)thrift_paged_decode(p, THRIFT_BF16, p, p, 8, i, a, i, a, b, c, 128, need ? 16 : 17, 0.f, p, THRIFT_F32, nullptr, p, need ? need - 1 : 0, nullptr);
         EXPECT(s, need ? THRIFT_ERR_WORKSPACE : THRIFT_ERR_SHAPE);
         refused += need == 0;
       }

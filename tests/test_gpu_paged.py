@@ -394,7 +394,8 @@ def test_streams_workspaces_and_replays(T):
             results.append([one() for _ in range(20)])
     torch.cuda.synchronize()
     assert all(torch.equal(r, want) for rs in results for r in rs)
-    size = max(T.paged_decode_workspace_bytes(4, 8, 2, 60, 16, 128), 16)
+    size = T.paged_decode_workspace_bytes(4, 8, 2, 60, 16, 128)
+    assert size > 0
     shared = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
     graphs, outs = [], []
     for _ in range(2):
@@ -567,7 +568,9 @@ def test_the_module_leaves_other_arguments_to_the_general_path(T):
     assert m.paged_append(k, k, slots, pages, pages, None, None, None, freqs, 0, 1.0, 0, 0) is None
     assert m.paged_decode(k, pages, pages, table, lens, 0.0, None, None, 0, None, 1, 0) is None
     assert m.paged_decode(k, pages, pages, table[:2], lens, 0.0, None, None, 0, None, 0, 0) is None
-    assert m.paged_decode(k, pages, pages, table, lens, 0.0, None, None, 0, torch.empty(16, dtype=torch.uint8, device="cuda"), 0, 0) == 5
+    wide = torch.zeros(3, 100, dtype=I32, device="cuda")
+    assert m.paged_decode(k, pages, pages, wide, lens, 0.0, None, None, 0, torch.empty(16, dtype=torch.uint8, device="cuda"), 0, 0) == 5
+    assert m.paged_decode(k, pages, pages, table, lens, 0.0, None, None, 0, torch.empty(0, dtype=torch.uint8, device="cuda"), 0, 0).shape == (3, 2, 128)
     assert m.page_map(lens, lens, table, slots, lens[:1], 16, 4, 3, 1, 0) is None and m.page_map(lens, lens, table, slots, lens, 16, 4, 3, 0, 0) is None
     assert m.page_map(lens, lens, table, slots, lens[:1], 17, 4, 3, 0, 0) == 2 and len(m.page_map(lens, lens, table, slots, lens[:1], 16, 4, 3, 0, 0)) == 5
 

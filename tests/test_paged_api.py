@@ -110,9 +110,9 @@ def test_page_calls_refuse_before_a_launch():
         assert decode(**bad) == SHAPE, bad
     for bad in ("q", "kp", "vp", "out"):
         assert decode(**{bad: C.c_void_p(0x1008)}) == SHAPE, bad
-    need = L.thrift_paged_decode_workspace(2, 4, 2, 8, 16, 128)
-    assert need > 0
-    assert decode(ws=None) == WORKSPACE and decode(size=need - 1) == WORKSPACE and decode(ws=C.c_void_p(0x1008)) == WORKSPACE
+    need = L.thrift_paged_decode_workspace(2, 4, 2, 800, 16, 128)
+    assert need > 0 and L.thrift_paged_decode_workspace(2, 4, 2, 8, 16, 128) == 0            # a workgroup per row needs none
+    assert decode(mp=800, ws=None) == WORKSPACE and decode(mp=800, size=need - 1) == WORKSPACE and decode(mp=800, ws=C.c_void_p(0x1008)) == WORKSPACE
     assert L.thrift_paged_decode_workspace(2, 5, 2, 8, 16, 128) == 0 and L.thrift_paged_decode_workspace(2, 4, 2, 8, 16, 96) == 0
     if not torch.cuda.is_available():
         assert page_map() == ARCH and release() == ARCH and append() == ARCH and append(q=None, qo=None, Hq=0) == ARCH and decode() == ARCH
