@@ -18,8 +18,8 @@
 // its workgroup; otherwise each share leaves a partial, and a second launch joins a row's partials in the order of the shares.
 //
 // Bound by memory for long caches: what is fetched are the keys and values of the lengths and nothing else (counters), 8.6 GB for 16 x 131072 tokens,
-// 32/8 heads, in 1221 us (7.0 TB/s; a streaming read reaches 7.0-7.15), 775 MB for 8 x 16384-32768, 64/8 heads, in 124 us (6.3 TB/s).  Next to that the
-// chain of latencies counts: lengths, sums, page, keys, values (7.0 us of kernel for 1 x 1000 tokens), and the second launch (2.4-4.6 us).
+// 32/8 heads, in 1220 us (7.0 TB/s; a streaming read reaches 7.0-7.15), 775 MB for 8 x 16384-32768, 64/8 heads, in 123 us (6.3 TB/s).  Next to that the
+// chain of latencies counts: lengths, sums, page, keys, values (7.2 us of kernel for 1 x 1000 tokens), and the second launch (2.7-4.8 us).
 #include "thrift_device.h"
 #include "thrift_launch.h"
 #include "thrift_paged.h"
@@ -585,8 +585,8 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedDecodeArgs a
 }
 
 // A CU takes about 40 GB/s from memory, so that a row of its own costs it 6.4 us for 256 KiB of keys and values; where the block table has room for no
-// more, that is less than the search for a share and the second launch.  Shares / rows, us, 32/8 heads of 128 channels: 10.3 / 7.1 for 1 x 256,
-// 10.7 / 6.9 for 16 x 50-100, 12.8 / 10.7 for 16 x 250-500, 54.3 / 54.6 for 256 x 125-500; beyond: 10.3 / 12.5 for 1 x 1000, 15.2 / 17.8 for
+// more, that is less than the search for a share and the second launch.  Shares / rows, us, 32/8 heads of 128 channels: 10.3 / 6.3 for 1 x 256,
+// 10.7 / 5.7 for 16 x 50-100, 12.8 / 10.7 for 16 x 250-500, 54.3 / 54.6 for 256 x 125-500; beyond: 10.3 / 12.5 for 1 x 1000, 15.2 / 17.8 for
 // 16 x 500-1000.  64 channels: 14.0 / 11.5 for 64 x 125-500; 256 channels: 12.5 / 16.2 for 4 x 250-500, 16/16 heads.
 // With more than four rows per CU the shares are as fast (33.8 / 33.7 for 256 x 63-250) or faster (160 / 226 for 4096 x 15-60).
 constexpr long kRowBytes = 256 << 10, kRowMost = 4 * kCus;

@@ -1,9 +1,9 @@
 // Pages of the paged 16-bit cache: block tables and slots from the lengths on the device, return of pages, and the write of
 // new tokens with the rotation of their queries and keys.
 //
-// The map is bound by latency: 5.5 us of kernel for 256 sequences with a token each, 5.6 for 64 with 262144 rows (2 MB), 6.2 with the call.  The append is
+// The map is bound by latency: 5.6 us of kernel for 256 sequences with a token each, 5.8 for 64 with 262144 rows (2 MB), 6.0-6.1 with the call.  The append is
 // bound by memory: it reads and writes every element once (counters), 8192 rows of 64/8 heads in 72 us (4.7 TB/s), 32768 of 32/8 in 157
-// (5.1); a decode step's rows take the launch (3.5 us of kernel, 4.7 with the call).
+// (5.1); a decode step's rows take the launch (3.8 us of kernel, 4.5 with the call).
 #include "thrift_paged.h"
 #include "thrift_rotary.h"
 

@@ -1,8 +1,8 @@
 // Rotary positions of the query and key heads of a batch, forward and transposed (the gradient).
 //
 // Bound by memory: every element is read and written once (counters: 1.34 GB each way for 131072 tokens of 32/8 heads, which is what they hold), at
-// 5.4 TB/s there and 5.1 for 3001 tokens; a plain copy of 2 GiB runs at 4.8-4.9.  493 and 12.1 us; up to some hundred tokens the call is its
-// launch (3.4 us of kernel, 4.2 of host time).
+// 5.4 TB/s there and 5.1 for 3001 tokens; a plain copy of 2 GiB runs at 4.8-4.9.  493-504 and 12.1 us; up to some hundred tokens the call is
+// its launch (3.5 us of kernel, 4 of host time, 5.8 in all).
 #include "thrift_paged.h"
 #include "thrift_rotary.h"
 
