@@ -242,7 +242,7 @@ PyObject* rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int64_t step = positions && positions->dim() == 2 ? positions->stride(0) : 0;
   const Tensor q_out = qo ? *qo : at::empty(q->sizes(), q->options());
   const Tensor k_out = !k ? Tensor() : ko ? *ko : at::empty(k->sizes(), k->options());
-  int64_t st[4][3];
+  int64_t st[4][3] = {};
   for (int i = 0; i < 3; ++i) {
     st[0][i] = q->stride(i), st[1][i] = q_out.stride(i);
     if (k) st[2][i] = k->stride(i), st[3][i] = k_out.stride(i);
