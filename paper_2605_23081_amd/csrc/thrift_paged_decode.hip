@@ -533,6 +533,12 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedDecodeArgs a
   const int tid = threadIdx.x, first = blockIdx.x / z.G, g = blockIdx.x % z.G;
   const int quad = tid % kQuads, part = tid / kQuads;
   const int2 tail = z.w.tail[first];
+  // partial w of the row that begins in share `first`
+  auto slot = [&](int w) { return (size_t)(2 * (first + w) + (w == 0 ? 1 : 0)) * z.G + g; };
+  // the first kParts of them before it is known how many there are, or whether there are any
+  const size_t ahead = slot(min(part, kShares - 1 - first));
+  const v4f x0 = *reinterpret_cast<const v4f*>(z.w.part_o + ahead * D + 4 * quad);
+  const float2 y0 = *reinterpret_cast<const float2*>(z.w.part_ml + 2 * ahead);
   for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
     if (a.seqlens[b] > 0) continue;
     for (int i = tid; i < a.Hq * kQuads; i += kThreads) store_out4(a.out, a.out_dt, (size_t)b * a.Hq * D + 4 * (size_t)i, 0.f, 0.f, 0.f, 0.f);
@@ -544,13 +550,14 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedDecodeArgs a
   const size_t at = (size_t)tail.x * z.G + g;
   v4f o = {0.f, 0.f, 0.f, 0.f};
   float m = -__builtin_inff(), l = 0.f;
-  for (int i0 = part; i0 < n; i0 += kParts * kAhead) {
+  if (part < n) o = x0, m = y0.x, l = y0.y;
+  for (int i0 = part + kParts; i0 < n; i0 += kParts * kAhead) {
     v4f x[kAhead];
     float2 y[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const int w = min(n - 1, i0 + i * kParts);
-      const size_t s = (size_t)(2 * (first + w) + (w == 0 ? 1 : 0)) * z.G + g;
+      const size_t s = slot(w);
       x[i] = *reinterpret_cast<const v4f*>(z.w.part_o + s * D + 4 * quad);
       y[i] = *reinterpret_cast<const float2*>(z.w.part_ml + 2 * s);
       if (i0 + i * kParts >= n) y[i] = make_float2(-__builtin_inff(), 0.f);
