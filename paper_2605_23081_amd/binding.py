@@ -560,7 +560,8 @@ def _rope(name: str, q, k, freqs, positions, layout: str, gain: float, q_out, k_
 def thrift_rope(q, k, freqs, positions: Optional[torch.Tensor] = None, layout: str = "half", gain: float = 1.0,
                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q [B,Hq,N,D] and k [B,Hkv,N,D] (or None) with their first 2 * len(freqs) channels turned to positions ([B,N] or [N], default
-    0 .. N-1): (q_out, k_out), contiguous unless given.  Inputs and outputs may be views (a fused projection's [B,N,H,D])."""
+    0 .. N-1): (q_out, k_out), contiguous unless given.  Inputs and outputs may be views (a fused projection's [B,N,H,D]).  Nothing is
+    recorded for autograd: the gradient is thrift_rope_backward."""
     r = (_call or _native()).rope(0, q, k, freqs, positions, ROPE_LAYOUTS[layout], gain, q_out, k_out, *_here_now())
     if r is not None:
         return _result(r, "thrift_rope")

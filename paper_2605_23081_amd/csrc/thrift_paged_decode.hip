@@ -9,7 +9,8 @@
 //                  scores the lane holds, so that P goes from S to the next product without leaving the lane.
 // No tile passes through LDS.  P is split into two 16-bit pieces, high and low, for two products.  Rounded once, an fp32 output of bf16 inputs was off by
 // 1.1e-4 (1000 tokens) to 3.9e-4 (30000) relative to its norm, with two pieces by 2.4e-7 and 7.5e-7, in the same time (8 x 16384-32768
-// tokens, 64/8 heads: 129.0 and 129.1 us).  P is scaled by 2^15, so that an fp16 piece is a normal number down to 2^-29 of the largest.
+// tokens, 64/8 heads: 129.0 and 129.1 us).  For fp16, P is scaled by 2^15, so that a piece is a normal number down to 2^-29 of the largest;
+// bf16 needs no scale, and its largest values would overflow under one.
 //
 // The steps of all rows are counted through on the GPU from the lengths and cut into equal shares, one per workgroup, whatever the
 // lengths are; a wavefront walks a quarter of it, or every fourth step where the share lies in one row.  It asks for the keys of its next step as soon as the scores of this one are
@@ -33,7 +34,7 @@ constexpr int kThreads = 256;              // of the merge
 // heads: 74.1 -> 70.2 us); 64 channels: eight with as much were slower than four (23.6 -> 25.1 us).
 constexpr int waves_of(int D) { return D == 256 ? 2 : 4; }
 constexpr int kStep = 32;                  // keys per step of a wavefront
-constexpr float kShift = 15.f, kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f;
 // One workgroup per CU: its four wavefronts have 64 KiB on their way, 16 MiB on the chip.  More of them ask for more than the memory takes at a
 // time, and what waits in front of it is served unevenly (one / two / three per CU: 1220 / 1225 / 1265 us for 16 x 131072 tokens of 32/8 heads,
 // 130 / 132 / 150 for 8 x 16384-32768 of 64/8).
@@ -44,11 +45,13 @@ typedef const __attribute__((address_space(4))) int32_t* scalar_ints;
 __device__ __forceinline__ scalar_ints scalar(const int32_t* p) { return (scalar_ints)(uintptr_t)p; }
 
 struct Mfma16F16 {
+  static constexpr float kShift = 15.f;    // log2 of the scale of P
   static __device__ __forceinline__ v4f mma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
   }
 };
 struct Mfma16BF16 {
+  static constexpr float kShift = 0.f;
   static __device__ __forceinline__ v4f mma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
   }
@@ -72,7 +75,7 @@ __device__ __forceinline__ float over_groups_sum(float x) {
 }
 
 // Workspace: the row that every share leaves unfinished, and two partials per share: of a row that an earlier share has begun, and of
-// that unfinished row.  O [D], then m - 15 and the sum.
+// that unfinished row.  O [D], then the maximum less kShift and the sum.
 struct Space {
   int2* tail;                // [kShares] row (-1: none) and number of shares that it lies in
   float* part_o;             // [2*kShares][G][D]
@@ -104,7 +107,7 @@ struct Walk {
   v4i q[NB][KS], q_next[NB][KS], k[2][KS];
   uint32_t v[8][VC / 2];
   v4f o[NB][VC];                           // o [D] of one head is spread over the four lanes of its column: element r of tile j is channel(r, j)
-  float m[NB], l[NB];                      // maximum less 15; this lane's part of the sum
+  float m[NB], l[NB];                      // maximum less kShift; this lane's part of the sum
   // Loads of 16 keys go through a descriptor of their page's rows up to the length: what lies behind reads as 0 and is not fetched, and
   // a step that does not exist has none.
   __amdgpu_buffer_rsrc_t kd[2], vd[2];
@@ -199,7 +202,7 @@ struct Walk {
           if ((r < 4 ? 0 : 12) + 4 * grp + r >= behind) x[nb][r] = -__builtin_inff();
       }
       const float (&y)[8] = x[nb];
-      const float top = over_groups_max(fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])))) - kShift;
+      const float top = over_groups_max(fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])))) - Mma<T>::kShift;
       if (__ballot(top > m[nb])) {
         const float grown = fmaxf(top, m[nb]), keep = fast_exp2(m[nb] - grown);
         m[nb] = grown;

@@ -330,6 +330,16 @@ def test_flat_and_peaked_scores(T, dtype, gain, lens):
 
 
 @pytest.mark.parametrize("width", [6, 60])
+def test_the_largest_values(T, width):
+    """Values near the end of bfloat16's range: a mean of them is one of them, whatever the sums are scaled by in between."""
+    kp, vp, table = _cache(1, 1, 128, 16, width, torch.bfloat16, [90], seed=8)
+    live = ~torch.isnan(vp)
+    vp[live] = torch.where(vp[live] > 0, 1.0, -1.0).to(torch.bfloat16) * 2.0 ** 120
+    q = _randn(1, 2, 128, dtype=torch.bfloat16, seed=3)
+    _check_attention(T, q, kp, vp, table, [90])
+
+
+@pytest.mark.parametrize("width", [6, 60])
 def test_scores_of_minus_infinity_weigh_nothing(T, width):
     """Keys whose product with the query overflows downwards, a whole step of them first."""
     kp, vp, table = _cache(1, 1, 128, 16, width, torch.bfloat16, [90], seed=8)
