@@ -102,6 +102,9 @@ struct Walk {
   static constexpr int KS = D / 32;        // 16-byte pieces of a key's row per lane
   static constexpr int VC = D / 16;        // channels of a value's row per lane
   static constexpr int NR = NB * (VC * 4 + 2);                   // registers of a state
+  // the next row's queries are on their way during a step; 32 heads of 256 channels have no registers for that (64 x 2048-4096 tokens, 64/2 heads:
+  // 161 us with, 83 without)
+  static constexpr bool kQueryAhead = NB * D < 512;
   static constexpr int kStream = 2;        // non-temporal: keys and values are read once
   int lane, col, grp;
   v4i q[NB][KS], q_next[NB][KS], k[2][KS];
@@ -408,7 +411,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
     w.step(z.c, cur.len - cur.t * kStep, [&]() {
       w.describe(a, z, next, more);
       w.load_k();
-      w.load_q(a, z, next, turns);
+      if (W::kQueryAhead) w.load_q(a, z, next, turns);
     });
     w.load_v();
     if (!more || turns) {                  // the row ends, or what this wavefront has of it
@@ -423,6 +426,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 ? 2 : 1) paged
       }
       if (!more) break;
       w.clear();
+      if (!W::kQueryAhead) w.load_q(a, z, next, true);
       w.next_q();
       begin = 0, first_u = u;
     }
