@@ -9,8 +9,9 @@
 //                  scores the lane holds, so that P goes from S to the next product without leaving the lane.
 // No tile passes through LDS.  P is split into two 16-bit pieces, high and low, for two products.  Rounded once, an fp32 output of bf16 inputs was off by
 // 1.1e-4 (1000 tokens) to 3.9e-4 (30000) relative to its norm, with two pieces by 2.4e-7 and 7.5e-7, in the same time (8 x 16384-32768
-// tokens, 64/8 heads: 129.0 and 129.1 us).  For fp16, P is scaled by 2^15, so that a piece is a normal number down to 2^-29 of the largest;
-// bf16 needs no scale, and its largest values would overflow under one.
+// tokens, 64/8 heads: 129.0 and 129.1 us).  For fp16, the pieces are those of 2^15 P, so that a piece is a normal number down to 2^-29 of the largest;
+// bf16 needs no scale, and its largest values would overflow under one.  The scale is a factor behind the exponential: folded into the
+// maximum, m - 15 rounds to another number from 2^24 on, and the largest P to 2^16, which fp16 does not hold.
 //
 // The steps of all rows are counted through on the GPU from the lengths and cut into equal shares, one per workgroup, whatever the
 // lengths are; a wavefront walks a quarter of it, or every fourth step where the share lies in one row.  It asks for the keys of its next step as soon as the scores of this one are
@@ -45,13 +46,13 @@ typedef const __attribute__((address_space(4))) int32_t* scalar_ints;
 __device__ __forceinline__ scalar_ints scalar(const int32_t* p) { return (scalar_ints)(uintptr_t)p; }
 
 struct Mfma16F16 {
-  static constexpr float kShift = 15.f;    // log2 of the scale of P
+  static constexpr float kScale = 32768.f; // of P's pieces
   static __device__ __forceinline__ v4f mma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
   }
 };
 struct Mfma16BF16 {
-  static constexpr float kShift = 0.f;
+  static constexpr float kScale = 1.f;
   static __device__ __forceinline__ v4f mma(v4i a, v4i b, v4f c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
   }
@@ -75,7 +76,7 @@ __device__ __forceinline__ float over_groups_sum(float x) {
 }
 
 // Workspace: the row that every share leaves unfinished, and two partials per share: of a row that an earlier share has begun, and of
-// that unfinished row.  O [D], then the maximum less kShift and the sum.
+// that unfinished row.  O [D], then the maximum and the sum.
 struct Space {
   int2* tail;                // [kShares] row (-1: none) and number of shares that it lies in
   float* part_o;             // [2*kShares][G][D]
@@ -109,8 +110,8 @@ struct Walk {
   int lane, col, grp;
   v4i q[NB][KS], q_next[NB][KS], k[2][KS];
   uint32_t v[8][VC / 2];
-  v4f o[NB][VC];                           // o [D] of one head is spread over the four lanes of its column: element r of tile j is channel(r, j)
-  float m[NB], l[NB];                      // maximum less kShift; this lane's part of the sum
+  v4f o[NB][VC];                           // kScale o [D] of one head, spread over the four lanes of its column: element r of tile j is channel(r, j)
+  float m[NB], l[NB];                      // maximum; this lane's part of the sum
   // Loads of 16 keys go through a descriptor of their page's rows up to the length: what lies behind reads as 0 and is not fetched, and
   // a step that does not exist has none.
   __amdgpu_buffer_rsrc_t kd[2], vd[2];
@@ -184,6 +185,8 @@ struct Walk {
   // One step, of which the row has `behind` keys from its first on; `ask` when the keys' registers are free
   template <typename F>
   __device__ __forceinline__ void step(float c, int behind, F ask) {
+    // A score is rounded once, before the maximum: a fused s c - m would leave the largest one's rounding, units and more from 2^24 on
+#pragma clang fp contract(off)
     float x[NB][8];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -205,7 +208,7 @@ struct Walk {
           if ((r < 4 ? 0 : 12) + 4 * grp + r >= behind) x[nb][r] = -__builtin_inff();
       }
       const float (&y)[8] = x[nb];
-      const float top = over_groups_max(fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])))) - Mma<T>::kShift;
+      const float top = over_groups_max(fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7]))));
       if (__ballot(top > m[nb])) {
         const float grown = fmaxf(top, m[nb]), keep = fast_exp2(m[nb] - grown);
         m[nb] = grown;
@@ -218,8 +221,9 @@ struct Walk {
       for (int r = 0; r < 8; ++r) {
         const float p = fast_exp2(y[r] - m[nb]);
         l[nb] += p;
-        hi[r] = T::from_float(p);
-        lo[r] = T::from_float(p - T::to_float(hi[r]));
+        const float scaled = p * Mma<T>::kScale;
+        hi[r] = T::from_float(scaled);
+        lo[r] = T::from_float(scaled - T::to_float(hi[r]));
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -268,10 +272,11 @@ struct Walk {
   // The state as the row's result, or as a part of it in `slot`
   __device__ __forceinline__ void put(const PagedDecodeArgs& a, const Launch& z, const Step& s, bool whole, size_t slot) const {
     const size_t row = (size_t)s.b * a.Hkv + s.hk;
+    constexpr float kUnscale = 1.f / Mma<T>::kScale;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int head = col + 16 * nb;
-      const float sum = over_groups_sum(l[nb]), inv = 1.f / sum;
+      const float sum = over_groups_sum(l[nb]), inv = whole ? kUnscale / sum : kUnscale;
       if (head >= z.G) continue;
       if (whole) {
         const size_t to = row * z.G + head;
@@ -288,7 +293,7 @@ struct Walk {
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int j = 0; j < VC; j += 4)
-            *reinterpret_cast<v4f*>(z.w.part_o + to * D + channel(r, j)) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]};
+            *reinterpret_cast<v4f*>(z.w.part_o + to * D + channel(r, j)) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]} * inv;
       }
     }
   }
@@ -513,7 +518,7 @@ __global__ void __launch_bounds__(64 * kRowWaves, 1) paged_decode_rows_kernel(Pa
       for (int g = 0; g < 4; ++g) l += weight[i] * parts[i][4 * VC + 1][w.col + 16 * g];
     }
   }
-  const float inv = 1.f / l;
+  const float inv = 1.f / (Mma<T>::kScale * l);
   const size_t to = row0 + w.col;
   if (a.lse != nullptr && threadIdx.x == w.col) a.lse[to] = kLn2 * (top + __builtin_log2f(l));
   for (int u = wave; u < VC; u += W) {

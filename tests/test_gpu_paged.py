@@ -355,6 +355,39 @@ def test_scores_of_minus_infinity_weigh_nothing(T, width):
     assert bool(((lse[0].double() - torch.logsumexp(s, -1)).abs() <= 2 ** -14).all())
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("width", [6, 60])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("a", [900.0, 1100.0, 2000.0, 4000.0, 30720.0])
+def test_scores_past_24_bits(T, dtype, width, sign, a):
+    """Scores from 2^23 to 2^33 (in powers of two), where fp32's neighbours are up to hundreds apart: keys with the largest one share the
+    weight, the others have none."""
+    lens, D, Hkv = [90, 1, 33, 64], 128, 2
+    kp, vp, table = _cache(4, Hkv, D, 16, width, dtype, lens, seed=12)
+    a = float(torch.tensor(a).to(dtype))
+    q = torch.full((4, 2 * Hkv, D), a, dtype=dtype, device="cuda")
+    winners = [[0, 31, 32, 77, 89], [0], [32], list(range(64))]
+    low, high = (a / 2, a) if sign > 0 else (-a, -a / 2)
+    want = torch.empty(4, Hkv, D, dtype=torch.float64, device="cuda")
+    for b, n in enumerate(lens):
+        held = table[b, : -(-n // 16)].long()
+        place = torch.arange(len(held) * 16, device="cuda")
+        best = torch.isin(place, torch.tensor(winners[b], device="cuda"))
+        rows = torch.where(best, high, low).where(place < n, float("nan")).to(dtype)
+        kp[held] = rows.view(-1, 1, 16, 1).expand(-1, Hkv, -1, D)
+        want[b] = tokens(vp, table[b], n).double()[:, winners[b]].mean(1)
+    out, lse = T.thrift_paged_decode(q, kp, vp, table, _ints(lens), out_dtype=torch.float32, return_lse=True)
+    # a^2 has at most 17 bits from its first to its last one, so that every sum of up to 128 of them is an fp32 number: the largest scores are
+    # equal in the kernel, and the others 2^22 and more below.  P is 1 or 0; at most 64 values are added, each partial sum off by half a
+    # step of at most 64 times the largest, and the reciprocal of their number and the product with it follow: 66 U of the largest
+    top = vp[~torch.isnan(vp)].double().abs().max()
+    assert bool(((out.view(4, Hkv, 2, D).double() - want.unsqueeze(2)).abs() <= 66 * 2.0 ** -24 * top).all())
+    # eight roundings: root and quotient of the scale, log2(e), their product, the score's product, the sum with log2(n), ln 2, its product
+    n = torch.tensor([len(w) for w in winners], dtype=torch.float64, device="cuda")
+    exact = D * a * high / math.sqrt(D) + n.log()
+    assert bool(((lse.double() - exact.unsqueeze(1)).abs() <= 8 * 2.0 ** -24 * exact.abs().unsqueeze(1)).all())
+
+
 def test_the_same_page_twice(T):
     """Sequences that share their first pages, and a table that names a page twice."""
     kp, vp, table = _cache(3, 2, 128, 16, 6, torch.bfloat16, [96, 96, 96], seed=8)
