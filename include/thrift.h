@@ -478,7 +478,8 @@ size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int 
  * Attention of one new token per sequence over a paged 16-bit cache; the new token's key and value are in the cache already.
  *   o = sum_j p_j v_j,  p = softmax over j < seqlens[b] of softmax_scale * q . k_j; scores, probabilities and sums in fp32
  *   q [B,Hq,D] 16-bit (dt); k_pages, v_pages [n_pages,Hkv,page_size,D]; block_table [B,max_pages]; D 64, 128 or 256; Hq a multiple
- *     of Hkv, at most 32 heads per KV head; B * Hq below 2^23, B * Hkv * max_pages * page_size below 2^35
+ *     of Hkv, at most 32 heads per KV head; B * Hq below 2^23, n_pages * page_size and max_pages * page_size below 2^31,
+ *     B * Hkv * max_pages * page_size below 2^35
  *   seqlens [B]: cached tokens, clamped to 0 .. max_pages * page_size.  What pages hold past the length reaches no result, whatever
  *     it is.  A sequence of length 0 gives zeros.  Within the length, values are finite (an infinite one gives NaN in its channel).
  *   block_table entries within the length must name pages; others give unspecified numbers but are never followed outside

@@ -95,7 +95,8 @@ struct Step {
 };
 
 __device__ __forceinline__ int length_of(const PagedDecodeArgs& a, const Launch& z, int n) { return min(a.max_pages << z.shift, max(0, n)); }
-__device__ __forceinline__ int steps_of(int len) { return (len + kStep - 1) / kStep; }
+// len + 31 passes 31 bits at the longest lengths
+__device__ __forceinline__ int steps_of(int len) { return (int)(((unsigned)len + kStep - 1) / kStep); }
 
 // What a wavefront holds of a row, and its steps
 template <typename T, int D, int NB>

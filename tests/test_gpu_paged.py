@@ -420,6 +420,24 @@ def test_offsets_past_32_bits(T):
     _check_attention(T, q, kp, vp, table, [4 * page])
 
 
+@pytest.mark.parametrize("dtype,lens", [(torch.bfloat16, [2 ** 31 - 16 - 15, 37]), (torch.float16, [70, 2 ** 31 - 1])])
+def test_the_longest_block_table(T, dtype, lens):
+    """A table of 2^31 - 16 tokens that names four pages over and over; lengths whose last steps end past 2^31, a short sequence beside."""
+    D, page, width = 64, 16, 2 ** 27 - 1
+    kp = _randn(4, 1, page, D, dtype=dtype)
+    vp = torch.randint(-4, 5, (4, 1, page, D), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+    table = torch.arange(width, dtype=I32, device="cuda").remainder_(4).expand(2, width).contiguous()
+    print(f"longest table {dtype} {lens}", flush=True)
+    # queries of 0 weigh all keys alike: a wavefront's sums of 2^21 values of at most 4 are exact
+    out, lse = T.thrift_paged_decode(torch.zeros(2, 1, D, dtype=dtype, device="cuda"), kp, vp, table, _ints(lens), out_dtype=torch.float32, return_lse=True)
+    for b, n in enumerate(min(n, width * page) for n in lens):
+        count = torch.tensor([n // 64 + (j < n % 64) for j in range(64)], dtype=torch.float64, device="cuda")
+        want = (count.unsqueeze(1) * vp.view(64, D).double()).sum(0) / n
+        # the parts of 4 wavefronts and 256 shares: 260 additions each in the sums of values (half a step of at most 4 n) and of weights
+        assert bool(((out[b, 0].double() - want).abs() <= 4 * (2 * 260 + 4) * 2.0 ** -24).all())
+        assert abs(float(lse[b, 0]) - math.log(n)) <= (260 + 4 * math.log(n)) * 2.0 ** -24
+
+
 def test_streams_workspaces_and_replays(T):
     """Calls at the same time on two streams with workspaces of their own; a captured call replayed between eager ones with other
     lengths; two captured calls that share one workspace, replayed in turn."""
