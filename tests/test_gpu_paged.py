@@ -404,6 +404,20 @@ def test_bad_table_entries_are_not_followed(T):
     assert out.shape == (2, 8, 128)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("width", [6, 60])
+def test_bad_table_entries_are_clamped(T, dtype, width):
+    """The result is that of the table with its entries clamped to the pages, bit for bit, in both forms."""
+    lens = [96, 90, 17]
+    kp, vp, table = _cache(3, 2, 128, 16, width, dtype, lens, seed=9, garbage=0.5)
+    table[0, 2], table[1, 0], table[1, 5], table[2, 1] = -1, 2 ** 31 - 1, -2 ** 31, kp.shape[0]
+    q = _randn(3, 8, 128, dtype=dtype)
+    print(f"bad entries width={width} {dtype}", flush=True)
+    got = T.thrift_paged_decode(q, kp, vp, table, _ints(lens), out_dtype=torch.float32, return_lse=True)
+    want = T.thrift_paged_decode(q, kp, vp, table.clamp(0, kp.shape[0] - 1), _ints(lens), out_dtype=torch.float32, return_lse=True)
+    assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(got, want))
+
+
 def test_offsets_past_32_bits(T):
     """Pages whose elements lie past 2^31 (and bytes past 2^32)."""
     Hkv, page, D = 8, 128, 128
