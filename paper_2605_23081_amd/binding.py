@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import operator
 import os
 import warnings
 from typing import NamedTuple, Optional, Tuple
@@ -38,6 +39,15 @@ class ThriftError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
         super().__init__(f"{where}: status {code} ({status_string(code)})")
+
+
+class _Int:
+    """A C int that keeps to its range: ctypes alone would take the low 32 bits of a larger size, which then might be an accepted one.  The
+    ends of the range are refused by every call's limits."""
+
+    @staticmethod
+    def from_param(x):
+        return C.c_int(max(-2 ** 31, min(2 ** 31 - 1, operator.index(x))))
 
 
 def lib() -> C.CDLL:
@@ -75,7 +85,7 @@ def lib() -> C.CDLL:
         L.thrift_attention_forward_workspace.argtypes = [i, i, i, i, i, i, i, i, d, i]
         L.thrift_attention_forward.argtypes = [p, p, p, i, i, i, i, i, i, i, i, i, d, i, i, f, p, i, p, p, sz, p]
         L.thrift_kv_cache_append_advance.argtypes = [p, p, i, i, p, p, p, p, p, p, p, p, p, p, i, i, i, i, i, p]
-        i64 = C.c_int64
+        i64, i = C.c_int64, _Int
         L.thrift_rope_frequencies.argtypes = [i, d, i, d, d, d, d, C.POINTER(d), C.POINTER(f)]
         L.thrift_rope.argtypes = [p, p, p, p, i, p, p, p, p, i, i, p, i64, p, i, i, f, i, i, i, p]
         L.thrift_rope_backward.argtypes = L.thrift_rope.argtypes
@@ -85,7 +95,7 @@ def lib() -> C.CDLL:
         L.thrift_paged_decode_workspace.restype = sz
         L.thrift_paged_decode_workspace.argtypes = [i] * 6
         L.thrift_paged_decode.argtypes = [p, i, p, p, i, p, i, p, i, i, i, i, i, f, p, i, p, p, sz, p]
-        L.thrift_peak_probe.argtypes = [i, i, i, p, sz, C.POINTER(C.c_double), p]
+        L.thrift_peak_probe.argtypes = [C.c_int, C.c_int, C.c_int, p, sz, C.POINTER(C.c_double), p]
         _lib = L
     return _lib
 
@@ -496,7 +506,7 @@ ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "by_parts": 3}
 def rope_frequencies(rot: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, original: float = 0.0,
                      slow: float = 1.0, fast: float = 32.0, device=None) -> Tuple[torch.Tensor, float]:
     """Radians per position of the rot/2 pairs (fp64, on `device`) and the gain, for the scalings of include/thrift.h."""
-    freqs, gain = (C.c_double * max(rot // 2, 1))(), C.c_float()
+    freqs, gain = (C.c_double * max(min(rot // 2, 512), 1))(), C.c_float()               # more are refused
     _check(lib().thrift_rope_frequencies(int(rot), float(base), ROPE_SCALINGS[scaling], float(factor), float(original), float(slow),
                                          float(fast), freqs, C.byref(gain)), "thrift_rope_frequencies")
     return torch.tensor(list(freqs), dtype=torch.float64, device=device), float(gain.value)

@@ -119,6 +119,27 @@ def test_page_calls_refuse_before_a_launch():
         assert append(rot=0, pos=None, freqs=None) == ARCH
 
 
+def test_sizes_past_32_bits_are_refused():
+    """Sizes whose low 32 bits would be accepted."""
+    L, other, over = T.lib(), C.c_void_p(0x2000), 2 ** 32
+    page_map = lambda B=4, ps=16, n=64, mp=8, rows=32: L.thrift_page_map(FAKE, FAKE, B, ps, n, FAKE, mp, FAKE, 64, FAKE, rows, FAKE, FAKE, FAKE, other, other, None)
+    release = lambda B=4, ps=16, n=64, mp=8: L.thrift_page_release(FAKE, FAKE, B, ps, n, FAKE, mp, FAKE, 64, FAKE, other, other, None)
+    append = lambda Hq=4, Hkv=2, T_=8, rot=128, layout=0, n=8, ps=16, D=128: L.thrift_paged_append(
+        FAKE, None, FAKE, Hq, FAKE, None, FAKE, None, Hkv, 0, T_, FAKE, FAKE, FAKE, rot, layout, 1.0, FAKE, FAKE, n, ps, D, None)
+    decode = lambda n=8, mp=8, B=2, Hq=4, Hkv=2, D=128, ps=16: L.thrift_paged_decode(
+        FAKE, 0, FAKE, FAKE, n, FAKE, mp, FAKE, B, Hq, Hkv, D, ps, 0.0, FAKE, 0, None, FAKE, 1 << 40, None)
+    rope = lambda Hq=4, Hkv=2, rot=128, layout=0, B=1, N=8, D=128: L.thrift_rope(
+        FAKE, None, FAKE, None, Hq, FAKE, None, FAKE, None, Hkv, 0, None, 0, FAKE, rot, layout, 1.0, B, N, D, None)
+    for call in (page_map, release, append, decode, rope):
+        for name, value in zip(call.__code__.co_varnames, call.__defaults__):
+            assert call(**{name: value + over}) == SHAPE and call(**{name: value - over}) == SHAPE, (call, name)
+    assert L.thrift_paged_decode_workspace(2, 4, 2, 800 + over, 16, 128) == 0
+    assert append(rot=over) == SHAPE                                                     # whose low bits say that nothing is rotated
+    with pytest.raises(T.ThriftError) as e:
+        T.rope_frequencies(64 + over)
+    assert e.value.code == SHAPE
+
+
 def test_binding_refuses_what_the_kernels_cannot_index():
     h, i32, f64 = torch.float16, torch.int32, torch.float64
     q, k = torch.zeros(2, 4, 8, 128, dtype=h), torch.zeros(2, 2, 8, 128, dtype=h)
