@@ -313,8 +313,9 @@ void launch_append(const PagedAppendArgs& a, hipStream_t st) {
   }
   const HeadShape z = head_shape(a.T, a.Hq + 2 * a.Hkv, a.D, a.rot);
   const dim3 grid((unsigned)((a.T + z.tokens - 1) / z.tokens * z.splits)), block(kHeadThreads);
-  // Written past the caches where a store fills lines: 78.4 -> 71.8 us for 8192 rows of 64/8 heads of 128 channels, 167.7 -> 157.0 for 32768 of 32/8
-  const bool stream = a.D >= 128;
+  // Written past the caches where a store fills lines: 78.4 -> 71.8 us for 8192 rows of 64/8 heads of 128 channels, 167.7 -> 157.0 for 32768 of 32/8;
+  // with 64 channels turned by halves 78.1 cached, 82.4 past the caches, with none 46.1 and 54.0 (8192 rows of 32/8)
+  const bool stream = fills_lines(a.D, a.rot, a.layout);
 #define THRIFT_APPEND(L_)                                                                    \
   if (stream) paged_append_items_kernel<T, L_, true><<<grid, block, 0, st>>>(a, z);          \
   else paged_append_items_kernel<T, L_, false><<<grid, block, 0, st>>>(a, z)

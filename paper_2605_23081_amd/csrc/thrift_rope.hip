@@ -108,8 +108,8 @@ void launch(const RopeArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((tokens + z.tokens - 1) / z.tokens * z.splits)), block(kHeadThreads);
   // Past the caches where these cannot hold inputs and results of a pass (cached / streamed: 18.8 / 21.0 us for 84 MB, 36.8 / 35.2 for 168,
   // 50.6 / 48.4 for 268, 72.4 / 67.5 for 336, 142 / 131 for 671, 538 / 499 for 2.7 GB) and where a store fills lines (heads of 64 channels: 88 / 98
-  // us for 409 MB).
-  const bool stream = 4L * tokens * (a.side[0].heads + a.side[1].heads) * a.D > (128L << 20) && a.D >= 128;
+  // us for 409 MB; 128 channels with 64 turned by halves: 50 / 65 for 268 MB, 147 / 187 for 671; 256 with 128: 285 / 326 for 1.3 GB).
+  const bool stream = 4L * tokens * (a.side[0].heads + a.side[1].heads) * a.D > (128L << 20) && fills_lines(a.D, a.rot, a.layout);
 #define THRIFT_ROPE(L_)                                                              \
   if (stream) rope_items_kernel<T, L_, true><<<grid, block, 0, st>>>(a, z);          \
   else rope_items_kernel<T, L_, false><<<grid, block, 0, st>>>(a, z)

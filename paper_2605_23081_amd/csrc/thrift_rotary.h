@@ -89,6 +89,11 @@ struct Item {
   }
 };
 
+// Whether a store instruction fills lines of 128 bytes: neighbouring lanes write neighbouring chunks in the interleaved layout and where the whole
+// head is turned by halves; with a part turned by halves, the copied channels are written every other chunk at a time, and the
+// turned ones in runs of `rot` bytes.
+inline bool fills_lines(int D, int rot, int layout) { return D >= 128 && (layout == THRIFT_ROPE_INTERLEAVED || rot == D); }
+
 // 16 bytes, past the caches where STREAM
 template <bool STREAM>
 __device__ __forceinline__ v4i chunk_from(const uint16_t* p) {
