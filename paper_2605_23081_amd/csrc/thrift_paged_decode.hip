@@ -20,8 +20,8 @@
 // its workgroup; otherwise each share leaves a partial, and a second launch joins a row's partials in the order of the shares.
 //
 // Bound by memory for long caches: what is fetched are the keys and values of the lengths and nothing else (counters), 8.6 GB for 16 x 131072 tokens,
-// 32/8 heads, in 1220 us (7.0 TB/s; a streaming read reaches 7.0-7.15), 775 MB for 8 x 16384-32768, 64/8 heads, in 123 us (6.3 TB/s).  Next to that the
-// chain of latencies counts: lengths, sums, page, keys, values (7.2 us of kernel for 1 x 1000 tokens), and the second launch (2.7-4.8 us).
+// 32/8 heads, in 1220 us (7.0 TB/s; a streaming read reaches 7.0-7.15), 775 MB for 8 x 16384-32768, 64/8 heads, in 123-128 us (6.0-6.3 TB/s).  Next to that the
+// chain of latencies counts: lengths, sums, page, keys, values (7.0 us of kernel for 1 x 1000 tokens), and the second launch (2.4-5.5 us).
 #include "thrift_device.h"
 #include "thrift_launch.h"
 #include "thrift_paged.h"
@@ -104,8 +104,9 @@ struct Walk {
   static constexpr int KS = D / 32;        // 16-byte pieces of a key's row per lane
   static constexpr int VC = D / 16;        // channels of a value's row per lane
   static constexpr int NR = NB * (VC * 4 + 2);                   // registers of a state
-  // the next row's queries are on their way during a step; 32 heads of 256 channels have no registers for that (64 x 2048-4096 tokens, 64/2 heads:
-  // 161 us with, 83 without)
+  // the next row's queries are on their way during a step; 32 heads of 256 channels have no registers for that: with it they
+  // take 161 us for 64 x 2048-4096 tokens of 64/2 heads, without it 83-90.  They are still short of 26 registers per lane, some of which are
+  // reloaded inside the walk; no other form uses scratch memory.
   static constexpr bool kQueryAhead = NB * D < 512;
   static constexpr int kStream = 2;        // non-temporal: keys and values are read once
   int lane, col, grp;

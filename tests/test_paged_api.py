@@ -173,6 +173,17 @@ def test_binding_refuses_what_the_kernels_cannot_index():
             T.thrift_paged_decode(**{**ok, **bad})
 
 
+def test_only_32_heads_of_256_channels_reload_registers_in_the_walk(tmp_path):
+    """Keys and values are in flight during the walk over a row's steps, and a reload of a spilled register waits for them."""
+    import os
+    import subprocess
+    from paper_2605_23081_amd import build
+    source, listing = "thrift_paged_decode.hip", tmp_path / "paged.s"
+    subprocess.run(["hipcc", *build.flags(source), "-S", "--cuda-device-only", os.path.join(build.CSRC, source), "-o", str(listing)],
+                   check=True, capture_output=True)
+    assert all("paged_decode_kernel" in k and "Li256ELi2E" in k for k in build.scratch_in_loops(listing.read_text()))
+
+
 def test_elements_that_coincide_are_seen():
     x = torch.zeros(4, 6, 8)
     assert T._apart(x) and T._apart(x.transpose(0, 2)) and T._apart(x[:, ::2]) and T._apart(x[:1].expand(1, 6, 8)) and T._apart(torch.zeros(5, 1, 3))
