@@ -377,7 +377,7 @@ thrift_status thrift_kv_cache_append_advance(const void* k_new, const void* v_ne
  * Rotary positions.  Channels 0 .. rot-1 of a head are rot/2 pairs; pair i of the token at position p is turned by the angle
  * a = p * freqs[i] and both channels are multiplied by `gain`:
  *   y0 = gain * (x0 cos a - x1 sin a),   y1 = gain * (x1 cos a + x0 sin a);     channels rot .. D-1 are copied.
- * Angles are formed and reduced in fp64, cos and sin are good to 2e-7, the products are fp32 and are rounded once.
+ * Angles are formed and reduced in fp64, cos and sin of an angle a are good to 1e-7 + 3e-16 |a|, the products are fp32 and are rounded once.
  */
 typedef enum THRIFT_ENUM_INT { THRIFT_ROPE_HALF = 0,         /* pair i: channels i and i + rot/2 */
                                THRIFT_ROPE_INTERLEAVED = 1   /* pair i: channels 2i and 2i + 1 */ } thrift_rope_layout;
@@ -481,7 +481,9 @@ size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int 
  *     of Hkv, at most 32 heads per KV head; B * Hq below 2^23, n_pages * page_size and max_pages * page_size below 2^31,
  *     B * Hkv * max_pages * page_size below 2^35
  *   seqlens [B]: cached tokens, clamped to 0 .. max_pages * page_size.  What pages hold past the length reaches no result, whatever
- *     it is.  A sequence of length 0 gives zeros.  Within the length, values are finite (an infinite one gives NaN in its channel).
+ *     it is.  A sequence of length 0 gives zeros.  Within the length, values are finite (an infinite one gives NaN in its channel)
+ *     and so is the sum of `len` of them in fp32 (bf16 reaches past that from 2^128 / len on).  A key whose score is -inf weighs nothing; a row of such
+ *     keys alone gives NaN.
  *   block_table entries within the length must name pages; others give unspecified numbers but are never followed outside
  *     k_pages and v_pages (clamped to 0 .. n_pages - 1).
  *   softmax_scale <= 0 selects 1/sqrt(D)

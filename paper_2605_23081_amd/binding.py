@@ -588,7 +588,8 @@ def thrift_rope_backward(q, k, freqs, positions: Optional[torch.Tensor] = None, 
 
 
 class PageMap(NamedTuple):
-    """Places of a step's new tokens (include/thrift.h, thrift_page_map)."""
+    """Places of a step's new tokens (include/thrift.h, thrift_page_map).  The five share one allocation, which lives as long as any of them
+    (8 bytes a row: a PageTable holds it until its next step)."""
     slots: torch.Tensor        # [rows] int32
     positions: torch.Tensor    # [rows] int32
     starts: torch.Tensor       # [B+1] int32

@@ -1,9 +1,10 @@
 // Pages of the paged 16-bit cache: block tables and slots from the lengths on the device, return of pages, and the write of
 // new tokens with the rotation of their queries and keys.
 //
-// The map is bound by latency: 5.6 us of kernel for 256 sequences with a token each, 5.8 for 64 with 262144 rows (2 MB), 6.0-6.1 with the call.  The append is
+// The map is bound by latency: 5.5 us of kernel for 256 sequences with a token each, 5.6 for 64 with 262144 rows (2 MB), 6.0-6.3 with the call.  So is the
+// release: 8.7 us of kernel for 12 of 256 sequences of up to 1024 pages, 14.6-15 with the call, whose host part passes through ctypes.  The append is
 // bound by memory: it reads and writes every element once (counters), 8192 rows of 64/8 heads in 72 us (4.7 TB/s), 32768 of 32/8 in 157
-// (5.1); a decode step's rows take the launch (3.8 us of kernel, 4.5 with the call).
+// (5.1; a copy: 6.5); a decode step's rows take the launch (3.7 us of kernel, 4.5 with the call).
 #include "thrift_paged.h"
 #include "thrift_rotary.h"
 
@@ -227,7 +228,8 @@ __global__ void __launch_bounds__(kReleaseThreads) page_release_kernel(PageRelea
 constexpr int kAppendRowThreads = 128;
 
 // One workgroup per row, a thread per pair or channel; cos and sin are formed once for all heads.  For what cannot be moved in 16-byte
-// chunks; where it can, the kernel below is faster (8192 rows of 64/8 heads: 134 us here, 78 there with cached stores as well).
+// chunks; where it can, the kernel below is faster (8192 rows of 64/8 heads: 134 us here, 78 there with cached stores as well; 208 here with 20 of
+// 128 channels turned).
 template <typename T>
 __global__ void __launch_bounds__(kAppendRowThreads) paged_append_kernel(PagedAppendArgs a) {
   const long t = blockIdx.x;

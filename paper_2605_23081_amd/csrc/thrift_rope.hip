@@ -1,8 +1,9 @@
 // Rotary positions of the query and key heads of a batch, forward and transposed (the gradient).
 //
 // Bound by memory: every element is read and written once (counters: 1.34 GB each way for 131072 tokens of 32/8 heads, which is what they hold), at
-// 5.4 TB/s there and 5.1 for 3001 tokens; a plain copy of 2 GiB runs at 4.8-4.9.  493-504 and 12.1 us; up to some hundred tokens the call is
-// its launch (3.5 us of kernel, 4 of host time, 5.8 in all).
+// 5.4 TB/s there (493-504 us); a copy in 16-byte chunks past the caches runs at 6.5 from 1 GB on, the runtime's own of 2 GiB at 4.9.  3001 tokens, 61 MB,
+// stay in the cache in front of the memory where few other bytes come between: 12.1 us then, 5.1 TB/s.  Up to some hundred tokens the
+// call is its launch (3.5-3.7 us of kernel, 4 of host time, 5.8-6.3 in all).
 #include "thrift_paged.h"
 #include "thrift_rotary.h"
 
@@ -14,7 +15,7 @@ constexpr int kRopeThreads = 128;
 
 // One workgroup per token, a thread per pair or copied channel; cos and sin are formed once for all heads.  For what cannot be read in
 // 16-byte chunks; where it can, the kernel below takes half the time (131072 tokens, 32/8 heads: 1006 us here, 538 there with cached
-// stores as well).
+// stores as well; 32768 tokens with 20 of 128 channels turned, which go here: 398 us, 147 there with 64 turned).
 template <typename T>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs a) {
   const long token = blockIdx.x;

@@ -9,7 +9,7 @@ namespace thrift {
 // cos and sin (times gain) of position * freq.  Far positions times the fastest pair's radian per token are 2^17 and more: in fp32 such an
 // angle is off by 2^-7, so it is formed in turns in fp64, where whole turns and then whole quarter turns drop out exactly.
 // What is left, at most an eighth of a turn, is fp32 from there: Taylor's polynomials, whose first term left out is below
-// 3e-8 at pi/4.  Every fused product is written out, here and in rotate: all kernels give a head the same bits.
+// 3e-8 at pi/4; with the roundings, cos and sin are within 9e-8.  Every fused product is written out, here and in rotate: all kernels give a head the same bits.
 __device__ __forceinline__ void turn(int position, double freq, float gain, float& c, float& s) {
   const double f = freq * 0.15915494309189535;                     // 1 / (2 pi)
   const double t = 4.0 * __builtin_fma((double)position, f, -__builtin_rint((double)position * f));
