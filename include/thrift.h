@@ -13,8 +13,9 @@
  *   thrift_attn_prefill_chunk  the same kernel for a chunk of queries against a longer key range
  *   thrift_attn_decode      the same algorithm for one query token over a dual 4-bit / 16-bit KV
  *                           cache (Sec. 4.1, last sentences; Sec. 5), evaluated split-K
- * and, around them, rotary positions (thrift_rope) and a paged 16-bit cache (thrift_page_map, thrift_paged_append,
- * thrift_paged_decode).
+ * and, around them, rotary positions (thrift_rope) and a paged cache in 16 bits (thrift_page_map, thrift_paged_append,
+ * thrift_paged_decode, thrift_paged_read) or 8 bits (thrift_paged_append8, thrift_paged_decode8, thrift_paged_read8), with attention over
+ * common starts of sequences (thrift_paged_decode_prefix).
  *
  * Conventions shared by every call
  *   - Every pointer is a DEVICE pointer unless the comment says "host".  The caller owns every
@@ -372,7 +373,7 @@ thrift_status thrift_kv_cache_append_advance(const void* k_new, const void* v_ne
                                              int B, int Hkv, int Nkv, int D, int Bk, void* stream);
 
 /*
- * Around the attention: rotary positions, and a paged 16-bit cache with the attention that reads it.
+ * Around the attention: rotary positions, and a paged cache with the attention that reads it.
  *
  * Rotary positions.  Channels 0 .. rot-1 of a head are rot/2 pairs; pair i of the token at position p is turned by the angle
  * a = p * freqs[i] and both channels are multiplied by `gain`:
@@ -495,6 +496,78 @@ thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_
                                   const int32_t* block_table, int max_pages, const int32_t* seqlens, int B, int Hq, int Hkv, int D,
                                   int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Tokens of a paged 16-bit cache as dense rows, which thrift_attn_prefill_chunk and a pre-pass take: token i of sequence b's row is token
+ * first[b] + i of the sequence.
+ *   k_pages, v_pages [n_pages,Hkv,page_size,D] 16-bit; block_table [B,max_pages]; seqlens [B]: cached tokens, clamped to
+ *     0 .. max_pages * page_size; first (nullable: 0) [B], negative: 0
+ *   k_out, v_out [B,Hkv,N,D] 16-bit, overlapping no input.  Tokens at or past the length, and tokens of pages that the table names outside
+ *     0 .. n_pages - 1, become 0.  The others keep their bits.
+ * D even, <= 1024; n_pages * page_size and max_pages * page_size below 2^31; B * Hkv * N below 2^31 and B * Hkv * N * D below 2^38.
+ * Moved in 16-byte accesses where D is a multiple of 8 and pages and outputs are 16-byte aligned.
+ */
+thrift_status thrift_paged_read(const void* k_pages, const void* v_pages, int n_pages, const int32_t* block_table, int max_pages,
+                                const int32_t* first, const int32_t* seqlens, int B, int Hkv, int N, int D, int page_size,
+                                void* k_out, void* v_out, void* stream);
+
+/*
+ * The paged cache in 8 bits.  A head of a token is D codes (OCP E4M3: 1 sign, 4 exponent and 3 mantissa bits, bias 7, largest number 448, no
+ * infinity, 0x7f and 0xff NaN) and one scale byte s that stands for 2^(s - 127):
+ *   a = largest finite magnitude of the head; e the least integer with a <= 448 * 2^e, held within -100 .. 120, and 0 where a is 0;
+ *   s = e + 127; a code is x * 2^-e rounded to the nearest E4M3 number, ties to the even code.  NaN and infinite elements become NaN.
+ * So a code is off by at most 2^-4 of its element, or 2^(e - 10) for elements below 2^(e - 6).
+ *   k_codes, v_codes [n_pages,Hkv,page_size,D] bytes; k_scales, v_scales [n_pages,Hkv,page_size] bytes: (D + 1) / (2 D) of the bytes of the
+ *     16-bit cache.  Pages, block tables and slots are those of thrift_page_map.
+ *
+ * thrift_paged_append8: thrift_paged_append into this cache.  Keys are quantised from their rotated fp32 values, rounded once; queries
+ * and all other arguments are as there.
+ */
+thrift_status thrift_paged_append8(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
+                                   const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,
+                                   const int32_t* positions, const double* freqs, int rot, int layout, float gain,
+                                   uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int n_pages, int page_size, int D,
+                                   void* stream);
+
+/* Host: bytes of workspace thrift_paged_decode8 needs (0: none, and for sizes that it refuses). */
+size_t thrift_paged_decode8_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D);
+
+/* thrift_paged_decode over the 8-bit cache: the numbers that codes and scales stand for take the place of keys and values, exactly; arguments,
+ * limits and results are as there.  A NaN in a key or value within the length gives NaN.  Codes and scales are 16-byte aligned. */
+thrift_status thrift_paged_decode8(const void* q, thrift_dtype dt, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                                   const uint8_t* v_scales, int n_pages, const int32_t* block_table, int max_pages, const int32_t* seqlens,
+                                   int B, int Hq, int Hkv, int D, int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* thrift_paged_read of the 8-bit cache: the numbers that codes and scales stand for, rounded to dt.  Within dt's normal range they are exact; past its
+ * largest finite number they become that (a head's largest elements may be rounded up past it). */
+thrift_status thrift_paged_read8(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes, const uint8_t* v_scales, int n_pages,
+                                 const int32_t* block_table, int max_pages, const int32_t* first, const int32_t* seqlens, int B, int Hkv, int N,
+                                 int D, int page_size, void* k_out, void* v_out, thrift_dtype dt, void* stream);
+
+/* Host: bytes of workspace thrift_paged_decode_prefix (bits 16) and thrift_paged_decode_prefix8 (bits 8) need; 0 for sizes that they refuse. */
+size_t thrift_paged_decode_prefix_workspace(int bits, int B, int Hq, int Hkv, int n_groups, int max_pages, int page_size, int D);
+
+/*
+ * Attention of one new token per sequence where sequences start with the same pages: thrift_paged_decode, with the keys and values of a common
+ * start read once for all of its sequences.  The result is that of thrift_paged_decode but for the order of its fp32 sums, and for the
+ * probabilities of the common tokens, which are rounded to 16 bits (dt's; bf16 over the 8-bit cache) for the product with the values.
+ *   group_of [B] int32: the group of each sequence, any order; a number outside 0 .. n_groups - 1: none
+ *   group_lens [n_groups] int32: tokens in front that the sequences of a group have in the same pages, rounded down to whole pages, at most
+ *     max_pages * page_size.  They are read through the block table of one of them.  A sequence shorter than that, or of no group, is read
+ *     by itself.
+ *   1 <= n_groups <= 4096; B <= 4096; all other arguments, limits and results as thrift_paged_decode; a workspace is always needed
+ */
+thrift_status thrift_paged_decode_prefix(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,
+                                         const int32_t* block_table, int max_pages, const int32_t* seqlens, const int32_t* group_of,
+                                         const int32_t* group_lens, int n_groups, int B, int Hq, int Hkv, int D, int page_size,
+                                         float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                         void* workspace, size_t workspace_bytes, void* stream);
+thrift_status thrift_paged_decode_prefix8(const void* q, thrift_dtype dt, const uint8_t* k_codes, const uint8_t* k_scales,
+                                          const uint8_t* v_codes, const uint8_t* v_scales, int n_pages, const int32_t* block_table, int max_pages,
+                                          const int32_t* seqlens, const int32_t* group_of, const int32_t* group_lens, int n_groups, int B,
+                                          int Hq, int Hkv, int D, int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                          void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement helper (not a step of the method): one launch of a microbenchmark of a hardware rate that the

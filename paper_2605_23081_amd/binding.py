@@ -29,7 +29,9 @@ EXPORTS = (
     "thrift_kv_cache_append", "thrift_kv_cache_append_advance",
     "thrift_attention_forward_workspace", "thrift_attention_forward",
     "thrift_rope_frequencies", "thrift_rope", "thrift_rope_backward", "thrift_page_map", "thrift_page_release",
-    "thrift_paged_append", "thrift_paged_decode_workspace", "thrift_paged_decode", "thrift_peak_probe",
+    "thrift_paged_append", "thrift_paged_decode_workspace", "thrift_paged_decode", "thrift_paged_read",
+    "thrift_paged_append8", "thrift_paged_decode8_workspace", "thrift_paged_decode8", "thrift_paged_read8",
+    "thrift_paged_decode_prefix_workspace", "thrift_paged_decode_prefix", "thrift_paged_decode_prefix8", "thrift_peak_probe",
 )
 
 _lib = None
@@ -95,6 +97,15 @@ def lib() -> C.CDLL:
         L.thrift_paged_decode_workspace.restype = sz
         L.thrift_paged_decode_workspace.argtypes = [i] * 6
         L.thrift_paged_decode.argtypes = [p, i, p, p, i, p, i, p, i, i, i, i, i, f, p, i, p, p, sz, p]
+        L.thrift_paged_read.argtypes = [p, p, i, p, i, p, p, i, i, i, i, i, p, p, p]
+        L.thrift_paged_append8.argtypes = [p, p, p, i, p, p, p, p, i, i, i, p, p, p, i, i, f, p, p, p, p, i, i, i, p]
+        L.thrift_paged_decode8_workspace.restype = L.thrift_paged_decode_prefix_workspace.restype = sz
+        L.thrift_paged_decode8_workspace.argtypes = [i] * 6
+        L.thrift_paged_decode8.argtypes = [p, i, p, p, p, p, i, p, i, p, i, i, i, i, i, f, p, i, p, p, sz, p]
+        L.thrift_paged_read8.argtypes = [p, p, p, p, i, p, i, p, p, i, i, i, i, i, p, p, i, p]
+        L.thrift_paged_decode_prefix_workspace.argtypes = [i] * 8
+        L.thrift_paged_decode_prefix.argtypes = [p, i, p, p, i, p, i, p, p, p, i, i, i, i, i, i, f, p, i, p, p, sz, p]
+        L.thrift_paged_decode_prefix8.argtypes = [p, i, p, p, p, p, i, p, i, p, p, p, i, i, i, i, i, i, f, p, i, p, p, sz, p]
         L.thrift_peak_probe.argtypes = [C.c_int, C.c_int, C.c_int, p, sz, C.POINTER(C.c_double), p]
         _lib = L
     return _lib
@@ -497,7 +508,7 @@ def thrift_peak_probe(kind: int, buffer: torch.Tensor, iters: int = 2000, dtype:
     return float(work.value)
 
 
-# ---- around the attention: rotary positions and the paged 16-bit cache ----
+# ---- around the attention: rotary positions and the paged cache ----
 
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "by_parts": 3}
@@ -644,19 +655,18 @@ def _pages(k_pages, v_pages) -> None:
     assert k_pages.shape == v_pages.shape and k_pages.dtype == v_pages.dtype and k_pages.is_contiguous() and v_pages.is_contiguous()
 
 
-def thrift_paged_append(k, v, slots, k_pages, v_pages, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
-                        positions: Optional[torch.Tensor] = None, freqs: Optional[torch.Tensor] = None, layout: str = "half",
-                        gain: float = 1.0) -> Optional[torch.Tensor]:
-    """k, v [T,Hkv,D] into the pages [n_pages,Hkv,page_size,D] at slots [T]; with freqs, k and q [T,Hq,D] are rotated to
-    positions [T].  Returns q_out (contiguous; rows of skipped tokens are left as they were)."""
-    r = (_call or _native()).paged_append(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs, ROPE_LAYOUTS[layout], gain, *_here_now())
-    if r is not None:
-        return None if r is True else _result(r, "thrift_paged_append")
-    _pages(k_pages, v_pages)
+def _pages8(k_codes, k_scales, v_codes, v_scales) -> None:
+    assert k_codes.dim() == 4 and k_codes.shape == v_codes.shape and k_scales.shape == v_scales.shape == k_codes.shape[:3], \
+        (tuple(k_codes.shape), tuple(k_scales.shape), tuple(v_codes.shape), tuple(v_scales.shape))
+    assert all(t.dtype == torch.uint8 and t.is_contiguous() for t in (k_codes, k_scales, v_codes, v_scales))
+
+
+def _paged_append(name: str, k, v, slots, pages, dtype, q, q_out, positions, freqs, layout: str, gain: float):
+    """pages: the tensors of the cache, the first of them [n_pages,Hkv,page_size,D]."""
     T, Hkv, D = k.shape
-    n_pages, _, page_size, _ = k_pages.shape
-    _heads(k, (T, Hkv, D), k_pages.dtype), _heads(v, (T, Hkv, D), k_pages.dtype), _ints((T,), slots)
-    assert k_pages.shape[1] == Hkv and k_pages.shape[3] == D, (tuple(k_pages.shape), tuple(k.shape))
+    n_pages, _, page_size, _ = pages[0].shape
+    _heads(k, (T, Hkv, D), dtype), _heads(v, (T, Hkv, D), dtype), _ints((T,), slots)
+    assert pages[0].shape[1] == Hkv and pages[0].shape[3] == D, (tuple(pages[0].shape), tuple(k.shape))
     rot = 0
     if freqs is not None:
         assert freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and freqs.numel() > 0, (freqs.dtype, tuple(freqs.shape))
@@ -666,20 +676,109 @@ def thrift_paged_append(k, v, slots, k_pages, v_pages, q: Optional[torch.Tensor]
     if q is None:
         assert q_out is None
     else:
-        _heads(q, (T, q.shape[1], D), k_pages.dtype)
+        _heads(q, (T, q.shape[1], D), dtype)
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         assert q_out.shape == q.shape and q_out.dtype == q.dtype and q_out.is_contiguous(), (tuple(q_out.shape), q_out.dtype)
-    _here(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs)
+    _here(k, v, slots, *pages, q, q_out, positions, freqs)
     s = lambda t: None if t is None else _strides(t, (0, 1))
-    _check(lib().thrift_paged_append(_ptr(q), s(q), _ptr(q_out), 0 if q is None else q.shape[1], _ptr(k), s(k), _ptr(v), s(v), Hkv,
-                                     _DT[k.dtype], T, _ptr(slots), _ptr(positions), _ptr(freqs), rot, ROPE_LAYOUTS[layout], float(gain),
-                                     _ptr(k_pages), _ptr(v_pages), n_pages, page_size, D, _stream()), "thrift_paged_append")
+    _check(getattr(lib(), name)(_ptr(q), s(q), _ptr(q_out), 0 if q is None else q.shape[1], _ptr(k), s(k), _ptr(v), s(v), Hkv,
+                                _DT[k.dtype], T, _ptr(slots), _ptr(positions), _ptr(freqs), rot, ROPE_LAYOUTS[layout], float(gain),
+                                *(_ptr(t) for t in pages), n_pages, page_size, D, _stream()), name)
     return q_out
+
+
+def thrift_paged_append(k, v, slots, k_pages, v_pages, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                        positions: Optional[torch.Tensor] = None, freqs: Optional[torch.Tensor] = None, layout: str = "half",
+                        gain: float = 1.0) -> Optional[torch.Tensor]:
+    """k, v [T,Hkv,D] into the pages [n_pages,Hkv,page_size,D] at slots [T]; with freqs, k and q [T,Hq,D] are rotated to
+    positions [T].  Returns q_out (contiguous; rows of skipped tokens are left as they were)."""
+    r = (_call or _native()).paged_append(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs, ROPE_LAYOUTS[layout], gain, *_here_now())
+    if r is not None:
+        return None if r is True else _result(r, "thrift_paged_append")
+    _pages(k_pages, v_pages)
+    return _paged_append("thrift_paged_append", k, v, slots, (k_pages, v_pages), k_pages.dtype, q, q_out, positions, freqs, layout, gain)
+
+
+def thrift_paged_append8(k, v, slots, k_codes, k_scales, v_codes, v_scales, q: Optional[torch.Tensor] = None,
+                         q_out: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                         freqs: Optional[torch.Tensor] = None, layout: str = "half", gain: float = 1.0) -> Optional[torch.Tensor]:
+    """thrift_paged_append into the 8-bit cache: codes [n_pages,Hkv,page_size,D] and scales [n_pages,Hkv,page_size], bytes."""
+    pages = (k_codes, k_scales, v_codes, v_scales)
+    _pages8(*pages)
+    assert k.dtype in (torch.float16, torch.bfloat16), k.dtype
+    return _paged_append("thrift_paged_append8", k, v, slots, pages, k.dtype, q, q_out, positions, freqs, layout, gain)
+
+
+def _paged_read(name: str, pages, block_table, seqlens, N: int, dtype, first, k_out, v_out, *last):
+    assert block_table.dim() == 2, tuple(block_table.shape)
+    B, max_pages = block_table.shape
+    n_pages, Hkv, page_size, D = pages[0].shape
+    _ints((B, max_pages), block_table), _ints((B,), seqlens)
+    if first is not None:
+        _ints((B,), first)
+    out = [torch.empty(B, Hkv, max(N, 0), D, dtype=dtype, device=block_table.device) if x is None else x for x in (k_out, v_out)]
+    for x in out:
+        assert tuple(x.shape) == (B, Hkv, N, D) and x.dtype == dtype and x.is_contiguous(), (tuple(x.shape), x.dtype)
+    _here(*pages, block_table, seqlens, first, *out)
+    _check(getattr(lib(), name)(*(_ptr(t) for t in pages), n_pages, _ptr(block_table), max_pages, _ptr(first), _ptr(seqlens), B, Hkv, N, D,
+                                page_size, *(_ptr(t) for t in out), *last, _stream()), name)
+    return tuple(out)
+
+
+def thrift_paged_read(k_pages, v_pages, block_table, seqlens, N: int, first: Optional[torch.Tensor] = None,
+                      k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Tokens first[b] .. first[b] + N - 1 (default: from 0) of every sequence as rows (k, v) [B,Hkv,N,D]; 0 past the lengths."""
+    _pages(k_pages, v_pages)
+    return _paged_read("thrift_paged_read", (k_pages, v_pages), block_table, seqlens, N, k_pages.dtype, first, k_out, v_out)
+
+
+def thrift_paged_read8(k_codes, k_scales, v_codes, v_scales, block_table, seqlens, N: int, dtype: torch.dtype = torch.bfloat16,
+                       first: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                       v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """thrift_paged_read of the 8-bit cache, in dtype."""
+    _pages8(k_codes, k_scales, v_codes, v_scales)
+    assert dtype in (torch.float16, torch.bfloat16), dtype
+    return _paged_read("thrift_paged_read8", (k_codes, k_scales, v_codes, v_scales), block_table, seqlens, N, dtype, first, k_out, v_out, _DT[dtype])
 
 
 def paged_decode_workspace_bytes(B: int, Hq: int, Hkv: int, max_pages: int, page_size: int, D: int) -> int:
     return int(lib().thrift_paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D))
+
+
+def paged_decode8_workspace_bytes(B: int, Hq: int, Hkv: int, max_pages: int, page_size: int, D: int) -> int:
+    return int(lib().thrift_paged_decode8_workspace(B, Hq, Hkv, max_pages, page_size, D))
+
+
+def paged_decode_prefix_workspace_bytes(bits: int, B: int, Hq: int, Hkv: int, n_groups: int, max_pages: int, page_size: int, D: int) -> int:
+    return int(lib().thrift_paged_decode_prefix_workspace(bits, B, Hq, Hkv, n_groups, max_pages, page_size, D))
+
+
+def _paged_decode(name: str, q, pages, block_table, seqlens, groups, need, softmax_scale: float, out, out_dtype, lse, return_lse: bool, workspace):
+    """groups: () or (group_of, group_lens); need(B, Hq, Hkv, max_pages, page_size, D): bytes of workspace."""
+    B, Hq, D = q.shape
+    n_pages, Hkv, page_size, _ = pages[0].shape
+    assert _dev(q).dtype in (torch.float16, torch.bfloat16) and pages[0].shape[3] == D, (q.dtype, tuple(q.shape), tuple(pages[0].shape))
+    assert block_table.dim() == 2, tuple(block_table.shape)
+    max_pages = block_table.shape[1]
+    _ints((B, max_pages), block_table), _ints((B,), seqlens)
+    if groups:
+        _ints((B,), groups[0]), _ints((groups[1].numel(),), groups[1])
+    if out is None:
+        out = torch.empty(B, Hq, D, dtype=out_dtype or q.dtype, device=q.device)
+    assert tuple(_dev(out).shape) == (B, Hq, D) and out.dtype in _DT, (tuple(out.shape), out.dtype)
+    if lse is None and return_lse:
+        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
+    assert lse is None or tuple(_dev(lse, torch.float32).shape) == (B, Hq)
+    if workspace is None:
+        workspace = torch.empty(need(B, Hq, Hkv, max_pages, page_size, D), dtype=torch.uint8, device=q.device)
+    _dev(workspace, torch.uint8)
+    _here(q, *pages, block_table, seqlens, *groups, out, lse, workspace)
+    more = (_ptr(groups[0]), _ptr(groups[1]), groups[1].numel()) if groups else ()
+    _check(getattr(lib(), name)(_ptr(q), _DT[q.dtype], *(_ptr(t) for t in pages), n_pages, _ptr(block_table), max_pages, _ptr(seqlens), *more,
+                                B, Hq, Hkv, D, page_size, float(softmax_scale), _ptr(out), _DT[out.dtype], _ptr(lse),
+                                _ptr(workspace), workspace.numel(), _stream()), name)
+    return (out, lse) if return_lse else out
 
 
 def thrift_paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
@@ -692,27 +791,40 @@ def thrift_paged_decode(q, k_pages, v_pages, block_table, seqlens, softmax_scale
         if r is not None:
             return _result(r, "thrift_paged_decode")
     _pages(k_pages, v_pages)
-    B, Hq, D = q.shape
-    n_pages, Hkv, page_size, _ = k_pages.shape
-    assert _dev(q).dtype == k_pages.dtype and k_pages.shape[3] == D, (q.dtype, k_pages.dtype, tuple(q.shape), tuple(k_pages.shape))
-    assert block_table.dim() == 2, tuple(block_table.shape)
-    max_pages = block_table.shape[1]
-    _ints((B, max_pages), block_table), _ints((B,), seqlens)
-    if out is None:
-        out = torch.empty(B, Hq, D, dtype=out_dtype or q.dtype, device=q.device)
-    assert tuple(_dev(out).shape) == (B, Hq, D) and out.dtype in _DT, (tuple(out.shape), out.dtype)
-    if lse is None and return_lse:
-        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
-    assert lse is None or tuple(_dev(lse, torch.float32).shape) == (B, Hq)
-    if workspace is None:
-        need = paged_decode_workspace_bytes(B, Hq, Hkv, max_pages, page_size, D)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _dev(workspace, torch.uint8)
-    _here(q, k_pages, v_pages, block_table, seqlens, out, lse, workspace)
-    _check(lib().thrift_paged_decode(_ptr(q), _DT[q.dtype], _ptr(k_pages), _ptr(v_pages), n_pages, _ptr(block_table), max_pages, _ptr(seqlens),
-                                     B, Hq, Hkv, D, page_size, float(softmax_scale), _ptr(out), _DT[out.dtype], _ptr(lse),
-                                     _ptr(workspace), workspace.numel(), _stream()), "thrift_paged_decode")
-    return (out, lse) if return_lse else out
+    assert q.dtype == k_pages.dtype, (q.dtype, k_pages.dtype)
+    return _paged_decode("thrift_paged_decode", q, (k_pages, v_pages), block_table, seqlens, (), paged_decode_workspace_bytes, softmax_scale,
+                         out, out_dtype, lse, return_lse, workspace)
+
+
+def thrift_paged_decode8(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, softmax_scale: float = 0.0,
+                         out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None, lse: Optional[torch.Tensor] = None,
+                         return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """thrift_paged_decode over the 8-bit cache."""
+    _pages8(k_codes, k_scales, v_codes, v_scales)
+    return _paged_decode("thrift_paged_decode8", q, (k_codes, k_scales, v_codes, v_scales), block_table, seqlens, (),
+                         paged_decode8_workspace_bytes, softmax_scale, out, out_dtype, lse, return_lse, workspace)
+
+
+def thrift_paged_decode_prefix(q, k_pages, v_pages, block_table, seqlens, group_of, group_lens, softmax_scale: float = 0.0,
+                               out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                               lse: Optional[torch.Tensor] = None, return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """thrift_paged_decode where the sequences of group g (group_of [B] == g) have the same pages for their first group_lens [n_groups] [g]
+    tokens, which are read once for all of them."""
+    _pages(k_pages, v_pages)
+    assert q.dtype == k_pages.dtype, (q.dtype, k_pages.dtype)
+    need = lambda B, Hq, Hkv, *sizes: paged_decode_prefix_workspace_bytes(16, B, Hq, Hkv, group_lens.numel(), *sizes)
+    return _paged_decode("thrift_paged_decode_prefix", q, (k_pages, v_pages), block_table, seqlens, (group_of, group_lens), need, softmax_scale,
+                         out, out_dtype, lse, return_lse, workspace)
+
+
+def thrift_paged_decode_prefix8(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, group_of, group_lens,
+                                softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                                lse: Optional[torch.Tensor] = None, return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """thrift_paged_decode_prefix over the 8-bit cache."""
+    _pages8(k_codes, k_scales, v_codes, v_scales)
+    need = lambda B, Hq, Hkv, *sizes: paged_decode_prefix_workspace_bytes(8, B, Hq, Hkv, group_lens.numel(), *sizes)
+    return _paged_decode("thrift_paged_decode_prefix8", q, (k_codes, k_scales, v_codes, v_scales), block_table, seqlens, (group_of, group_lens),
+                         need, softmax_scale, out, out_dtype, lse, return_lse, workspace)
 
 
 class PageTable:
@@ -755,6 +867,47 @@ class PagedKVCache:
     def decode(self, q, softmax_scale: float = 0.0, **kw):
         """Attention of q [B,Hq,D], the newest token of every sequence (thrift_paged_decode)."""
         return thrift_paged_decode(q, self.k_pages, self.v_pages, self.table.block_table, self.table.seqlens, softmax_scale, **kw)
+
+    def read(self, N: int, first: Optional[torch.Tensor] = None, **kw) -> Tuple[torch.Tensor, torch.Tensor]:
+        """N tokens of every sequence as dense rows (thrift_paged_read)."""
+        return thrift_paged_read(self.k_pages, self.v_pages, self.table.block_table, self.table.seqlens, N, first, **kw)
+
+    def decode_prefix(self, q, group_of, group_lens, softmax_scale: float = 0.0, **kw):
+        """decode where the sequences of a group start with the same pages (thrift_paged_decode_prefix)."""
+        return thrift_paged_decode_prefix(q, self.k_pages, self.v_pages, self.table.block_table, self.table.seqlens, group_of, group_lens,
+                                          softmax_scale, **kw)
+
+
+class PagedKVCache8:
+    """8-bit pages of one layer, with the methods of PagedKVCache; dtype: of the keys and values that are read back."""
+
+    def __init__(self, table: PageTable, Hkv: int, D: int, dtype):
+        u8, dev = torch.uint8, table.block_table.device
+        shape = (table.n_pages, Hkv, table.page_size)
+        self.table, self.dtype = table, dtype
+        self.k_codes, self.v_codes = (torch.empty(*shape, D, dtype=u8, device=dev) for _ in range(2))
+        self.k_scales, self.v_scales = (torch.empty(shape, dtype=u8, device=dev) for _ in range(2))
+
+    @property
+    def pages(self) -> Tuple[torch.Tensor, ...]:
+        return self.k_codes, self.k_scales, self.v_codes, self.v_scales
+
+    def append(self, k, v, m: PageMap, q: Optional[torch.Tensor] = None, freqs: Optional[torch.Tensor] = None, layout: str = "half",
+               gain: float = 1.0, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """k, v [T,Hkv,D] of the step's rows into the pages, rotated with q [T,Hq,D] where freqs is given; returns the rotated q."""
+        return thrift_paged_append8(k, v, m.slots, *self.pages, q, q_out, m.positions, freqs, layout, gain)
+
+    def decode(self, q, softmax_scale: float = 0.0, **kw):
+        """Attention of q [B,Hq,D], the newest token of every sequence (thrift_paged_decode8)."""
+        return thrift_paged_decode8(q, *self.pages, self.table.block_table, self.table.seqlens, softmax_scale, **kw)
+
+    def read(self, N: int, first: Optional[torch.Tensor] = None, **kw) -> Tuple[torch.Tensor, torch.Tensor]:
+        """N tokens of every sequence as dense rows of the cache's dtype (thrift_paged_read8)."""
+        return thrift_paged_read8(*self.pages, self.table.block_table, self.table.seqlens, N, self.dtype, first, **kw)
+
+    def decode_prefix(self, q, group_of, group_lens, softmax_scale: float = 0.0, **kw):
+        """decode where the sequences of a group start with the same pages (thrift_paged_decode_prefix8)."""
+        return thrift_paged_decode_prefix8(q, *self.pages, self.table.block_table, self.table.seqlens, group_of, group_lens, softmax_scale, **kw)
 
 
 # ---- Alg. 1 end to end: the user-level form of the paper's signature ----

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libthrift_hip.so")
 CALL = os.path.join(HERE, "_call.so")          # the Python entry of the calls of a serving loop (host code only)
-SOURCES = ["thrift_api.hip", "thrift_prepass.hip", "thrift_prefill.hip", "thrift_prefill_split.hip", "thrift_decode.hip", "thrift_decode_split.hip", "thrift_cache.hip", "thrift_rope.hip", "thrift_pages.hip", "thrift_paged_decode.hip", "thrift_probe.hip"]
+SOURCES = ["thrift_api.hip", "thrift_prepass.hip", "thrift_prefill.hip", "thrift_prefill_split.hip", "thrift_decode.hip", "thrift_decode_split.hip", "thrift_cache.hip", "thrift_rope.hip", "thrift_pages.hip", "thrift_paged_decode.hip", "thrift_paged_read.hip", "thrift_pages8.hip", "thrift_paged_prefix.hip", "thrift_probe.hip"]
 DMA_SOURCES = ["thrift_prefill.hip", "thrift_prefill_split.hip", "thrift_decode.hip", "thrift_decode_split.hip"]      # kernels whose inline assembly sets M0 and keeps DMA in flight
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # NaN inputs are outside the contract (include/thrift.h); without this every maximum of matrix-unit results
@@ -21,7 +21,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-u
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", INCLUDE, "-I", CSRC]
 # rotary positions and the paged cache pass a NaN of their inputs on as plain arithmetic does
-HONOR_NANS = ["thrift_rope.hip", "thrift_pages.hip", "thrift_paged_decode.hip"]
+HONOR_NANS = ["thrift_rope.hip", "thrift_pages.hip", "thrift_paged_decode.hip", "thrift_paged_read.hip", "thrift_pages8.hip", "thrift_paged_prefix.hip"]
 
 
 def flags(src):

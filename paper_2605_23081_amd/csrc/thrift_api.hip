@@ -703,55 +703,184 @@ thrift_status thrift_page_release(const int32_t* seqlens, const int32_t* drop, i
   return after_launch();
 }
 
-thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
-                                  const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,
-                                  const int32_t* positions, const double* freqs, int rot, int layout, float gain,
-                                  void* k_pages, void* v_pages, int n_pages, int page_size, int D, void* stream) {
+static thrift_status paged_append_args(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
+                                       const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,
+                                       const int32_t* positions, const double* freqs, int rot, int layout, float gain,
+                                       void* k_pages, void* v_pages, int n_pages, int page_size, int D, PagedAppendArgs& a) {
   if (!k || !v || !slots || !k_pages || !v_pages || (q && !q_out) || (rot != 0 && (!positions || !freqs))) return THRIFT_ERR_NULL;
   if (!is16(dt)) return THRIFT_ERR_DTYPE;
   if (!fits_int(T, 256) || (q && (Hq <= 0 || !fits_int(Hq, D))) || Hkv <= 0 || !fits_int(Hkv, D) || D < 2 || D > kRopeMaxDim || D % 2 != 0 ||
       (rot != 0 && !rope_ok(rot, layout, D)) || !page_size_ok(page_size) || !fits_int(n_pages, page_size))
     return THRIFT_ERR_SHAPE;
-  if (thrift_status s = check_arch()) return s;
-  PagedAppendArgs a;
   a.q = (const uint16_t*)q; a.k = (const uint16_t*)k; a.v = (const uint16_t*)v; a.q_out = (uint16_t*)q_out;
   a.qt = q_strides ? (long)q_strides[0] : (long)Hq * D; a.qh = q_strides ? (long)q_strides[1] : D;
   a.kt = k_strides ? (long)k_strides[0] : (long)Hkv * D; a.kh = k_strides ? (long)k_strides[1] : D;
   a.vt = v_strides ? (long)v_strides[0] : (long)Hkv * D; a.vh = v_strides ? (long)v_strides[1] : D;
   a.slots = slots; a.positions = positions; a.freqs = freqs; a.k_pages = (uint16_t*)k_pages; a.v_pages = (uint16_t*)v_pages;
   a.T = T; a.Hq = q ? Hq : 0; a.Hkv = Hkv; a.D = D; a.rot = rot; a.layout = layout; a.n_pages = n_pages; a.page_size = page_size; a.gain = gain;
+  return check_arch();
+}
+
+thrift_status thrift_paged_append(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
+                                  const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,
+                                  const int32_t* positions, const double* freqs, int rot, int layout, float gain,
+                                  void* k_pages, void* v_pages, int n_pages, int page_size, int D, void* stream) {
+  PagedAppendArgs a;
+  if (thrift_status s = paged_append_args(q, q_strides, q_out, Hq, k, k_strides, v, v_strides, Hkv, dt, T, slots, positions, freqs, rot, layout, gain,
+                                          k_pages, v_pages, n_pages, page_size, D, a))
+    return s;
   launch_paged_append(a, dt, (hipStream_t)stream);
   return after_launch();
+}
+
+thrift_status thrift_paged_append8(const void* q, const int64_t* q_strides, void* q_out, int Hq, const void* k, const int64_t* k_strides,
+                                   const void* v, const int64_t* v_strides, int Hkv, thrift_dtype dt, int T, const int32_t* slots,
+                                   const int32_t* positions, const double* freqs, int rot, int layout, float gain,
+                                   uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, int n_pages, int page_size, int D,
+                                   void* stream) {
+  if (!k_scales || !v_scales) return THRIFT_ERR_NULL;
+  PagedAppend8Args a;
+  if (thrift_status s = paged_append_args(q, q_strides, q_out, Hq, k, k_strides, v, v_strides, Hkv, dt, T, slots, positions, freqs, rot, layout, gain,
+                                          k_codes, v_codes, n_pages, page_size, D, a.in))
+    return s;
+  a.k_codes = k_codes; a.k_scales = k_scales; a.v_codes = v_codes; a.v_scales = v_scales;
+  launch_paged_append8(a, dt, (hipStream_t)stream);
+  return after_launch();
+}
+
+static thrift_status paged_read_impl(const void* k_pages, const uint8_t* k_scales, const void* v_pages, const uint8_t* v_scales, int n_pages,
+                                     const int32_t* block_table, int max_pages, const int32_t* first, const int32_t* seqlens, int B, int Hkv,
+                                     int N, int D, int page_size, void* k_out, void* v_out, thrift_dtype dt, void* stream) {
+  if (!k_pages || !v_pages || !block_table || !seqlens || !k_out || !v_out) return THRIFT_ERR_NULL;
+  if (!is16(dt)) return THRIFT_ERR_DTYPE;
+  if (D < 2 || D > kRopeMaxDim || D % 2 != 0 || !page_size_ok(page_size) || !fits_int(n_pages, page_size) || !fits_int(max_pages, page_size) ||
+      !fits_int(B, Hkv, N) || (long)B * Hkv * N * D >= 1L << 38)
+    return THRIFT_ERR_SHAPE;
+  if (thrift_status s = check_arch()) return s;
+  PagedReadArgs a;
+  a.k_pages = k_pages; a.v_pages = v_pages; a.k_scales = k_scales; a.v_scales = v_scales; a.table = block_table; a.first = first; a.seqlens = seqlens;
+  a.k_out = (uint16_t*)k_out; a.v_out = (uint16_t*)v_out;
+  a.B = B; a.Hkv = Hkv; a.N = N; a.D = D; a.n_pages = n_pages; a.max_pages = max_pages; a.page_size = page_size;
+  launch_paged_read(a, dt, (hipStream_t)stream);
+  return after_launch();
+}
+
+thrift_status thrift_paged_read(const void* k_pages, const void* v_pages, int n_pages, const int32_t* block_table, int max_pages,
+                                const int32_t* first, const int32_t* seqlens, int B, int Hkv, int N, int D, int page_size,
+                                void* k_out, void* v_out, void* stream) {
+  return paged_read_impl(k_pages, nullptr, v_pages, nullptr, n_pages, block_table, max_pages, first, seqlens, B, Hkv, N, D, page_size, k_out, v_out,
+                         THRIFT_F16, stream);
+}
+
+thrift_status thrift_paged_read8(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes, const uint8_t* v_scales, int n_pages,
+                                 const int32_t* block_table, int max_pages, const int32_t* first, const int32_t* seqlens, int B, int Hkv, int N,
+                                 int D, int page_size, void* k_out, void* v_out, thrift_dtype dt, void* stream) {
+  if (!k_scales || !v_scales) return THRIFT_ERR_NULL;
+  return paged_read_impl(k_codes, k_scales, v_codes, v_scales, n_pages, block_table, max_pages, first, seqlens, B, Hkv, N, D, page_size, k_out, v_out,
+                         dt, stream);
 }
 
 static bool paged_decode_ok(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
   return B > 0 && Hq > 0 && Hkv > 0 && Hq % Hkv == 0 && Hq / Hkv <= 32 && (D == 64 || D == 128 || D == 256) && page_size_ok(page_size) &&
          fits_int(max_pages, page_size) && fits_int(B, Hq, 256) && fits_int(2L * B, Hkv, ((long)max_pages * page_size + 31) / 32);
 }
+static bool prefix_ok(int B, int n_groups) { return B <= kMapMaxSeqs && n_groups > 0 && n_groups <= kMapMaxSeqs; }
 
 size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
   return paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) ? paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D) : 0;
+}
+size_t thrift_paged_decode8_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
+  return paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) ? paged_decode8_workspace(B, Hq, Hkv, max_pages, page_size, D) : 0;
+}
+size_t thrift_paged_decode_prefix_workspace(int bits, int B, int Hq, int Hkv, int n_groups, int max_pages, int page_size, int D) {
+  return (bits == 16 || bits == 8) && paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) && prefix_ok(B, n_groups)
+             ? paged_prefix_workspace(bits, B, Hq, Hkv, n_groups, max_pages, page_size, D) : 0;
+}
+
+// scales: whether the pages are codes with scales
+static thrift_status paged_decode_args(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, bool scales, const uint8_t* k_scales,
+                                       const uint8_t* v_scales, int n_pages, const int32_t* block_table, int max_pages, const int32_t* seqlens,
+                                       int B, int Hq, int Hkv, int D, int page_size, float softmax_scale, void* out, thrift_dtype out_dt,
+                                       float* lse, void* workspace, PagedDecodeArgs& a) {
+  if (!q || !k_pages || !v_pages || !block_table || !seqlens || !out || (scales && (!k_scales || !v_scales))) return THRIFT_ERR_NULL;
+  if (!is16(dt) || !is_out(out_dt)) return THRIFT_ERR_DTYPE;
+  if (!paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) || !fits_int(n_pages, page_size)) return THRIFT_ERR_SHAPE;
+  if ((((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)out | (uintptr_t)k_scales | (uintptr_t)v_scales) & 15) != 0)
+    return THRIFT_ERR_SHAPE;
+  a.q = (const uint16_t*)q; a.k_pages = k_pages; a.v_pages = v_pages; a.k_scales = k_scales; a.v_scales = v_scales; a.table = block_table;
+  a.seqlens = seqlens; a.out = out; a.lse = lse; a.workspace = workspace;
+  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.n_pages = n_pages; a.max_pages = max_pages; a.page_size = page_size;
+  a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D);
+  a.dt = dt; a.out_dt = out_dt;
+  return THRIFT_OK;
+}
+static thrift_status workspace_ok(size_t need, const void* workspace, size_t bytes) {
+  return need > 0 && (!workspace || bytes < need || ((uintptr_t)workspace & 15) != 0) ? THRIFT_ERR_WORKSPACE : THRIFT_OK;
 }
 
 thrift_status thrift_paged_decode(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,
                                   const int32_t* block_table, int max_pages, const int32_t* seqlens, int B, int Hq, int Hkv, int D,
                                   int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
                                   void* workspace, size_t workspace_bytes, void* stream) {
-  if (!q || !k_pages || !v_pages || !block_table || !seqlens || !out) return THRIFT_ERR_NULL;
-  if (!is16(dt) || !is_out(out_dt)) return THRIFT_ERR_DTYPE;
-  if (!paged_decode_ok(B, Hq, Hkv, max_pages, page_size, D) || !fits_int(n_pages, page_size)) return THRIFT_ERR_SHAPE;
-  if ((((uintptr_t)q | (uintptr_t)k_pages | (uintptr_t)v_pages | (uintptr_t)out) & 15) != 0) return THRIFT_ERR_SHAPE;
-  const size_t need = paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D);
-  if (need > 0 && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15) != 0)) return THRIFT_ERR_WORKSPACE;
-  if (thrift_status s = check_arch()) return s;
   PagedDecodeArgs a;
-  a.q = (const uint16_t*)q; a.k_pages = (const uint16_t*)k_pages; a.v_pages = (const uint16_t*)v_pages; a.table = block_table;
-  a.seqlens = seqlens; a.out = out; a.lse = lse; a.workspace = workspace;
-  a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.D = D; a.n_pages = n_pages; a.max_pages = max_pages; a.page_size = page_size;
-  a.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)D);
-  a.dt = dt; a.out_dt = out_dt;
+  if (thrift_status s = paged_decode_args(q, dt, k_pages, v_pages, false, nullptr, nullptr, n_pages, block_table, max_pages, seqlens, B, Hq, Hkv, D,
+                                          page_size, softmax_scale, out, out_dt, lse, workspace, a))
+    return s;
+  if (thrift_status s = workspace_ok(paged_decode_workspace(B, Hq, Hkv, max_pages, page_size, D), workspace, workspace_bytes)) return s;
+  if (thrift_status s = check_arch()) return s;
   launch_paged_decode(a, (hipStream_t)stream);
   return after_launch();
+}
+
+thrift_status thrift_paged_decode8(const void* q, thrift_dtype dt, const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                                   const uint8_t* v_scales, int n_pages, const int32_t* block_table, int max_pages, const int32_t* seqlens,
+                                   int B, int Hq, int Hkv, int D, int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream) {
+  PagedDecodeArgs a;
+  if (thrift_status s = paged_decode_args(q, dt, k_codes, v_codes, true, k_scales, v_scales, n_pages, block_table, max_pages, seqlens, B, Hq, Hkv, D,
+                                          page_size, softmax_scale, out, out_dt, lse, workspace, a))
+    return s;
+  if (thrift_status s = workspace_ok(paged_decode8_workspace(B, Hq, Hkv, max_pages, page_size, D), workspace, workspace_bytes)) return s;
+  if (thrift_status s = check_arch()) return s;
+  launch_paged_decode8(a, (hipStream_t)stream);
+  return after_launch();
+}
+
+static thrift_status paged_prefix_impl(PagedPrefixArgs& a, int bits, const int32_t* group_of, const int32_t* group_lens, int n_groups,
+                                       size_t workspace_bytes, void* stream) {
+  const PagedDecodeArgs& d = a.d;
+  if (!group_of || !group_lens) return THRIFT_ERR_NULL;
+  if (!prefix_ok(d.B, n_groups)) return THRIFT_ERR_SHAPE;
+  if (thrift_status s = workspace_ok(paged_prefix_workspace(bits, d.B, d.Hq, d.Hkv, n_groups, d.max_pages, d.page_size, d.D), d.workspace, workspace_bytes))
+    return s;
+  if (thrift_status s = check_arch()) return s;
+  a.group_of = group_of; a.group_lens = group_lens; a.n_groups = n_groups;
+  launch_paged_prefix(a, bits, (hipStream_t)stream);
+  return after_launch();
+}
+
+thrift_status thrift_paged_decode_prefix(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,
+                                         const int32_t* block_table, int max_pages, const int32_t* seqlens, const int32_t* group_of,
+                                         const int32_t* group_lens, int n_groups, int B, int Hq, int Hkv, int D, int page_size,
+                                         float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+  PagedPrefixArgs a;
+  if (thrift_status s = paged_decode_args(q, dt, k_pages, v_pages, false, nullptr, nullptr, n_pages, block_table, max_pages, seqlens, B, Hq, Hkv, D,
+                                          page_size, softmax_scale, out, out_dt, lse, workspace, a.d))
+    return s;
+  return paged_prefix_impl(a, 16, group_of, group_lens, n_groups, workspace_bytes, stream);
+}
+
+thrift_status thrift_paged_decode_prefix8(const void* q, thrift_dtype dt, const uint8_t* k_codes, const uint8_t* k_scales,
+                                          const uint8_t* v_codes, const uint8_t* v_scales, int n_pages, const int32_t* block_table, int max_pages,
+                                          const int32_t* seqlens, const int32_t* group_of, const int32_t* group_lens, int n_groups, int B,
+                                          int Hq, int Hkv, int D, int page_size, float softmax_scale, void* out, thrift_dtype out_dt, float* lse,
+                                          void* workspace, size_t workspace_bytes, void* stream) {
+  PagedPrefixArgs a;
+  if (thrift_status s = paged_decode_args(q, dt, k_codes, v_codes, true, k_scales, v_scales, n_pages, block_table, max_pages, seqlens, B, Hq, Hkv, D,
+                                          page_size, softmax_scale, out, out_dt, lse, workspace, a.d))
+    return s;
+  return paged_prefix_impl(a, 8, group_of, group_lens, n_groups, workspace_bytes, stream);
 }
 
 thrift_status thrift_peak_probe(int kind, thrift_dtype dt, int iters, void* buffer, size_t bytes, double* work, void* stream) {

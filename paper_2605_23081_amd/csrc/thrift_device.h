@@ -26,6 +26,7 @@ constexpr int kBk = 64;   // key-block size supported by this version
 
 // ---- 16-bit element traits: the same kernels serve fp16 and bf16 inputs ----
 struct F16 {
+  static constexpr uint16_t kLargest = 0x7bff;      // 65504
   typedef _Float16 scalar;
   typedef v8h vec8;
   static __device__ __forceinline__ float to_float(uint16_t u) {
@@ -47,6 +48,7 @@ struct F16 {
 };
 
 struct BF16 {
+  static constexpr uint16_t kLargest = 0x7f7f;
   typedef __bf16 scalar;
   typedef v8bf vec8;
   static __device__ __forceinline__ float to_float(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }

@@ -1,4 +1,4 @@
-// Host-side launch interface of rotary positions and of the paged 16-bit cache.
+// Host-side launch interface of rotary positions and of the paged cache in 16 and 8 bits.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -68,10 +68,29 @@ struct PagedAppendArgs {
 };
 void launch_paged_append(const PagedAppendArgs& a, thrift_dtype dt, hipStream_t st);
 
+struct PagedAppend8Args {
+  PagedAppendArgs in;         // but for its pages
+  uint8_t *k_codes, *k_scales, *v_codes, *v_scales;   // [n_pages,Hkv,page_size,D] and [n_pages,Hkv,page_size]
+};
+void launch_paged_append8(const PagedAppend8Args& a, thrift_dtype dt, hipStream_t st);
+
+struct PagedReadArgs {
+  const void *k_pages, *v_pages;                  // 16-bit elements, or codes
+  const uint8_t *k_scales, *v_scales;             // nullptr: 16-bit pages
+  const int32_t* table;       // [B,max_pages]
+  const int32_t* first;       // nullable [B]
+  const int32_t* seqlens;     // [B]
+  uint16_t *k_out, *v_out;    // [B,Hkv,N,D]
+  int B, Hkv, N, D, n_pages, max_pages, page_size;
+};
+void launch_paged_read(const PagedReadArgs& a, thrift_dtype dt, hipStream_t st);   // dt: of what 8-bit pages become
+
 struct PagedDecodeArgs {
   const uint16_t* q;          // [B,Hq,D]
-  const uint16_t* k_pages;    // [n_pages,Hkv,page_size,D]
-  const uint16_t* v_pages;
+  const void* k_pages;        // [n_pages,Hkv,page_size,D] 16-bit elements, or codes
+  const void* v_pages;
+  const uint8_t* k_scales;    // [n_pages,Hkv,page_size] of codes
+  const uint8_t* v_scales;
   const int32_t* table;       // [B,max_pages]
   const int32_t* seqlens;     // [B]
   void* out;                  // [B,Hq,D]
@@ -83,5 +102,16 @@ struct PagedDecodeArgs {
 };
 size_t paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D);   // 0: none is needed
 void launch_paged_decode(const PagedDecodeArgs& a, hipStream_t st);
+size_t paged_decode8_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D);
+void launch_paged_decode8(const PagedDecodeArgs& a, hipStream_t st);
+
+struct PagedPrefixArgs {
+  PagedDecodeArgs d;
+  const int32_t* group_of;    // [B]
+  const int32_t* group_lens;  // [n_groups]
+  int n_groups;
+};
+size_t paged_prefix_workspace(int bits, int B, int Hq, int Hkv, int n_groups, int max_pages, int page_size, int D);
+void launch_paged_prefix(const PagedPrefixArgs& a, int bits, hipStream_t st);
 
 }  // namespace thrift

@@ -133,8 +133,8 @@ struct Walk {
       const int key = s.t * kStep + 16 * sub, rows = __builtin_amdgcn_readfirstlane(there ? min(16, max(0, s.len - key)) : 0);
       const int p = __builtin_amdgcn_readfirstlane(min(a.n_pages - 1, max(0, page[sub])));
       const size_t at = ((((size_t)p * a.Hkv + s.hk) << z.shift) + (key & ((1 << z.shift) - 1))) * D;
-      kd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_pages + at), 0, rows * D * 2, 0x00020000);
-      vd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_pages + at), 0, rows * D * 2, 0x00020000);
+      kd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint16_t*)a.k_pages + at), 0, rows * D * 2, 0x00020000);
+      vd[sub] = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint16_t*)a.v_pages + at), 0, rows * D * 2, 0x00020000);
     }
   }
   __device__ __forceinline__ void load_q(const PagedDecodeArgs& a, const Launch& z, const Step& s, bool there) {

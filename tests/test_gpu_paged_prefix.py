@@ -1,0 +1,267 @@
+"""Attention over common starts of sequences on the GPU against 64 bits, in 16 and 8 bits: any grouping, lengths and sizes."""
+import math
+
+import pytest
+import torch
+
+from tests.paged8_util import cache8, prefix64, values64
+from tests.paged_util import check_rounded
+from tests.test_gpu_paged import DTYPES, I32, _ints, _randn
+
+pytestmark = pytest.mark.gpu
+U8 = torch.uint8
+
+
+@pytest.fixture(scope="module")
+def T():
+    from paper_2605_23081_amd import binding
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    binding.lib()
+    return binding
+
+
+class Batch:
+    """Sequences of groups: `of` [B], group_lens in tokens (as given to the call), lens [B].  Pages behind the lengths hold NaN."""
+
+    def __init__(self, of, group_lens, lens, Hkv, D, page, width, dtype, bits, seed=0):
+        self.of, self.group_lens, self.lens, self.bits, self.dtype = of, group_lens, lens, bits, dtype
+        g = torch.Generator().manual_seed(seed)
+        B = len(of)
+        # whole pages that members share, whatever the call says of lengths below or above that
+        whole = [max(0, min(n, width * page)) // page for n in group_lens]
+        self.shared = [whole[o] * page if 0 <= o < len(group_lens) and n >= whole[o] * page else 0 for o, n in zip(of, lens)]
+        n_pages = sum(whole) + B * width + 3
+        names = torch.randperm(n_pages, generator=g)
+        table = names[sum(whole):sum(whole) + B * width].view(B, width).clone()
+        starts = [sum(whole[:i]) for i in range(len(whole))]
+        live = torch.zeros(n_pages, page, dtype=torch.bool)
+        for b, n in enumerate(lens):
+            n = min(max(n, 0), width * page)
+            if self.shared[b]:
+                o = of[b]
+                table[b, :whole[o]] = names[starts[o]:starts[o] + whole[o]]
+            for j in range(-(-n // page)):
+                live[table[b, j], :min(page, n - j * page)] = True
+            table[b, -(-n // page):] = torch.tensor([-1, 2 ** 31 - 1, -2 ** 31, n_pages], dtype=torch.long)[torch.arange(width - -(-n // page)) % 4]
+        self.table = table.to(I32).cuda()
+        dead = ~live.cuda()
+        kp, vp = (_randn(n_pages, Hkv, page, D, dtype=dtype, seed=seed + i) for i in (0, 1))
+        if bits == 16:
+            for p in (kp, vp):
+                p.transpose(1, 2)[dead] = float("nan")
+            self.pages, self.values = (kp, vp), (kp, vp)
+        else:
+            kp.mul_((0.3 * _randn(*kp.shape[:3], 1, dtype=dtype, seed=seed + 5)).exp())
+            vp.mul_((2 * _randn(*vp.shape[:3], 1, dtype=dtype, seed=seed + 6)).exp())
+            self.pages = cache8(kp, vp)
+            for p in self.pages:
+                p.transpose(1, 2)[dead] = 0x7f if p.dim() == 4 else 255
+            self.values = values64(*self.pages[:2]), values64(*self.pages[2:])
+
+    def call(self, T, q, **kw):
+        f = T.thrift_paged_decode_prefix if self.bits == 16 else T.thrift_paged_decode_prefix8
+        return f(q, *self.pages, self.table, _ints(self.lens), _ints(self.of), _ints(self.group_lens), **kw)
+
+    def check(self, T, q, scale=0.0):
+        B, Hq, D = q.shape
+        clamped = [min(max(n, 0), self.table.shape[1] * self.values[0].shape[2]) for n in self.lens]
+        real = scale if scale > 0 else 1 / math.sqrt(D)
+        want, lse, eo, el = prefix64(q, *self.values, self.table, clamped, self.shared, real, self.dtype if self.bits == 16 else torch.bfloat16)
+        for dt in (torch.float32, q.dtype):
+            got, glse = self.call(T, q, softmax_scale=scale, out_dtype=dt, return_lse=True)
+            check_rounded(got, want, eo)
+            finite = torch.isfinite(lse)
+            assert torch.equal(finite, torch.isfinite(glse)) and bool((glse[~finite] == -math.inf).all())
+            assert bool(((glse.double() - lse)[finite].abs() <= el[finite]).all())
+        return got
+
+
+def _mixed(page):
+    """Three groups of different sizes anywhere in the batch, sequences of none, empty ones, members without tokens of their own, members
+    shorter than their group's start."""
+    of = [0, 1, -1, 0, 2, 1, 0, 7, 0, 1, -2 ** 31, 0, 2, 0, 1, 2 ** 31 - 1, 0]
+    group_lens = [5 * page + 3, 9 * page, 2 * page]
+    own = [1, 20, 77, 0, 5, 3 * page, page, 0, 2 * page + 1, 1, 9, -5 * page - 2, 33, 17, 0, 40, 64]
+    start = [group_lens[o] // page * page if 0 <= o < 3 else 0 for o in of]
+    return of, group_lens, [s + n for s, n in zip(start, own)]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("Hq,Hkv", [(4, 4), (8, 2), (32, 4), (7, 1), (32, 1), (40, 2), (17, 1)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [16, 8])
+def test_against_64_bits(T, D, Hq, Hkv, dtype, bits):
+    for page in (16, 64, 256):
+        print(f"prefix D={D} Hq={Hq} Hkv={Hkv} page={page} bits={bits} {dtype}", flush=True)
+        of, group_lens, lens = _mixed(page)
+        b = Batch(of, group_lens, lens, Hkv, D, page, 13, dtype, bits, seed=page)
+        b.check(T, _randn(len(of), Hq, D, dtype=dtype, seed=9))
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,prefix,own", [(2, 32, 8, 5000, 100), (130, 8, 2, 1000, 40), (64, 16, 16, 512, 200), (33, 8, 1, 20000, 10), (300, 4, 1, 640, 70), (7, 64, 8, 3000, 1),
+                                                 (1000, 2, 2, 64, 20)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [16, 8])
+def test_one_group(T, B, Hq, Hkv, prefix, own, dtype, bits):
+    print(f"prefix one group B={B} Hq={Hq} Hkv={Hkv} prefix={prefix} own={own} bits={bits} {dtype}", flush=True)
+    page = 32
+    g = torch.Generator().manual_seed(B)
+    start = prefix // page * page
+    lens = [start + n for n in torch.randint(0, own + 1, (B,), generator=g).tolist()]
+    b = Batch([0] * B, [prefix], lens, Hkv, 128, page, -(-(start + own) // page), dtype, bits, seed=B)
+    b.check(T, _randn(B, Hq, 128, dtype=dtype, seed=9))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_many_groups(T, bits):
+    """Pairs, groups of one, and groups that nobody is in, at the largest numbers of both."""
+    B, page, D = 4096, 16, 64
+    of = [(b * 2048 + b // 2) % 4096 if b % 3 else b % 50 for b in range(B)]
+    group_lens = [16 * (1 + o % 5) for o in range(4096)]
+    lens = [group_lens[o] + (b * 7) % 30 for b, o in enumerate(of)]
+    b = Batch(of, group_lens, lens, 1, D, page, 8, torch.float16, bits, seed=1)
+    b.check(T, _randn(B, 2, D, dtype=torch.float16, seed=9))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("gain", [0.01, 30.0])
+def test_flat_and_peaked_scores(T, bits, dtype, gain):
+    page, D = 32, 128
+    lens = [640, 700, 641, 650, 900]
+    b = Batch([0, 0, 0, 0, 0], [640], lens, 2, D, page, 30, dtype, bits, seed=6)
+    q = (_randn(5, 8, D, dtype=torch.float32, seed=7) * gain).to(dtype)
+    b.check(T, q)
+    b.check(T, q, scale=0.3)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("where", ["start", "own"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_ramps(T, bits, where, sign):
+    """Scores that fall or rise along the tokens by far more than exp can hold: all weight in the common tokens, or in a sequence's own."""
+    page, D, start = 16, 64, 400
+    lens = [start + n for n in (0, 1, 50, 100)]
+    b = Batch([0] * 4, [start], lens, 2, D, page, 40, torch.bfloat16, bits, seed=3)
+    if bits == 16:
+        k = b.pages[0]
+    else:
+        k = torch.zeros(b.values[0].shape, dtype=torch.bfloat16, device="cuda")
+    for i, n in enumerate(lens):
+        for j in range(-(-n // page)):
+            if where == "own" and j * page < start:
+                ramp = torch.zeros(page, device="cuda")
+            else:
+                ramp = sign * (torch.arange(page, device="cuda") + j * page) / 8.0
+            live = (torch.arange(page, device="cuda") + j * page < n).view(1, page, 1)
+            name = int(b.table[i, j])
+            k[name] = torch.where(live, (ramp.view(1, page, 1) / 8.0).expand(2, page, D).to(torch.bfloat16), k[name])
+    if bits == 16:
+        b.values = (k, b.values[1])
+    else:
+        codes = cache8(k, k)[:2]
+        dead = b.pages[1] == 255
+        codes[0][dead], codes[1][dead] = 0x7f, 255
+        b.pages = (*codes, *b.pages[2:])
+        b.values = (values64(*codes), b.values[1])
+    b.check(T, _randn(4, 8, D, dtype=torch.bfloat16, seed=7).abs())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_groups_that_share_nothing(T, bits):
+    """Lengths of groups below a page, of 0 and below: the result of the attention without groups, to the last bit of its sums' order."""
+    page, D = 64, 128
+    for group_lens in ([63, 0], [-1, -2 ** 31]):
+        b = Batch([0, 1, 0, 1, 1], group_lens, [100, 0, 64, 63, 500], 2, D, page, 9, torch.float16, bits, seed=2)
+        b.check(T, _randn(5, 8, D, dtype=torch.float16, seed=7))
+    # and a group whose start is longer than the table is wide: everything there is
+    b = Batch([0, 0, 0], [2 ** 31 - 1], [9 * page, 9 * page, 100], 2, D, page, 9, torch.float16, bits, seed=2)
+    b.check(T, _randn(3, 8, D, dtype=torch.float16, seed=7))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_one_sequence_and_none(T, bits):
+    page, D = 16, 128
+    for lens in ([50], [0], [16], [1]):
+        Batch([0], [16], lens, 2, D, page, 9, torch.float16, bits, seed=2).check(T, _randn(1, 8, D, dtype=torch.float16, seed=7))
+    b = Batch([0, 0, -1], [16], [0, 0, 0], 2, D, page, 9, torch.float16, bits, seed=2)
+    assert not bool(b.check(T, _randn(3, 8, D, dtype=torch.float16, seed=7)).any())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_bad_table_entries_are_not_followed(T, bits):
+    page, D = 16, 128
+    b = Batch([0, 0, 0], [64], [64, 90, 70], 2, D, page, 9, torch.float16, bits, seed=2)
+    pages = [torch.zeros_like(p) if p.dim() == 4 else torch.full_like(p, 127) if p.dtype == U8 else p for p in b.pages]
+    b.pages = tuple(pages)
+    n = pages[0].shape[0]
+    b.table[:, 1], b.table[1, 5], b.table[2, 4], b.table[0, 0] = n, -9, 2 ** 31 - 1, -2 ** 31
+    assert bool(torch.isfinite(b.call(T, _randn(3, 8, D, dtype=torch.float16, seed=9))).all())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_streams_workspaces_and_replays(T, bits):
+    """Calls at the same time on two streams; captured calls that share one workspace, replayed between eager ones with other lengths and groups."""
+    page, D, width = 16, 128, 100
+    b = Batch([0, 0, 0, 1, 1], [640, 320], [1600] * 5, 2, D, page, width, torch.float16, bits, seed=4)
+    q = _randn(5, 8, D, dtype=torch.float16, seed=12)
+    lens, of, group_lens = _ints(b.lens), _ints(b.of), _ints(b.group_lens)
+    f = T.thrift_paged_decode_prefix if bits == 16 else T.thrift_paged_decode_prefix8
+    one = lambda **kw: f(q, *b.pages, b.table, lens, of, group_lens, **kw)
+    want = one()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    results = []
+    torch.cuda.synchronize()
+    for s in streams:
+        with torch.cuda.stream(s):
+            results.append([one() for _ in range(20)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(r, want) for rs in results for r in rs)
+    shared = torch.full((T.paged_decode_prefix_workspace_bytes(bits, 5, 8, 2, 2, width, page, D),), 255, dtype=U8, device="cuda")
+    graphs, outs = [], []
+    for _ in range(2):
+        out = torch.empty(5, 8, D, dtype=torch.float16, device="cuda")
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            one(out=out, workspace=shared)
+        graphs.append(g), outs.append(out)
+    for i, (ln, o, gl) in enumerate((([1600] * 5, [0, 0, 0, 1, 1], [640, 320]), ([700, 640, 641, 0, 1600], [0, 0, 0, -1, -1], [640, 0]), ([0] * 5, [0] * 5, [640, 320]),
+                                     ([5, 900, 33, 320, 330], [1, 0, 0, 1, 1], [16, 320]), ([1599, 1600, 1, 900, 320], [-1] * 5, [640, 320]))):
+        lens.copy_(_ints(ln)), of.copy_(_ints(o)), group_lens.copy_(_ints(gl))
+        want = one()
+        torch.cuda.synchronize()
+        for g, out in zip(graphs, outs):
+            out.fill_(3)
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, want) for x in outs), i
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_server_whose_requests_share_a_prompt(T, bits):
+    """A prompt in whole pages that one sequence holds, requests that start with its pages and go on by themselves: every step's attention is that
+    of the cache without groups."""
+    B, Hq, Hkv, D, page, dtype = 6, 8, 2, 128, 16, torch.bfloat16
+    table = T.PageTable(B, 40, page, 200, "cuda")
+    cache = (T.PagedKVCache if bits == 16 else T.PagedKVCache8)(table, Hkv, D, dtype)
+    freqs, gain = T.rope_frequencies(D, 1e4, device="cuda")
+
+    def step(new, seed):
+        rows = sum(new)
+        x = _randn(rows, Hq + 2 * Hkv, D, dtype=dtype, seed=seed)
+        m = table.map(_ints(new), rows)
+        q = cache.append(x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], m, x[:, :Hq], freqs, "half", gain)
+        return q[(m.starts[1:].long() - 1).clamp(min=0)]
+
+    start = 20 * page
+    step([start, 0, 0, 0, 0, 0], 0)
+    table.block_table[1:5, :20] = table.block_table[0, :20]
+    table.seqlens = torch.where(torch.arange(B, device="cuda") < 5, start, 0).to(I32)
+    of, group_lens = _ints([0] * 5 + [-1]), _ints([start])
+    for i, new in enumerate(([0, 30, 5, 17, 1, 50], [1] * 6, [1, 1, 1, 0, 1, 1], [1] * 6)):
+        q = step(new, 1 + i)
+        got, lse = cache.decode_prefix(q, of, group_lens, out_dtype=torch.float32, return_lse=True)
+        want, wl = cache.decode(q, out_dtype=torch.float32, return_lse=True)
+        # probabilities of common tokens rounded once, half a step of bf16 of values of at most 6
+        assert float((got - want).abs().max()) <= 2.0 ** -8 * 6 and float((lse - wl).abs().max()) <= 2e-5
+        assert not torch.equal(got, torch.zeros_like(got))
