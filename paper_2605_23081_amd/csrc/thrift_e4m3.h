@@ -1,6 +1,8 @@
 // Heads in 8 bits: E4M3 codes with a power of two for each head of a token.
 #pragma once
 
+#include <type_traits>
+
 #include "thrift_device.h"
 
 namespace thrift {
@@ -27,6 +29,18 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 template <bool SEL>
 __device__ __forceinline__ uint32_t e4m3_pair(uint32_t old, float x, float y, float inv) {
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x * inv, y * inv, (int)old, SEL);
+}
+
+// The scale in byte i of a register
+__device__ __forceinline__ float scale_in(uint32_t bytes, int i) {
+  return __uint_as_float((i == 0 ? bytes << 23 : i == 1 ? bytes << 15 : i == 2 ? bytes << 7 : bytes >> 1) & 0x7f800000u);
+}
+
+// Codes 2 SEL and 2 SEL + 1 of a register as 16-bit numbers, exactly
+template <typename T, bool SEL>
+__device__ __forceinline__ uint32_t widen8(uint32_t codes) {
+  if constexpr (std::is_same_v<T, F16>) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.f, SEL));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, SEL));
 }
 
 // Codes 2 SEL and 2 SEL + 1 of a register, times a scale

@@ -71,17 +71,11 @@ void launch(const PagedDecodeArgs& a, hipStream_t st) {
 
 }  // namespace
 
-size_t paged_decode8_workspace(int B, int Hq, int Hkv, int max_pages, int page_size, int D) { return 0; }
-
-void launch_paged_decode8(const PagedDecodeArgs& a, hipStream_t st) {
-  if (a.dt == THRIFT_F16) launch<F16, true>(a, st);
-  else launch<BF16, true>(a, st);
-}
-
 size_t paged_prefix_workspace(int bits, int B, int Hq, int Hkv, int n_groups, int max_pages, int page_size, int D) { return 256; }
 
 void launch_paged_prefix(const PagedPrefixArgs& a, int bits, hipStream_t st) {
-  if (bits == 8) launch_paged_decode8(a.d, st);
+  if (bits == 8 && a.d.dt == THRIFT_F16) launch<F16, true>(a.d, st);
+  else if (bits == 8) launch<BF16, true>(a.d, st);
   else if (a.d.dt == THRIFT_F16) launch<F16, false>(a.d, st);
   else launch<BF16, false>(a.d, st);
 }
