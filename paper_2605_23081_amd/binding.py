@@ -121,7 +121,7 @@ class _General:
     def decode(*_):
         return None
 
-    append = attention = rope = page_map = paged_append = paged_decode = decode
+    append = attention = rope = page_map = paged_append = paged_decode = paged_append8 = paged_decode8 = paged_decode_prefix = paged_decode_prefix8 = decode
 
 
 def _native():
@@ -705,6 +705,9 @@ def thrift_paged_append8(k, v, slots, k_codes, k_scales, v_codes, v_scales, q: O
                          freqs: Optional[torch.Tensor] = None, layout: str = "half", gain: float = 1.0) -> Optional[torch.Tensor]:
     """thrift_paged_append into the 8-bit cache: codes [n_pages,Hkv,page_size,D] and scales [n_pages,Hkv,page_size], bytes."""
     pages = (k_codes, k_scales, v_codes, v_scales)
+    r = (_call or _native()).paged_append8(k, v, slots, *pages, q, q_out, positions, freqs, ROPE_LAYOUTS[layout], gain, *_here_now())
+    if r is not None:
+        return None if r is True else _result(r, "thrift_paged_append8")
     _pages8(*pages)
     assert k.dtype in (torch.float16, torch.bfloat16), k.dtype
     return _paged_append("thrift_paged_append8", k, v, slots, pages, k.dtype, q, q_out, positions, freqs, layout, gain)
@@ -800,6 +803,11 @@ def thrift_paged_decode8(q, k_codes, k_scales, v_codes, v_scales, block_table, s
                          out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None, lse: Optional[torch.Tensor] = None,
                          return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
     """thrift_paged_decode over the 8-bit cache."""
+    if out is not None or out_dtype is None:
+        r = (_call or _native()).paged_decode8(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, softmax_scale, out, lse, int(bool(return_lse)), workspace,
+                                                     *_here_now())
+        if r is not None:
+            return _result(r, "thrift_paged_decode8")
     _pages8(k_codes, k_scales, v_codes, v_scales)
     return _paged_decode("thrift_paged_decode8", q, (k_codes, k_scales, v_codes, v_scales), block_table, seqlens, (),
                          paged_decode8_workspace_bytes, softmax_scale, out, out_dtype, lse, return_lse, workspace)
@@ -810,6 +818,11 @@ def thrift_paged_decode_prefix(q, k_pages, v_pages, block_table, seqlens, group_
                                lse: Optional[torch.Tensor] = None, return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
     """thrift_paged_decode where the sequences of group g (group_of [B] == g) have the same pages for their first group_lens [n_groups] [g]
     tokens, which are read once for all of them."""
+    if out is not None or out_dtype is None:
+        r = (_call or _native()).paged_decode_prefix(q, k_pages, v_pages, block_table, seqlens, group_of, group_lens, softmax_scale, out, lse, int(bool(return_lse)), workspace,
+                                                           *_here_now())
+        if r is not None:
+            return _result(r, "thrift_paged_decode_prefix")
     _pages(k_pages, v_pages)
     assert q.dtype == k_pages.dtype, (q.dtype, k_pages.dtype)
     need = lambda B, Hq, Hkv, *sizes: paged_decode_prefix_workspace_bytes(16, B, Hq, Hkv, group_lens.numel(), *sizes)
@@ -821,6 +834,11 @@ def thrift_paged_decode_prefix8(q, k_codes, k_scales, v_codes, v_scales, block_t
                                 softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
                                 lse: Optional[torch.Tensor] = None, return_lse: bool = False, workspace: Optional[torch.Tensor] = None):
     """thrift_paged_decode_prefix over the 8-bit cache."""
+    if out is not None or out_dtype is None:
+        r = (_call or _native()).paged_decode_prefix8(q, k_codes, k_scales, v_codes, v_scales, block_table, seqlens, group_of, group_lens, softmax_scale, out, lse, int(bool(return_lse)), workspace,
+                                                            *_here_now())
+        if r is not None:
+            return _result(r, "thrift_paged_decode_prefix8")
     _pages8(k_codes, k_scales, v_codes, v_scales)
     need = lambda B, Hq, Hkv, *sizes: paged_decode_prefix_workspace_bytes(8, B, Hq, Hkv, group_lens.numel(), *sizes)
     return _paged_decode("thrift_paged_decode_prefix8", q, (k_codes, k_scales, v_codes, v_scales), block_table, seqlens, (group_of, group_lens),

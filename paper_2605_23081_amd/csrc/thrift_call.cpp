@@ -308,21 +308,37 @@ bool pages(PyObject* ko, PyObject* vo, int device, const Tensor** k, const Tenso
   return true;
 }
 
+// codes and scales of an 8-bit cache: k, k scales, v, v scales
+bool pages8(PyObject* const* a, int device, const Tensor* (&p)[4]) {
+  for (int i = 0; i < 4; ++i)
+    if (!plain(a[i], device, &p[i]) || p[i]->scalar_type() != at::kByte) return false;
+  if (p[0]->dim() != 4 || p[2]->sizes() != p[0]->sizes() || p[1]->sizes() != p[0]->sizes().slice(0, 3) || p[3]->sizes() != p[1]->sizes()) return false;
+  for (const int64_t x : p[0]->sizes()) if (x < 1 || x > 0x7fffffff) return false;
+  return true;
+}
+
 // paged_append(k, v, slots, k_pages, v_pages, q, q_out, positions, freqs, layout, gain, device, stream): q_out, or True without q
+// paged_append8: the same with k_codes, k_scales, v_codes, v_scales for the pages
+template <bool CODES>
 PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  const Tensor *k, *v, *slots, *kp, *vp, *q = nullptr, *qo, *positions, *freqs;
+  constexpr int kPages = CODES ? 4 : 2;
+  const Tensor *k, *v, *slots, *p[4] = {}, *q = nullptr, *qo, *positions, *freqs;
   int layout, device;
   double gain;
   void* stream;
   thrift_dtype dt;
-  if (n != 13 || !integer(a[11], &device) || !heads(a[0], device, &k) || !heads(a[1], device, &v) || !plain(a[2], device, &slots) ||
-      !pages(a[3], a[4], device, &kp, &vp, &dt) || (a[5] != Py_None && !heads(a[5], device, &q)) || !plain_or_none(a[6], device, &qo) ||
-      !plain_or_none(a[7], device, &positions) || !plain_or_none(a[8], device, &freqs) || !integer(a[9], &layout) || !real(a[10], &gain) ||
-      !stream_of(a[12], &stream) || k->dim() != 3 || (qo && !q))
+  if (n != 11 + kPages) Py_RETURN_NONE;
+  PyObject* const* b = a + 3 + kPages;     // behind the pages
+  if (!integer(b[6], &device) || !heads(a[0], device, &k) || !heads(a[1], device, &v) || !plain(a[2], device, &slots) ||
+      !(CODES ? pages8(a + 3, device, p) && dtype16(*k, &dt) : pages(a[3], a[4], device, &p[0], &p[1], &dt)) ||
+      (b[0] != Py_None && !heads(b[0], device, &q)) || !plain_or_none(b[1], device, &qo) ||
+      !plain_or_none(b[2], device, &positions) || !plain_or_none(b[3], device, &freqs) || !integer(b[4], &layout) || !real(b[5], &gain) ||
+      !stream_of(b[7], &stream) || k->dim() != 3 || (qo && !q))
     Py_RETURN_NONE;
-  const int64_t T = k->size(0), Hkv = kp->size(1), D = kp->size(3);
-  if (!like(*k, *kp, {T, Hkv, D}) || !like(*v, *kp, {T, Hkv, D}) || !is(*slots, at::kInt, {T}) ||
-      (q && (q->dim() != 3 || !like(*q, *kp, {T, q->size(1), D}))) || (qo && !like(*qo, *q, q->sizes())))
+  const Tensor& of = CODES ? *k : *p[0];   // whose type keys, values and queries have
+  const int64_t T = k->size(0), Hkv = p[0]->size(1), D = p[0]->size(3);
+  if (!like(*k, of, {T, Hkv, D}) || !like(*v, of, {T, Hkv, D}) || !is(*slots, at::kInt, {T}) ||
+      (q && (q->dim() != 3 || !like(*q, of, {T, q->size(1), D}))) || (qo && !like(*qo, *q, q->sizes())))
     Py_RETURN_NONE;
   if (freqs && (freqs->scalar_type() != at::kDouble || freqs->dim() != 1 || freqs->numel() < 1 || freqs->numel() > 0x3fffffff || !positions ||
                 !is(*positions, at::kInt, {T})))
@@ -335,10 +351,15 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   thrift_status r;
   {
     const Unlocked unlocked;
-    r = thrift_paged_append(ptr(q), st[0], q ? q_out.data_ptr() : nullptr, q ? (int)q->size(1) : 0, ptr(k), st[1], ptr(v), st[2], (int)Hkv,
-                                                dt, (int)T, ptr_as<int32_t>(slots), ptr_as<int32_t>(positions), ptr_as<double>(freqs),
-                                                freqs ? 2 * (int)freqs->numel() : 0, layout, (float)gain, ptr(kp), ptr(vp), (int)kp->size(0),
-                                                (int)kp->size(2), (int)D, stream);
+    const int Hq = q ? (int)q->size(1) : 0, rot = freqs ? 2 * (int)freqs->numel() : 0, n_pages = (int)p[0]->size(0), page = (int)p[0]->size(2);
+    void* to = q ? q_out.data_ptr() : nullptr;
+    if constexpr (CODES)
+      r = thrift_paged_append8(ptr(q), st[0], to, Hq, ptr(k), st[1], ptr(v), st[2], (int)Hkv, dt, (int)T, ptr_as<int32_t>(slots),
+                               ptr_as<int32_t>(positions), ptr_as<double>(freqs), rot, layout, (float)gain, ptr_as<uint8_t>(p[0]), ptr_as<uint8_t>(p[1]),
+                               ptr_as<uint8_t>(p[2]), ptr_as<uint8_t>(p[3]), n_pages, page, (int)D, stream);
+    else
+      r = thrift_paged_append(ptr(q), st[0], to, Hq, ptr(k), st[1], ptr(v), st[2], (int)Hkv, dt, (int)T, ptr_as<int32_t>(slots),
+                              ptr_as<int32_t>(positions), ptr_as<double>(freqs), rot, layout, (float)gain, ptr(p[0]), ptr(p[1]), n_pages, page, (int)D, stream);
   }
   if (r != THRIFT_OK) return PyLong_FromLong((long)r);
   if (!q) Py_RETURN_TRUE;
@@ -346,33 +367,56 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // paged_decode(q, k_pages, v_pages, block_table, seqlens, scale, out, lse, return_lse, workspace, device, stream): out, or (out, lse)
+// CODES: k_codes, k_scales, v_codes, v_scales for the pages; PREFIX: group_of and group_lens behind the lengths
+template <bool CODES, bool PREFIX>
 PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  const Tensor *q, *kp, *vp, *table, *lens, *out_given, *lse_given, *ws_given;
+  constexpr int kPages = CODES ? 4 : 2, kGroups = PREFIX ? 2 : 0;
+  const Tensor *q, *p[4] = {}, *table, *lens, *of = nullptr, *group_lens = nullptr, *out_given, *lse_given, *ws_given;
   int return_lse, device;
   double scale;
   void* stream;
   thrift_dtype dt, odt;
-  if (n != 12 || !integer(a[10], &device) || !plain(a[0], device, &q) || !pages(a[1], a[2], device, &kp, &vp, &dt) || !plain(a[3], device, &table) ||
-      !plain(a[4], device, &lens) || !real(a[5], &scale) || !plain_or_none(a[6], device, &out_given) || !plain_or_none(a[7], device, &lse_given) ||
-      !integer(a[8], &return_lse) || !plain_or_none(a[9], device, &ws_given) || !stream_of(a[11], &stream) || q->dim() != 3 || table->dim() != 2)
+  if (n != 10 + kPages + kGroups) Py_RETURN_NONE;
+  PyObject* const* b = a + 1 + kPages;     // behind the pages
+  PyObject* const* c = b + 2 + kGroups;    // behind the groups
+  if (!integer(c[5], &device) || !plain(a[0], device, &q) ||
+      !(CODES ? pages8(a + 1, device, p) && dtype16(*q, &dt) : pages(a[1], a[2], device, &p[0], &p[1], &dt)) || !plain(b[0], device, &table) ||
+      !plain(b[1], device, &lens) || (PREFIX && (!plain(b[2], device, &of) || !plain(b[3], device, &group_lens))) || !real(c[0], &scale) ||
+      !plain_or_none(c[1], device, &out_given) || !plain_or_none(c[2], device, &lse_given) || !integer(c[3], &return_lse) ||
+      !plain_or_none(c[4], device, &ws_given) || !stream_of(c[6], &stream) || q->dim() != 3 || table->dim() != 2)
     Py_RETURN_NONE;
   const int64_t B = q->size(0), Hq = q->size(1), D = q->size(2), width = table->size(1);
-  if (B > 0x7fffffff || Hq > 0x7fffffff || width > 0x7fffffff || !like(*q, *kp, {B, Hq, kp->size(3)}) || !is(*table, at::kInt, {B, width}) ||
+  if (B > 0x7fffffff || Hq > 0x7fffffff || width > 0x7fffffff || !like(*q, CODES ? *q : *p[0], {B, Hq, p[0]->size(3)}) || !is(*table, at::kInt, {B, width}) ||
       !is(*lens, at::kInt, {B}) || (out_given && out_given->sizes() != q->sizes()) || (lse_given && !is(*lse_given, at::kFloat, {B, Hq})) ||
       (ws_given && ws_given->scalar_type() != at::kByte))
     Py_RETURN_NONE;
+  if (PREFIX && (!is(*of, at::kInt, {B}) || group_lens->scalar_type() != at::kInt || group_lens->dim() != 1 || group_lens->numel() > 0x7fffffff)) Py_RETURN_NONE;
   const Tensor out = out_given ? *out_given : at::empty({B, Hq, D}, q->options());
   if (!dtype_out(out, &odt)) Py_RETURN_NONE;
   const Tensor lse = lse_given ? *lse_given : return_lse ? at::empty({B, Hq}, q->options().dtype(at::kFloat)) : Tensor();
-  const int Hkv = (int)kp->size(1), page = (int)kp->size(2);
-  const size_t need = ws_given ? 0 : thrift_paged_decode_workspace((int)B, (int)Hq, Hkv, (int)width, page, (int)D);
+  const int Hkv = (int)p[0]->size(1), page = (int)p[0]->size(2), n_pages = (int)p[0]->size(0), groups = PREFIX ? (int)group_lens->numel() : 0;
+  const size_t need = ws_given ? 0
+                      : PREFIX ? thrift_paged_decode_prefix_workspace(CODES ? 8 : 16, (int)B, (int)Hq, Hkv, groups, (int)width, page, (int)D)
+                               : (CODES ? thrift_paged_decode8_workspace : thrift_paged_decode_workspace)((int)B, (int)Hq, Hkv, (int)width, page, (int)D);
   const Tensor ws = ws_given ? *ws_given : need > 0 ? bytes_like(*q, need) : Tensor();
   thrift_status r;
   {
     const Unlocked unlocked;
-    r = thrift_paged_decode(ptr(q), dt, ptr(kp), ptr(vp), (int)kp->size(0), ptr_as<int32_t>(table), (int)width, ptr_as<int32_t>(lens),
-                                                (int)B, (int)Hq, Hkv, (int)D, page, (float)scale, out.data_ptr(), odt,
-                                                lse.defined() ? lse.data_ptr<float>() : nullptr, ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? (size_t)ws.numel() : 0, stream);
+    const int32_t *t = ptr_as<int32_t>(table), *l = ptr_as<int32_t>(lens), *g = ptr_as<int32_t>(of), *gl = ptr_as<int32_t>(group_lens);
+    const uint8_t *kc = ptr_as<uint8_t>(p[0]), *ks = ptr_as<uint8_t>(p[1]), *vc = ptr_as<uint8_t>(p[2]), *vs = ptr_as<uint8_t>(p[3]);
+    float* e = lse.defined() ? lse.data_ptr<float>() : nullptr;
+    void* w = ws.defined() ? ws.data_ptr() : nullptr;
+    const size_t bytes = ws.defined() ? (size_t)ws.numel() : 0;
+    const int nb = (int)B, hq = (int)Hq, m = (int)width, d = (int)D;
+    const float s = (float)scale;
+    if constexpr (CODES && PREFIX)
+      r = thrift_paged_decode_prefix8(ptr(q), dt, kc, ks, vc, vs, n_pages, t, m, l, g, gl, groups, nb, hq, Hkv, d, page, s, out.data_ptr(), odt, e, w, bytes, stream);
+    else if constexpr (CODES)
+      r = thrift_paged_decode8(ptr(q), dt, kc, ks, vc, vs, n_pages, t, m, l, nb, hq, Hkv, d, page, s, out.data_ptr(), odt, e, w, bytes, stream);
+    else if constexpr (PREFIX)
+      r = thrift_paged_decode_prefix(ptr(q), dt, ptr(p[0]), ptr(p[1]), n_pages, t, m, l, g, gl, groups, nb, hq, Hkv, d, page, s, out.data_ptr(), odt, e, w, bytes, stream);
+    else
+      r = thrift_paged_decode(ptr(q), dt, ptr(p[0]), ptr(p[1]), n_pages, t, m, l, nb, hq, Hkv, d, page, s, out.data_ptr(), odt, e, w, bytes, stream);
   }
   if (r != THRIFT_OK || !return_lse) return answer(r, out);
   PyObject* both = PyTuple_New(2);
@@ -399,8 +443,12 @@ PyMethodDef methods[] = {
     {"attention", (PyCFunction)(void (*)(void))guarded<attention>, METH_FASTCALL, nullptr},
     {"rope", (PyCFunction)(void (*)(void))guarded<rope>, METH_FASTCALL, nullptr},
     {"page_map", (PyCFunction)(void (*)(void))guarded<page_map>, METH_FASTCALL, nullptr},
-    {"paged_append", (PyCFunction)(void (*)(void))guarded<paged_append>, METH_FASTCALL, nullptr},
-    {"paged_decode", (PyCFunction)(void (*)(void))guarded<paged_decode>, METH_FASTCALL, nullptr},
+    {"paged_append", (PyCFunction)(void (*)(void))guarded<paged_append<false>>, METH_FASTCALL, nullptr},
+    {"paged_append8", (PyCFunction)(void (*)(void))guarded<paged_append<true>>, METH_FASTCALL, nullptr},
+    {"paged_decode", (PyCFunction)(void (*)(void))guarded<paged_decode<false, false>>, METH_FASTCALL, nullptr},
+    {"paged_decode8", (PyCFunction)(void (*)(void))guarded<paged_decode<true, false>>, METH_FASTCALL, nullptr},
+    {"paged_decode_prefix", (PyCFunction)(void (*)(void))guarded<paged_decode<false, true>>, METH_FASTCALL, nullptr},
+    {"paged_decode_prefix8", (PyCFunction)(void (*)(void))guarded<paged_decode<true, true>>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
