@@ -147,7 +147,7 @@ def _read64(pages, table, lens, first, N):
     return torch.where(there.view(B, 1, N, *[1] * (rows.dim() - 3)), rows, 0)
 
 
-@pytest.mark.parametrize("D", [128, 2, 6, 64, 72, 256, 1024])
+@pytest.mark.parametrize("D", [128, 2, 6, 8, 64, 72, 256, 1000, 1024])
 @pytest.mark.parametrize("N", [1, 7, 64, 301])
 @pytest.mark.parametrize("page", [16, 128])
 def test_read_is_a_copy(T, D, N, page):
@@ -412,3 +412,25 @@ def test_the_general_path_gives_the_same_results(T, monkeypatch):
     monkeypatch.setattr(T, "_call", T._General)
     for i, (a, b) in enumerate(zip(results(), want)):
         assert torch.equal(a, b), i
+
+
+def test_the_module_leaves_other_arguments_to_the_general_path(T):
+    m = T._native()
+    k, slots, table, lens = torch.zeros(3, 2, 128, dtype=torch.float16, device="cuda"), _ints([0, 1, 2]), _ints([[0], [1], [2]]), _ints([1, 1, 1])
+    p = _pages8(4, 2, 16, 128, 0)
+    one = lambda **kw: m.paged_append8(*{**dict(k=k, v=k, slots=slots, a=p[0], b=p[1], c=p[2], d=p[3], q=None, qo=None, pos=None, freqs=None, layout=0, gain=1.0, device=0, stream=0), **kw}.values())
+    assert one() is True
+    for bad in (dict(device=1), dict(k=k.float()), dict(v=k.bfloat16()), dict(k=k[:2]), dict(slots=slots.long()), dict(a=p[1]), dict(b=p[0]), dict(c=p[2][:, :1]), dict(d=p[3].float()),
+                dict(a=p[0].cpu()), dict(qo=k), dict(q=k[:2]), dict(freqs=torch.zeros(64, dtype=torch.float64, device="cuda")), dict(layout="half")):
+        assert one(**bad) is None, bad
+    assert one(pos=slots, freqs=torch.zeros(65, dtype=torch.float64, device="cuda")) == 2
+    for f, pages in ((m.paged_decode8, p), (m.paged_decode_prefix8, p), (m.paged_decode_prefix, [k.new_zeros(4, 2, 16, 128)] * 2)):
+        groups = dict(of=slots, gl=lens) if f is not m.paged_decode8 else {}
+        one = lambda **kw: f(*{**dict(q=k, **{f"p{i}": x for i, x in enumerate(pages)}, table=table, lens=lens, **groups, scale=0.0, out=None, lse=None, rl=0, ws=None, device=0, stream=0), **kw}.values())
+        assert one().shape == (3, 2, 128)
+        for bad in (dict(device=1), dict(q=k.float()), dict(table=table[:2]), dict(lens=lens.long()), dict(p0=pages[0][:, :1]), dict(p1=pages[0].cpu()), dict(out=k[:2]), dict(lse=k),
+                    dict(ws=k), *([dict(of=slots[:2]), dict(gl=lens.long()), dict(gl=table), dict(of=None)] if groups else [])):
+            assert one(**bad) is None, bad
+        wide = torch.zeros(3, 100, dtype=I32, device="cuda")
+        assert one(table=wide, ws=torch.empty(16, dtype=U8, device="cuda")) == 5
+    assert all(f() is None for f in (m.paged_append8, m.paged_decode8, m.paged_decode_prefix, m.paged_decode_prefix8))
