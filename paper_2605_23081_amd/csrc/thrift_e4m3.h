@@ -43,6 +43,23 @@ __device__ __forceinline__ uint32_t widen8(uint32_t codes) {
   else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, SEL));
 }
 
+// Eight codes times a scale as 16-bit numbers
+template <typename T>
+__device__ __forceinline__ v4i widen_chunk(v2i codes, float scale) {
+  v4i y;
+#pragma unroll
+  for (int d = 0; d < 2; ++d) {
+    if constexpr (std::is_same_v<T, F16>) {
+      y[2 * d] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)codes[d], scale, false));
+      y[2 * d + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)codes[d], scale, true));
+    } else {
+      y[2 * d] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[d], scale, false));
+      y[2 * d + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[d], scale, true));
+    }
+  }
+  return y;
+}
+
 // Codes 2 SEL and 2 SEL + 1 of a register, times a scale
 template <bool SEL>
 __device__ __forceinline__ float2 e4m3_values(uint32_t codes, float scale) {

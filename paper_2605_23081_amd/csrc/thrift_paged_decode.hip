@@ -17,9 +17,15 @@ bool by_rows(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {
 
 template <typename T, int D, bool C8>
 void launch(const PagedDecodeArgs& a, hipStream_t st) {
-  const Launch z = launch_of(a, C8, a.workspace, nullptr);
-  if (by_rows(a.B, a.Hq, a.Hkv, a.max_pages, a.page_size, a.D)) launch_rows<T, D, C8, false>(a, z, st);
-  else launch_shares<T, D, C8, false>(a, z, st);
+  const Launch z = launch_of(a, C8, a.workspace);
+  if (by_rows(a.B, a.Hq, a.Hkv, a.max_pages, a.page_size, a.D)) {
+    paged_decode_rows_kernel<T, D, C8><<<dim3((unsigned)((long)a.B * a.Hkv)), dim3(64 * kRowWaves), 0, st>>>(a, z);
+    return;
+  }
+  const dim3 grid(shares_of(C8)), block(64 * waves_of(D));
+  if (z.G <= 16) paged_decode_kernel<T, D, 1, C8, false><<<grid, block, 0, st>>>(a, z);
+  else paged_decode_kernel<T, D, 2, C8, false><<<grid, block, 0, st>>>(a, z);
+  paged_merge_kernel<D, shares_of(C8)><<<dim3(shares_of(C8) * z.G), dim3(kThreads), 0, st>>>(a, z);
 }
 template <typename T, bool C8>
 void launch(const PagedDecodeArgs& a, hipStream_t st) {

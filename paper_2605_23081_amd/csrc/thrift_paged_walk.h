@@ -86,9 +86,25 @@ struct Space {
   float* part_ml;            // [2*shares][G][2]
 };
 
+// Groups of sequences that start with the same pages
+struct Groups {
+  const int32_t* of;         // [B]
+  const int32_t* lens;       // [n]
+  int n;
+};
+// Tokens in front of sequence b, of length len, that it has in common with its group: whole pages, 0 for none
+__device__ __forceinline__ int common_tokens(const Groups& g, int capacity, int shift, int b, int len) {
+  const int of = g.of[b];
+  if ((unsigned)of >= (unsigned)g.n) return 0;
+  const int n = min(capacity, max(0, g.lens[of])) >> shift << shift;
+  return len >= n ? n : 0;
+}
+
 struct Launch {
   Space w;
-  const int32_t* skip;       // [B] pages in front that are passed over: seqlens and what is read begin behind them (SKIP)
+  Groups groups;             // SKIP only: the tokens that sequences of a group have in common are passed over,
+  float *own_o, *own_ml;     // a row's part that holds its first step goes here, [B*Hq][D] and [B*Hq][2], instead of to `out` or a slot,
+  int2* own_span;            // [B*Hkv] and here the first share with more of the row, and how many there are; slots: [shares][G]
   int G, shift;
   float c;                   // softmax scale * log2(e)
 };
@@ -96,6 +112,7 @@ struct Launch {
 // a step: which keys of which row
 struct Step {
   int b, hk, t, len, steps;                // sequence, KV head, number in the row; the sequence's length and steps
+  int skip;                                // pages in front that the row does not have
 };
 
 __device__ __forceinline__ int length_of(const PagedDecodeArgs& a, const Launch& z, int n) { return min(a.max_pages << z.shift, max(0, n)); }
@@ -138,9 +155,8 @@ struct Walk {
 
   __device__ __forceinline__ void look_up(const PagedDecodeArgs& a, const Launch& z, const Step& s) {
     const scalar_ints table = scalar(a.table + (size_t)s.b * a.max_pages);
-    const int skip = SKIP ? scalar(z.skip)[s.b] : 0;
 #pragma unroll
-    for (int sub = 0; sub < 2; ++sub) page[sub] = table[min(a.max_pages - 1, skip + ((s.t * kStep + 16 * sub) >> z.shift))];
+    for (int sub = 0; sub < 2; ++sub) page[sub] = table[min(a.max_pages - 1, (SKIP ? s.skip : 0) + ((s.t * kStep + 16 * sub) >> z.shift))];
   }
   __device__ __forceinline__ void describe(const PagedDecodeArgs& a, const Launch& z, const Step& s, bool there) {
 #pragma unroll
@@ -341,6 +357,25 @@ struct Walk {
         for (int r = 0; r < 4; ++r) o[nb][j][r] = o[nb][j][r] * k1 + p[4 * j + r][lane] * k2;
     }
   }
+  // The state as a part of a row: with its first step, or a later one, which is this share's first
+  __device__ __forceinline__ void put_part(const Launch& z, const PagedDecodeArgs& a, const Step& s, bool from_start) const {
+    const size_t first = from_start ? ((size_t)s.b * a.Hkv + s.hk) * z.G : (size_t)blockIdx.x * z.G;
+    float *to_o = from_start ? z.own_o : z.w.part_o, *to_ml = from_start ? z.own_ml : z.w.part_ml;
+    constexpr float kUnscale = 1.f / Mma<P>::kScale;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int head = col + 16 * nb;
+      const float sum = over_groups_sum(l[nb]);
+      if (head >= z.G) continue;
+      const size_t to = first + head;
+      if (grp == 0) to_ml[2 * to] = m[nb], to_ml[2 * to + 1] = sum;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < VC; j += 4)
+          *reinterpret_cast<v4f*>(to_o + to * D + channel(r, j)) = v4f{o[nb][j][r], o[nb][j + 1][r], o[nb][j + 2][r], o[nb][j + 3][r]} * kUnscale;
+    }
+  }
   // The state as the row's result, or as a part of it in `slot`
   __device__ __forceinline__ void put(const PagedDecodeArgs& a, const Launch& z, const Step& s, bool whole, size_t slot) const {
     const size_t row = (size_t)s.b * a.Hkv + s.hk;
@@ -380,8 +415,15 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
 
   // ---- this workgroup's share, steps u .. u_end - 1, and the first one's place ----
-  int u = 0, u_end = 0, each = 0, window = 0, lens;         // lens: length of sequence window + lane
+  int u = 0, u_end = 0, each = 0, window = 0, lens, skips = 0;    // lens, skips: of sequence window + lane
   Step cur;
+  auto length = [&](int b) {               // and its skips
+    const int n = length_of(a, z, a.seqlens[b]);
+    if constexpr (!SKIP) return n;
+    const int common = common_tokens(z.groups, a.max_pages << z.shift, z.shift, b, n);
+    skips = common >> z.shift;
+    return n - common;
+  };
   {
     int n = a.B, per, base = 0, b = 0;
     bool first = true;
@@ -390,7 +432,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
       int sum = 0;
       for (int i = 0; i < per; ++i) {
         const int at = lane * per + i;
-        lens = b + at < a.B ? length_of(a, z, a.seqlens[b + at]) : 0;     // the last round's reach past its part: the sequences that follow
+        lens = b + at < a.B ? length(b + at) : 0;                         // the last round's reach past its part: the sequences that follow
         if (at < n) sum += a.Hkv * steps_of(lens);
       }
       int incl = sum;
@@ -402,7 +444,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
       if (first) {
         const int total = __builtin_amdgcn_readlane(incl, 63);
         const int quarter = max(1, (total + kShares * kWaves - 1) / (kShares * kWaves));
-        if (threadIdx.x == 0) z.w.tail[blockIdx.x] = make_int2(-1, 0);
+        if (!SKIP && threadIdx.x == 0) z.w.tail[blockIdx.x] = make_int2(-1, 0);
         const long begin = (long)blockIdx.x * kWaves * quarter;
         if (begin >= total) return;        // the whole workgroup
         u = (int)begin, u_end = min(total, u + quarter * kWaves);
@@ -420,6 +462,7 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
     window = __builtin_amdgcn_readfirstlane(window), base = __builtin_amdgcn_readfirstlane(base);
     cur.b = __builtin_amdgcn_readfirstlane(b);
     cur.len = __builtin_amdgcn_readlane(lens, cur.b - window);
+    cur.skip = SKIP ? __builtin_amdgcn_readlane(skips, cur.b - window) : 0;
     cur.steps = steps_of(cur.len);
     cur.hk = __builtin_amdgcn_readfirstlane((u - base) / cur.steps);
     cur.t = (u - base) - cur.hk * cur.steps;
@@ -434,10 +477,11 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
       if (later != 0) {
         const int at = __builtin_ctzll(later);
         s.b = window + at, s.len = __builtin_amdgcn_readlane(lens, at);
+        if (SKIP) s.skip = __builtin_amdgcn_readlane(skips, at);
         break;
       }
       window += 64, s.b = window - 1;
-      lens = window + lane < a.B ? length_of(a, z, a.seqlens[window + lane]) : 0;
+      lens = window + lane < a.B ? length(window + lane) : 0;
     }
     s.steps = steps_of(s.len);
   };
@@ -497,7 +541,12 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
         w.give(parts[wave]);
         if (ends && lane == 0) ended[wave] = 1;
       } else if (ends && !one_row) {
-        w.put(a, z, cur, begin == 0, 2 * (size_t)blockIdx.x);
+        if constexpr (SKIP) {
+          w.put_part(z, a, cur, begin == 0);
+          if (begin == 0 && lane == 0) z.own_span[(size_t)cur.b * a.Hkv + cur.hk] = make_int2(0, 0);
+        } else {
+          w.put(a, z, cur, begin == 0, 2 * (size_t)blockIdx.x);
+        }
       } else {
         kept = true;
       }
@@ -518,12 +567,15 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
     w.take(parts[i]);
     ends |= ended[i] > 0;
   }
-  w.put(a, z, cur, begin == 0 && ends, 2 * (size_t)blockIdx.x + (begin == 0 ? 1 : 0));
+  if constexpr (SKIP) w.put_part(z, a, cur, begin == 0);
+  else w.put(a, z, cur, begin == 0 && ends, 2 * (size_t)blockIdx.x + (begin == 0 ? 1 : 0));
   // the state began with the row's first step, at each * kWaves * (shares so far) + what this share has of other rows; the rest of the
   // row's steps fill the shares behind
-  if (begin == 0 && !ends && lane == 0) {
+  if (begin == 0 && (SKIP || !ends) && lane == 0) {
     const int share = each * kWaves, here = min(share - (first_u - (int)blockIdx.x * share), cur.steps);
-    z.w.tail[blockIdx.x] = make_int2(cur.b * a.Hkv + cur.hk, 1 + (cur.steps - here + share - 1) / share);
+    const int more = (cur.steps - here + share - 1) / share;
+    if (SKIP) z.own_span[(size_t)cur.b * a.Hkv + cur.hk] = make_int2((int)blockIdx.x + 1, more);
+    else z.w.tail[blockIdx.x] = make_int2(cur.b * a.Hkv + cur.hk, 1 + more);
   }
 }
 
@@ -531,9 +583,9 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
 // join afterwards.  Wavefronts take every fourth step (eight instead of four gained nothing); at the end each joins some channels of all
 // of them.
 constexpr int kRowWaves = 4;
-template <typename T, int D, bool C8, bool SKIP>
+template <typename T, int D, bool C8>
 __global__ void __launch_bounds__(64 * kRowWaves, 1) paged_decode_rows_kernel(PagedDecodeArgs a, Launch z) {
-  using Rows = Walk<T, D, 1, C8, SKIP>;
+  using Rows = Walk<T, D, 1, C8, false>;
   constexpr int W = kRowWaves;
   constexpr int VC = Rows::VC;
   __shared__ float parts[W][Rows::NR][64];
@@ -675,28 +727,14 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedDecodeArgs a
   if (a.lse != nullptr && tid == 0) a.lse[at] = kLn2 * (top + __builtin_log2f(sum));
 }
 
-template <typename T, int D, bool C8, bool SKIP>
-void launch_rows(const PagedDecodeArgs& a, const Launch& z, hipStream_t st) {
-  paged_decode_rows_kernel<T, D, C8, SKIP><<<dim3((unsigned)((long)a.B * a.Hkv)), dim3(64 * kRowWaves), 0, st>>>(a, z);
-}
-// The shares of all rows, and their join
-template <typename T, int D, bool C8, bool SKIP>
-void launch_shares(const PagedDecodeArgs& a, const Launch& z, hipStream_t st) {
-  const dim3 grid(shares_of(C8)), block(64 * waves_of(D));
-  if (z.G <= 16) paged_decode_kernel<T, D, 1, C8, SKIP><<<grid, block, 0, st>>>(a, z);
-  else paged_decode_kernel<T, D, 2, C8, SKIP><<<grid, block, 0, st>>>(a, z);
-  paged_merge_kernel<D, shares_of(C8)><<<dim3(shares_of(C8) * z.G), dim3(kThreads), 0, st>>>(a, z);
-}
-
 inline size_t space_bytes(bool codes, int G, int D) {
   return shares_of(codes) * sizeof(int2) + 2 * (size_t)shares_of(codes) * G * (D + 2) * sizeof(float);
 }
-inline Launch launch_of(const PagedDecodeArgs& a, bool codes, void* workspace, const int32_t* skip) {
-  Launch z;
+inline Launch launch_of(const PagedDecodeArgs& a, bool codes, void* workspace) {
+  Launch z = {};
   z.G = a.Hq / a.Hkv;
   z.shift = __builtin_ctz(a.page_size);
   z.c = a.scale * 1.4426950408889634f;
-  z.skip = skip;
   char* w = (char*)workspace;
   z.w.tail = (int2*)w;
   z.w.part_o = (float*)(w + shares_of(codes) * sizeof(int2));
