@@ -8,9 +8,8 @@
 // tiles and walks blocks of 64 keys:
 //   S = K Q^T      64 keys x 32 rows;  r: a reference of the row, P = 2^(S c - r) <= 2^15
 //   O^T += V^T P^T channels x 32 rows; a lane's part of S is its operand P, without passing through LDS or other lanes
-// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come through registers, two blocks ahead, from loads whose
-// descriptors end at the common tokens.  With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
-//   8-bit pages are converted on their way to LDS, once for all wavefronts: values and, for bf16 queries, keys times their scales, which bf16
+// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come by LDS DMA, three blocks ahead.  With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
+//   8-bit pages come through registers, two blocks ahead, and are converted on their way to LDS, once for all wavefronts: values and, for bf16 queries, keys times their scales, which bf16
 // holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
 //   P is rounded to 16 bits once, unlike in the walk of own tokens: two pieces would be half as many matrix instructions again, which
 // bound this kernel for large groups.  Sums are those of the unrounded P.
@@ -21,6 +20,7 @@
 // price.  The part of a tile that has its first block is written to the rows' places, any other is the first of its share and is
 // written to the share's slot.
 #include "thrift_paged_walk.h"
+#include "thrift_tile.h"
 
 namespace thrift {
 
@@ -43,8 +43,12 @@ struct PrefixLaunch {
   Launch own;
 };
 
-// Workgroup barrier that orders LDS traffic only, and leaves loads in flight
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// Two numbers rounded to 16 bits, the first in the lower half
+template <typename T>
+__device__ __forceinline__ uint32_t pack16(float x, float y) {
+  if constexpr (std::is_same_v<T, F16>) return __builtin_bit_cast(uint32_t, v2h{(_Float16)x, (_Float16)y});
+  else return __builtin_bit_cast(uint32_t, v2bf{(__bf16)x, (__bf16)y});
+}
 
 template <typename T> struct Reference;                // how far below the largest score the reference lies, and how far one may pass it
 template <> struct Reference<F16> { static constexpr float kBelow = 7.f, kMost = 15.f; };
@@ -59,13 +63,14 @@ struct Tiles {
   static constexpr int kWaves = prefix_waves(D), kThreads = 64 * kWaves, kTile = tile_rows(D);
   static constexpr int kRow = 2 * D;                                        // bytes of a row in LDS
   static constexpr int kSide = kBlock * kRow, kSlot = 2 * kSide;
+  static constexpr int kRing = C8 || D == 256 ? 2 : 4;                      // blocks in LDS
   static constexpr int kChunks = kBlock * D / 8 / kThreads;                 // 16-byte chunks of K, and of V, of a thread
   static constexpr int kRowsOf = 512 / D;                                   // rows of a wavefront's chunk
   static_assert(kChunks * kWaves * kRowsOf == kBlock, "");
 
   struct Shared {
-    char stage[2][kSlot];
-    float scales[kScaled ? 2 : 1][kScaled ? kBlock : 1];
+    char stage[kRing][kSlot];
+    float scales[kScaled ? kRing : 1][kScaled ? kBlock : 1];
     float ml[kWaves / 2][2][64];
     int count[kMaxGroups];                             // members of every group
     uint16_t group[kMaxSeqs];                          // of every sequence; 0xffff: none
@@ -76,12 +81,14 @@ struct Tiles {
     int start_group;
   };
 
-  // A block on its way
+  // A block of codes on its way
   struct Block {
-    std::conditional_t<C8, v2i, v4i> k[kChunks], v[kChunks];
+    v2i k[kChunks], v[kChunks];
     uint32_t ks[kChunks], vs[kChunks];
   };
 };
+
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
 // One tile's rows in a wavefront: 32 of them
 template <typename T, int D, bool C8, int PARTS>
@@ -90,6 +97,8 @@ struct Rows {
   using P = typename L::P;
   static constexpr int NT = 2 / PARTS;                 // 32-key halves of a block
   v8s q[D / 16];
+  v16f s[NT];                                          // scores of a block,
+  v4i p[NT][2];                                        // and P
   v16f o[D / 32];
   float r, l;                                          // reference, this lane's part of the sum
   bool large;                                          // of the wavefront: some reference from 2^20 on
@@ -102,21 +111,45 @@ struct Rows {
     r = -__FLT_MAX__, l = 0.f, large = false;
   }
 
-  // A block in LDS, of which `valid` keys are there; part: which half, of PARTS
-  __device__ __forceinline__ void step(const char* slot, const float* scales, int part, int valid, float c) {
+  // The products with a block in LDS; part: which half of its keys, of PARTS.  Operands are asked for a phase ahead of the products that take them: fences
+  // keep the compiler from putting every read in front of its use.
+  __device__ __forceinline__ void scores(const char* slot, int part) {
     const int lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31;
-    v16f s[NT];
-    // chunk x of a K row lies at x ^ (row & 7): eight neighbouring rows at one chunk fill all banks
+    // Chunk x of a K row lies at x ^ (row & 7): eight neighbouring rows at one chunk fill all banks
     const char* k0 = slot + (32 * part + row) * L::kRow;
     const uint32_t swizzled = 16u * (half ^ (row & 7));
+    constexpr int kPiece = D / 16 < 8 ? D / 16 : 8, kPieces = NT * D / 16 / kPiece;       // K operands in flight, and of a block
+    v8s k[2][kPiece];
+    auto read_k = [&](int i) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+      for (int x = 0; x < kPiece; ++x) {
+        const int t = i * kPiece / (D / 16), e = i * kPiece % (D / 16) + x;
+        k[i & 1][x] = *reinterpret_cast<const v8s*>(k0 + 32 * t * L::kRow + ((swizzled ^ (32u * (e & 3))) + 128u * (e >> 2)));
+      }
+    };
+    read_k(0);
+    fence();
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+    for (int i = 0; i < kPieces; ++i) {
+      if (i + 1 < kPieces) {
+        read_k(i + 1);
+        fence();
+      }
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e)
-        s[t] = T::mfma(*reinterpret_cast<const v8s*>(k0 + 32 * t * L::kRow + ((swizzled ^ (32u * (e & 3))) + 128u * (e >> 2))), q[e], s[t]);
+      for (int x = 0; x < kPiece; ++x) {
+        const int t = i * kPiece / (D / 16), e = i * kPiece % (D / 16) + x;
+        if (e == 0) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
+        }
+        s[t] = T::mfma(k[i & 1][x], q[e], s[t]);
+      }
     }
+  }
+
+  // Scores to P, with the reference and the sum; `valid` keys of the block are there
+  __device__ __forceinline__ void soften(const float* scales, int part, int valid, float c) {
+    const int half = (threadIdx.x & 63) >> 5;
     // register i of half t: key 32 t + 8 (i / 4) + 4 half + i % 4
     if constexpr (L::kScaled) {
 #pragma unroll
@@ -163,32 +196,52 @@ struct Rows {
         }
       f = 1.f, off = 0.f;
     }
-    v8s p[NT][2];
+    float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = fast_exp2(__builtin_fmaf(s[t][i], f, -off));
-        l += x;
-        p[t][i >> 3][i & 7] = (short)P::from_float(x);
+      for (int i = 0; i < 16; i += 2) {
+        const float x = fast_exp2(__builtin_fmaf(s[t][i], f, -off)), y = fast_exp2(__builtin_fmaf(s[t][i + 1], f, -off));
+        sums[i & 2] += x, sums[(i & 2) + 1] += y;
+        p[t][i >> 3][(i & 7) >> 1] = (int)pack16<P>(x, y);
       }
-    // operand slots 8 half + e of step u of half t are keys 32 t + 16 u + 8 (e / 4) + 4 half + e % 4, as P's registers are.  A group of 16 lanes reads four
-    // keys x 16 channels and gets four keys of a channel per lane
+    l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  }
+
+  __device__ __forceinline__ void multiply(const char* slot, int part) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    // V operands: slots 8 half + e of step u of half t are keys 32 t + 16 u + 8 (e / 4) + 4 half + e % 4, as P's registers are.  A group of 16 lanes
+    // reads four keys x 16 channels and gets four keys of a channel per lane
     const int i16 = lane & 15, g = (lane >> 4) & 1, key = 4 * half + (i16 >> 2);
     typedef v4s __attribute__((address_space(3))) * lds_v4s_ptr;
     const char* v0 = slot + L::kSide + (32 * part + key) * L::kRow;
     const uint32_t at = (32u * g + 8u * (i16 & 3)) ^ v_swizzle(key);
+    constexpr int kWide = D / 32 < 4 ? D / 32 : 4, kSteps = 2 * NT * (D / 32) / kWide;     // channel tiles of a phase; phases
+    v4s v[2][kWide][2];
+    auto read_v = [&](int i) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+      for (int x = 0; x < kWide; ++x) {
+        const int tu = i * kWide / (D / 32), n = i * kWide % (D / 32) + x;
+        const char* from = v0 + 16 * tu * L::kRow + ((at ^ (64u * (n & 3))) + 256u * (n >> 2));
+        v[i & 1][x][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from));
+        v[i & 1][x][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from + 8 * L::kRow));
+      }
+    };
+    read_v(0);
+    fence();
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < kSteps; ++i) {
+      if (i + 1 < kSteps) {
+        read_v(i + 1);
+        fence();
+      }
 #pragma unroll
-        for (int n = 0; n < D / 32; ++n) {
-          const char* from = v0 + (32 * t + 16 * u) * L::kRow + ((at ^ (64u * (n & 3))) + 256u * (n >> 2));
-          const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from));
-          const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from + 8 * L::kRow));
-          o[n] = P::mfma(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7), p[t][u], o[n]);
-        }
+      for (int x = 0; x < kWide; ++x) {
+        const int tu = i * kWide / (D / 32), n = i * kWide % (D / 32) + x;
+        o[n] = P::mfma(__builtin_shufflevector(v[i & 1][x][0], v[i & 1][x][1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(v8s, p[tu >> 1][tu & 1]), o[n]);
+      }
+      fence();
+    }
   }
 
   // Bytes that a V row's offsets are swizzled by: four neighbouring rows at one 64-byte piece fill all banks
@@ -300,76 +353,109 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         const uint16_t* from = a.q + home * D + 8 * (lane >> 5);
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) w.q[e] = *reinterpret_cast<const v8s*>(from + 16 * e);
+        // they arrive here: a wait inside the walk would be one for the blocks on their way
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) asm volatile("" : "+v"(w.q[e]));
       }
       w.clear();
 
-      // blocks on their way: the rows that this wavefront brings
-      const scalar_ints table = scalar(a.table + (size_t)__builtin_amdgcn_readfirstlane(sh.list[0]) * a.max_pages);
+      // blocks on their way: the rows that this wavefront brings.  Common tokens are whole pages, so that all rows of a chunk are there or none;
+      // LDS gets other rows of the block for those (P is 0 there), or, from codes, zeros
       const int my_row = lane * 8 / D, my_chunk = lane % (D / 8);
       auto first_row = [&](int i) { return (i * kWaves + wave) * L::kRowsOf; };
-      int page[L::kChunks];
-      auto look_up = [&](int t) {
-#pragma unroll
-        for (int i = 0; i < L::kChunks; ++i) page[i] = table[min((unsigned)a.max_pages - 1, ((unsigned)t * kBlock + first_row(i)) >> shift)];   // t may lie past the end, and 31 bits
+      auto key_of = [&](int t, int i) {                // 31 bits are passed behind the end, where nothing is read
+        const unsigned key = (unsigned)t * kBlock + first_row(i);
+        return C8 || key < (unsigned)tokens ? key : (unsigned)t * kBlock + first_row(i) % 16;
       };
-      auto load = [&](typename L::Block& x, int t) {
+      // a lane has the page of one chunk of one block, from block page_t on: no scalar loads in the walk, whose results would be waited for with the
+      // reads of LDS
+      constexpr int kPages = 64 / L::kChunks;
+      const int32_t* table = a.table + (size_t)__builtin_amdgcn_readfirstlane(sh.list[0]) * a.max_pages;
+      int pages, page_t = t0 - kPages;
+      auto row_at = [&](int t, int i) {
+        if (t >= page_t + kPages) {
+          page_t = t;
+          const unsigned at = min((unsigned)a.max_pages - 1, key_of(t + lane / L::kChunks, lane % L::kChunks) >> shift);
+          pages = min(a.n_pages - 1, max(0, table[at]));
+        }
+        const int p = __builtin_amdgcn_readlane(pages, (t - page_t) * L::kChunks + i);
+        return (((size_t)p * a.Hkv + hk) << shift) + (key_of(t, i) & ((1u << shift) - 1));
+      };
+      constexpr int kRing = L::kRing;
+      auto step = [&](int t, int s) {
+        if (!busy) return;
+        w.scores(sh.stage[s], part);
+        w.soften(sh.scales[L::kScaled ? s : 0], part, tokens - t * kBlock, z.own.c);
+        w.multiply(sh.stage[s], part);
+      };
+      auto next_slot = [&](int s) { return s + 1 == kRing ? 0 : s + 1; };
+      if constexpr (C8) {
+        auto load = [&](typename L::Block& x, int t) {
 #pragma unroll
-        for (int i = 0; i < L::kChunks; ++i) {
-          const int key = t * kBlock + first_row(i);
-          const bool there = t < t1 && key < tokens;   // common tokens are whole pages, so all of these rows or none
-          const int p = __builtin_amdgcn_readfirstlane(min(a.n_pages - 1, max(0, page[i])));
-          const size_t at = (((size_t)p * a.Hkv + hk) << shift) + (key & ((1 << shift) - 1));
-          constexpr int kBytes = C8 ? 1 : 2;
-          const auto kd = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.k_pages + at * D * kBytes), 0, there ? L::kRowsOf * D * kBytes : 0, 0x00020000);
-          const auto vd = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.v_pages + at * D * kBytes), 0, there ? L::kRowsOf * D * kBytes : 0, 0x00020000);
-          if constexpr (C8) {
+          for (int i = 0; i < L::kChunks; ++i) {
+            const bool there = t < t1 && (int)key_of(t, i) < tokens;
+            const size_t at = row_at(t, i);
+            const auto kd = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.k_pages + at * D), 0, there ? L::kRowsOf * D : 0, 0x00020000);
+            const auto vd = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.v_pages + at * D), 0, there ? L::kRowsOf * D : 0, 0x00020000);
             const auto ksd = __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_scales + at), 0, there ? L::kRowsOf : 0, 0x00020000);
             const auto vsd = __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_scales + at), 0, there ? L::kRowsOf : 0, 0x00020000);
             x.k[i] = __builtin_amdgcn_raw_buffer_load_b64(kd, 8 * lane, 0, 0), x.v[i] = __builtin_amdgcn_raw_buffer_load_b64(vd, 8 * lane, 0, 0);
             x.ks[i] = __builtin_amdgcn_raw_buffer_load_b8(ksd, my_row, 0, 0), x.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(vsd, my_row, 0, 0);
-          } else {
-            x.k[i] = __builtin_amdgcn_raw_buffer_load_b128(kd, 16 * lane, 0, 0), x.v[i] = __builtin_amdgcn_raw_buffer_load_b128(vd, 16 * lane, 0, 0);
           }
-        }
-      };
-      auto write = [&](const typename L::Block& x, int s) {
+        };
+        auto write = [&](const typename L::Block& x, int s) {
 #pragma unroll
-        for (int i = 0; i < L::kChunks; ++i) {
-          const int r = first_row(i) + my_row;
-          char *k = sh.stage[s] + r * L::kRow + 16 * (my_chunk ^ (r & 7)), *v = sh.stage[s] + L::kSide + r * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r));
-          if constexpr (C8) {
+          for (int i = 0; i < L::kChunks; ++i) {
+            const int r = first_row(i) + my_row;
+            char *k = sh.stage[s] + r * L::kRow + 16 * (my_chunk ^ (r & 7)), *v = sh.stage[s] + L::kSide + r * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r));
             *reinterpret_cast<v4i*>(k) = widen_chunk<T>(x.k[i], L::kScaled ? 1.f : scale_of(x.ks[i]));
             *reinterpret_cast<v4i*>(v) = widen_chunk<BF16>(x.v[i], scale_of(x.vs[i]));
             if constexpr (L::kScaled)
               if (my_chunk == 0) sh.scales[s][r] = scale_of(x.ks[i]);
-          } else {
-            *reinterpret_cast<v4i*>(k) = x.k[i], *reinterpret_cast<v4i*>(v) = x.v[i];
           }
-        }
-      };
-      auto step = [&](int t, int s) {
-        if (busy) w.step(sh.stage[s], sh.scales[L::kScaled ? s : 0], part, tokens - t * kBlock, z.own.c);
-      };
-      typename L::Block x, y;
-      look_up(t0);
-      load(x, t0);
-      look_up(t0 + 1);
-      load(y, t0 + 1);
-      look_up(t0 + 2);
-      write(x, 0);
-      lds_barrier();
-      for (int t = t0; t < t1; t += 2) {
-        load(x, t + 2);
-        look_up(t + 3);
-        step(t, 0);
-        write(y, 1);
-        lds_barrier();
-        if (t + 1 == t1) break;
-        load(y, t + 3);
-        look_up(t + 4);
-        step(t + 1, 1);
+        };
+        typename L::Block x, y;
+        load(x, t0);
+        load(y, t0 + 1);
         write(x, 0);
         lds_barrier();
+        for (int t = t0; t < t1; t += 2) {
+          load(x, t + 2);
+          step(t, 0);
+          write(y, 1);
+          lds_barrier();
+          if (t + 1 == t1) break;
+          load(y, t + 3);
+          step(t + 1, 1);
+          write(x, 0);
+          lds_barrier();
+        }
+      } else {
+        // LDS is written in the order of the lanes: a lane reads the chunk that belongs in its place
+        constexpr int kLoads = 2 * L::kChunks;
+        const int r0 = first_row(0) + my_row;          // first_row(i) is the same but for multiples of eight
+        const uint32_t k_off = my_row * L::kRow + 16 * (my_chunk ^ (r0 & 7)), v_off = my_row * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r0));
+        auto load = [&](int t, int s) {
+          if (t >= t1) return;
+#pragma unroll
+          for (int i = 0; i < L::kChunks; ++i) {
+            const size_t at = row_at(t, i) * L::kRow;
+            const uint32_t to = lds_address(sh.stage[s]) + first_row(i) * L::kRow;
+            dma_b128((const char*)a.k_pages + at, k_off, to);
+            dma_b128((const char*)a.v_pages + at, v_off, to + L::kSide);
+          }
+        };
+#pragma unroll
+        for (int i = 0; i < kRing - 1; ++i) load(t0 + i, i);
+        for (int t = t0, s = 0; t < t1; ++t, s = next_slot(s)) {
+          // block t is here: those behind it that are on their way may stay so
+          if (kRing > 3 && t + 2 < t1) vm_wait<2 * kLoads>();
+          else if (kRing > 2 && t + 1 < t1) vm_wait<kLoads>();
+          else vm_wait<0>();
+          lds_barrier();
+          load(t + kRing - 1, s == 0 ? kRing - 1 : s - 1);
+          step(t, s);
+        }
       }
 
       // ---- both halves of a row's keys, and its place ----
@@ -380,7 +466,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
       }
       if constexpr (PARTS == 2) {
-        lds_barrier();
+        lds_barrier();                                 // nobody reads the last block any more
         float(*mail)[64] = reinterpret_cast<float(*)[64]>(sh.stage) + (wave >> 1) * (D / 2);
         if (part == 1 && busy) {
 #pragma unroll
