@@ -545,18 +545,20 @@ thrift_status thrift_paged_read8(const uint8_t* k_codes, const uint8_t* k_scales
                                  const int32_t* block_table, int max_pages, const int32_t* first, const int32_t* seqlens, int B, int Hkv, int N,
                                  int D, int page_size, void* k_out, void* v_out, thrift_dtype dt, void* stream);
 
-/* Host: bytes of workspace thrift_paged_decode_prefix (bits 16) and thrift_paged_decode_prefix8 (bits 8) need; 0 for sizes that they refuse. */
+/* Host: bytes of workspace thrift_paged_decode_prefix (bits 16) and thrift_paged_decode_prefix8 (bits 8) need; 0: none (workspace may be NULL), and
+ * for sizes that they refuse. */
 size_t thrift_paged_decode_prefix_workspace(int bits, int B, int Hq, int Hkv, int n_groups, int max_pages, int page_size, int D);
 
 /*
  * Attention of one new token per sequence where sequences start with the same pages: thrift_paged_decode, with the keys and values of a common
  * start read once for all of its sequences.  The result is that of thrift_paged_decode but for the order of its fp32 sums, and for the
- * probabilities of the common tokens, which are rounded to 16 bits (dt's; bf16 over the 8-bit cache) for the product with the values.
+ * probabilities of the common tokens, which are rounded to 16 bits (dt's; bf16 over the 8-bit cache) for the product with the values.  Over the 8-bit cache,
+ * common values past bf16's largest number, 3.39e38, count as infinite, and so do common keys for bf16 queries.
  *   group_of [B] int32: the group of each sequence, any order; a number outside 0 .. n_groups - 1: none
  *   group_lens [n_groups] int32: tokens in front that the sequences of a group have in the same pages, rounded down to whole pages, at most
  *     max_pages * page_size.  They are read through the block table of one of them.  A sequence shorter than that, or of no group, is read
- *     by itself.
- *   1 <= n_groups <= 4096; B <= 4096; all other arguments, limits and results as thrift_paged_decode; a workspace is always needed
+ *     by itself, and so are all where little would be saved.
+ *   1 <= n_groups <= 4096; B <= 4096; all other arguments, limits and results as thrift_paged_decode
  */
 thrift_status thrift_paged_decode_prefix(const void* q, thrift_dtype dt, const void* k_pages, const void* v_pages, int n_pages,
                                          const int32_t* block_table, int max_pages, const int32_t* seqlens, const int32_t* group_of,

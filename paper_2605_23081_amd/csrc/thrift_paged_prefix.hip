@@ -16,9 +16,8 @@
 //   The reference is the row's largest score so far where that has grown by more than fp16 (or 8 binades, bf16) would hold, so that O is rarely
 // multiplied; for fp16 it lies 7 binades lower, which keeps P normal down to 2^-21 of the largest.  Scores from 2^20 on are rounded before r is
 // taken off, as in the walk: a fused difference would be off by binades.
-//   The blocks of all tiles are counted through on the GPU and cut into equal shares, one per workgroup and CU, a full tile's at twice the
-// price.  The part of a tile that has its first block is written to the rows' places, any other is the first of its share and is
-// written to the share's slot.
+//   Tiles are cut into parts of equal numbers of blocks on the GPU, so that there is one for every CU: a tile's first part is written to its rows' places, the
+// others to slots.
 #include "thrift_paged_walk.h"
 #include "thrift_tile.h"
 
@@ -28,18 +27,27 @@ namespace {
 
 constexpr int kBlock = 64;                             // keys
 constexpr int kPrefixShares = kCus;
+constexpr int kPriceFull = 3, kPriceHalf = 2;          // of a block for a tile of rows, and for half a one at most
 // Wavefronts of a workgroup.  256 channels: four, with all registers that two have otherwise.
 constexpr int prefix_waves(int D) { return D == 256 ? 4 : 8; }
 constexpr int tile_rows(int D) { return 32 * prefix_waves(D); }
 
 struct Prefix {
-  float *home_o, *home_ml;                             // [B*Hq][D], [B*Hq][2]: parts with a tile's first block
-  int4* home_span;                                     // [B*Hq]: first share with more of the row's tile, how many, the row in the tile
-  float *slot_o, *slot_ml;                             // [kPrefixShares][tile_rows][D], [..][2]
+  float *home_o, *home_ml;                             // [B*Hq][D], [B*Hq][2]: a tile's first part
+  int4* home_span;                                     // [B*Hq]: first slot with more of the row's tile, how many, the row in the tile
+  float *slot_o, *slot_ml;                             // [kPrefixShares][tile_rows][D], [..][2]: the other parts
 };
 
+// Groups of sequences that start with the same pages
+struct Groups {
+  const int32_t* of;         // [B]
+  const int32_t* lens;       // [n]
+  int n;
+};
 struct PrefixLaunch {
   Prefix p;
+  Groups groups;
+  int32_t* common;           // [B] tokens in front of every sequence that the first launch takes
   Launch own;
 };
 
@@ -55,6 +63,10 @@ template <> struct Reference<F16> { static constexpr float kBelow = 7.f, kMost =
 template <> struct Reference<BF16> { static constexpr float kBelow = 0.f, kMost = 8.f; };
 
 constexpr int kMaxSeqs = kMapMaxSeqs, kMaxGroups = kMapMaxSeqs;
+// A group whose common tokens, but for one member's, are fewer than this together is left alone: a part of a tile costs as much in front of and behind its walk as
+// reading about so many tokens
+constexpr int kLeastShared = 512;
+
 
 template <typename T, int D, bool C8>
 struct Tiles {
@@ -62,48 +74,60 @@ struct Tiles {
   static constexpr bool kScaled = C8 && std::is_same_v<T, F16>;             // keys lie in LDS without their scales
   static constexpr int kWaves = prefix_waves(D), kThreads = 64 * kWaves, kTile = tile_rows(D);
   static constexpr int kRow = 2 * D;                                        // bytes of a row in LDS
-  static constexpr int kSide = kBlock * kRow, kSlot = 2 * kSide;
-  static constexpr int kRing = C8 || D == 256 ? 2 : 4;                      // blocks in LDS
+  static constexpr int kSide = kBlock * kRow;                               // bytes of a block of K or V
+  static constexpr int kRing = C8 || D == 256 ? 2 : 4;                      // blocks of K, and of V, in LDS
   static constexpr int kChunks = kBlock * D / 8 / kThreads;                 // 16-byte chunks of K, and of V, of a thread
   static constexpr int kRowsOf = 512 / D;                                   // rows of a wavefront's chunk
   static_assert(kChunks * kWaves * kRowsOf == kBlock, "");
 
   struct Shared {
-    char stage[kRing][kSlot];
+    union {
+      struct {
+        char k[kRing][kSide], v[kRing][kSide];
+      };
+      char stage[8192 * kWaves];                       // of results
+    };
     float scales[kScaled ? kRing : 1][kScaled ? kBlock : 1];
     float ml[kWaves / 2][2][64];
     int count[kMaxGroups];                             // members of every group
     uint16_t group[kMaxSeqs];                          // of every sequence; 0xffff: none
     int list[kTile + 1];                               // members that have rows in the tile
-    long sums[kWaves];
+    uint3 sums[kWaves];
     int waves[kWaves];
-    long start_base;
+    uint32_t start_share, start_unit;
     int start_group;
   };
 
-  // A block of codes on its way
+  // K or V of a block of codes on its way
   struct Block {
-    v2i k[kChunks], v[kChunks];
-    uint32_t ks[kChunks], vs[kChunks];
+    v2i codes[kChunks];
+    uint32_t scales[kChunks];
   };
 };
 
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
-// One tile's rows in a wavefront: 32 of them
+// One tile's rows in a wavefront: 32 of them.
+//
+// A step has the scores of block t in `s`.  It forms P of block t between the products of the queries with the keys of block t + 1, and the largest of
+// those scores between the products of P with the values of block t: matrix and vector instructions take turns in one stream, held in place by
+// fences, and reads of LDS run some products ahead.  Without that the two kinds hardly overlapped, neither within a wavefront nor between the two of a SIMD.
 template <typename T, int D, bool C8, int PARTS>
 struct Rows {
   using L = Tiles<T, D, C8>;
   using P = typename L::P;
   static constexpr int NT = 2 / PARTS;                 // 32-key halves of a block
+  static constexpr int kKeys = NT * D / 16, kValues = 2 * NT * (D / 32);    // products with the keys and with the values of a block
+  static constexpr int kAhead = 4;                     // reads ahead of their products
+  typedef v16f Scores[NT];
   v8s q[D / 16];
-  v16f s[NT];                                          // scores of a block,
-  v4i p[NT][2];                                        // and P
   v16f o[D / 32];
-  float r, l;                                          // reference, this lane's part of the sum
+  float r, l, top;                                     // reference, this lane's part of the sum, largest score of the next block
   bool large;                                          // of the wavefront: some reference from 2^20 on
+  int part, half, row;                                 // which half of a block's keys, of PARTS; of the lane
 
-  __device__ __forceinline__ void clear() {
+  __device__ __forceinline__ void clear(int which) {
+    part = which, half = (threadIdx.x & 63) >> 5, row = threadIdx.x & 31;
 #pragma unroll
     for (int n = 0; n < D / 32; ++n)
 #pragma unroll
@@ -111,46 +135,38 @@ struct Rows {
     r = -__FLT_MAX__, l = 0.f, large = false;
   }
 
-  // The products with a block in LDS; part: which half of its keys, of PARTS.  Operands are asked for a phase ahead of the products that take them: fences
-  // keep the compiler from putting every read in front of its use.
-  __device__ __forceinline__ void scores(const char* slot, int part) {
-    const int lane = threadIdx.x & 63, half = lane >> 5, row = lane & 31;
-    // Chunk x of a K row lies at x ^ (row & 7): eight neighbouring rows at one chunk fill all banks
-    const char* k0 = slot + (32 * part + row) * L::kRow;
-    const uint32_t swizzled = 16u * (half ^ (row & 7));
-    constexpr int kPiece = D / 16 < 8 ? D / 16 : 8, kPieces = NT * D / 16 / kPiece;       // K operands in flight, and of a block
-    v8s k[2][kPiece];
-    auto read_k = [&](int i) {
-#pragma unroll
-      for (int x = 0; x < kPiece; ++x) {
-        const int t = i * kPiece / (D / 16), e = i * kPiece % (D / 16) + x;
-        k[i & 1][x] = *reinterpret_cast<const v8s*>(k0 + 32 * t * L::kRow + ((swizzled ^ (32u * (e & 3))) + 128u * (e >> 2)));
-      }
-    };
-    read_k(0);
-    fence();
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      if (i + 1 < kPieces) {
-        read_k(i + 1);
-        fence();
-      }
-#pragma unroll
-      for (int x = 0; x < kPiece; ++x) {
-        const int t = i * kPiece / (D / 16), e = i * kPiece % (D / 16) + x;
-        if (e == 0) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j) s[t][j] = 0.f;
-        }
-        s[t] = T::mfma(k[i & 1][x], q[e], s[t]);
-      }
+  // Operand i of the keys: half i / (D / 16) of the block.  Chunk x of a K row lies at x ^ (row & 7): eight neighbouring rows at one chunk fill all banks
+  struct KeyReader {
+    const char* from;
+    uint32_t swizzled;
+    __device__ __forceinline__ v8s operator()(int i) const {
+      const int t = i / (D / 16), e = i % (D / 16);
+      return *reinterpret_cast<const v8s*>(from + 32 * t * L::kRow + ((swizzled ^ (32u * (e & 3))) + 128u * (e >> 2)));
     }
+  };
+  __device__ __forceinline__ KeyReader keys_in(const char* k) const { return KeyReader{k + (32 * part + row) * L::kRow, 16u * (half ^ (row & 7))}; }
+  __device__ __forceinline__ void product(Scores& n, int i, v8s k) const {
+    if (i % (D / 16) == 0) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) n[i / (D / 16)][j] = 0.f;
+    }
+    n[i / (D / 16)] = T::mfma(k, q[i % (D / 16)], n[i / (D / 16)]);
   }
 
-  // Scores to P, with the reference and the sum; `valid` keys of the block are there
-  __device__ __forceinline__ void soften(const float* scales, int part, int valid, float c) {
-    const int half = (threadIdx.x & 63) >> 5;
-    // register i of half t: key 32 t + 8 (i / 4) + 4 half + i % 4
+  // The scores of a block, where nothing else is to be done
+  __device__ __forceinline__ void scores(Scores& n, const char* k, const float* scales, int valid, float c) {
+    const KeyReader key = keys_in(k);
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) product(n, i, key(i));
+    settle(n, scales, valid);
+    float x = n[0][0];
+#pragma unroll
+    for (int i = 1; i < 16 * NT; ++i) x = fmaxf(x, n[i >> 4][i & 15]);
+    top = both_halves_max(x) * c;
+  }
+
+  // Scales of the keys, where K lies in LDS without them; `valid` keys of the block are there.  Register i of half t: key 32 t + 8 (i / 4) + 4 half + i % 4
+  __device__ __forceinline__ void settle(Scores& n, const float* scales, int valid) const {
     if constexpr (L::kScaled) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
@@ -158,7 +174,7 @@ struct Rows {
         for (int i = 0; i < 16; i += 4) {
           const v4f f = *reinterpret_cast<const v4f*>(scales + 32 * (part + t) + 2 * i + 4 * half);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[t][i + e] *= f[e];
+          for (int e = 0; e < 4; ++e) n[t][i + e] *= f[e];
         }
     }
     if (valid < kBlock) {
@@ -166,14 +182,13 @@ struct Rows {
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (32 * (part + t) + 8 * (i >> 2) + 4 * half + (i & 3) >= valid) s[t][i] = -__builtin_inff();
+          if (32 * (part + t) + 8 * (i >> 2) + 4 * half + (i & 3) >= valid) n[t][i] = -__builtin_inff();
     }
-    float top = s[0][0];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-    top = both_halves_max(top) * c;
+  }
+
+  // k: K of block t + 1 (whatever LDS holds there behind the last one), with its scales and keys; v: V of block t; ask(): between the two series of products
+  template <typename F>
+  __device__ __forceinline__ void step(Scores& s, Scores& n, const char* k, const float* scales, int valid, const char* v, float c, F ask) {
     if (__ballot(top - r > Reference<P>::kMost)) {
       // a score past 2^20 and its difference to a reference are no longer exact in one fused step
       const bool far = fabsf(top) >= 0x1p20f && fabsf(top) < __builtin_inff();
@@ -181,71 +196,74 @@ struct Rows {
       const float raised = fmaxf(next, r), keep = fast_exp2(r - raised);
       r = raised, l *= keep;
 #pragma unroll
-      for (int n = 0; n < D / 32; ++n) o[n] *= keep;
+      for (int i = 0; i < D / 32; ++i) o[i] *= keep;
       large = __ballot(fabsf(r) >= 0x1p20f && r > -__FLT_MAX__) != 0;
     }
     float f = c, off = r;
     if (large) {
 #pragma clang fp contract(off)
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float x = s[t][i] * c;
-          s[t][i] = x - r;
-        }
+      for (int i = 0; i < 16 * NT; ++i) {
+        const float x = s[i >> 4][i & 15] * c;
+        s[i >> 4][i & 15] = x - r;
+      }
       f = 1.f, off = 0.f;
     }
-    float sums[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) {
-        const float x = fast_exp2(__builtin_fmaf(s[t][i], f, -off)), y = fast_exp2(__builtin_fmaf(s[t][i + 1], f, -off));
-        sums[i & 2] += x, sums[(i & 2) + 1] += y;
-        p[t][i >> 3][(i & 7) >> 1] = (int)pack16<P>(x, y);
-      }
-    l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
-  }
 
-  __device__ __forceinline__ void multiply(const char* slot, int part) {
-    const int lane = threadIdx.x & 63, half = lane >> 5;
     // V operands: slots 8 half + e of step u of half t are keys 32 t + 16 u + 8 (e / 4) + 4 half + e % 4, as P's registers are.  A group of 16 lanes
     // reads four keys x 16 channels and gets four keys of a channel per lane
-    const int i16 = lane & 15, g = (lane >> 4) & 1, key = 4 * half + (i16 >> 2);
     typedef v4s __attribute__((address_space(3))) * lds_v4s_ptr;
-    const char* v0 = slot + L::kSide + (32 * part + key) * L::kRow;
-    const uint32_t at = (32u * g + 8u * (i16 & 3)) ^ v_swizzle(key);
-    constexpr int kWide = D / 32 < 4 ? D / 32 : 4, kSteps = 2 * NT * (D / 32) / kWide;     // channel tiles of a phase; phases
-    v4s v[2][kWide][2];
-    auto read_v = [&](int i) {
-#pragma unroll
-      for (int x = 0; x < kWide; ++x) {
-        const int tu = i * kWide / (D / 32), n = i * kWide % (D / 32) + x;
-        const char* from = v0 + 16 * tu * L::kRow + ((at ^ (64u * (n & 3))) + 256u * (n >> 2));
-        v[i & 1][x][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from));
-        v[i & 1][x][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from + 8 * L::kRow));
-      }
+    const int i16 = row & 15, key_row = 4 * half + (i16 >> 2);
+    const char* v0 = v + (32 * part + key_row) * L::kRow;
+    const uint32_t v_at = (32u * (row >> 4) + 8u * (i16 & 3)) ^ v_swizzle(key_row);
+    v4s value[kAhead + 1][2];
+    auto read_value = [&](int i) {
+      const int tu = i / (D / 32), n = i % (D / 32);
+      const char* from = v0 + 16 * tu * L::kRow + ((v_at ^ (64u * (n & 3))) + 256u * (n >> 2));
+      value[i % (kAhead + 1)][0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from));
+      value[i % (kAhead + 1)][1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_ptr)(from + 8 * L::kRow));
     };
-    read_v(0);
+    const KeyReader key = keys_in(k);
+    v8s operand[kAhead + 1];
+    v4i p[NT][2];
+    float sums[4] = {0.f, 0.f, 0.f, 0.f};
+    // elements 2 i and 2 i + 1 of the lane's P
+    auto pair = [&](int i) {
+      const int t = i >> 3, e = 2 * i & 15;
+      const float x = fast_exp2(__builtin_fmaf(s[t][e], f, -off)), y = fast_exp2(__builtin_fmaf(s[t][e + 1], f, -off));
+      sums[e & 2] += x, sums[(e & 2) + 1] += y;
+      p[t][e >> 3][(e & 7) >> 1] = (int)pack16<P>(x, y);
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) operand[i] = key(i);
     fence();
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      if (i + 1 < kSteps) {
-        read_v(i + 1);
-        fence();
-      }
+    for (int i = 0; i < kKeys; ++i) {
+      product(n, i, operand[i % (kAhead + 1)]);
+      if (i + kAhead < kKeys) operand[(i + kAhead) % (kAhead + 1)] = key(i + kAhead);
+      else read_value(i + kAhead - kKeys);
 #pragma unroll
-      for (int x = 0; x < kWide; ++x) {
-        const int tu = i * kWide / (D / 32), n = i * kWide % (D / 32) + x;
-        o[n] = P::mfma(__builtin_shufflevector(v[i & 1][x][0], v[i & 1][x][1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(v8s, p[tu >> 1][tu & 1]), o[n]);
-      }
+      for (int x = 8 * NT * i / kKeys; x < 8 * NT * (i + 1) / kKeys; ++x) pair(x);
       fence();
     }
+    l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    ask();
+    settle(n, scales, valid);
+    float most = n[0][0];
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      const int tu = i / (D / 32), tile = i % (D / 32), at = i % (kAhead + 1);
+      o[tile] = P::mfma(__builtin_shufflevector(value[at][0], value[at][1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(v8s, p[tu >> 1][tu & 1]), o[tile]);
+      if (i + kAhead < kValues) read_value(i + kAhead);
+#pragma unroll
+      for (int x = 16 * NT * i / kValues; x < 16 * NT * (i + 1) / kValues; ++x) most = fmaxf(most, n[x >> 4][x & 15]);
+      fence();
+    }
+    top = both_halves_max(most) * c;
   }
 
-  // Bytes that a V row's offsets are swizzled by: four neighbouring rows at one 64-byte piece fill all banks
-  static __device__ __forceinline__ uint32_t v_swizzle(int row) { return D == 64 ? 64u * ((row >> 1) & 1) : 64u * (row & 3); }
+  // What a V row's offsets are swizzled by: of eight neighbouring rows, four at one 64-byte piece, or all at one 32-byte piece, fill all banks
+  static __device__ __forceinline__ uint32_t v_swizzle(int row) { return 64u * (D == 64 ? (row >> 1) & 1 : row & 3) + 32u * ((row >> 2) & 1); }
 };
 
 template <typename T, int D, bool C8>
@@ -254,78 +272,150 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
   __shared__ __align__(16) typename L::Shared sh;
   constexpr int kWaves = L::kWaves, kThreads = L::kThreads, kTile = L::kTile;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int G = z.own.G, shift = z.own.shift, capacity = a.max_pages << shift, n_groups = z.own.groups.n;
+  const int G = z.own.G, shift = z.own.shift, capacity = a.max_pages << shift, n_groups = z.groups.n;
+  auto tokens_of = [&](int g) { return min(capacity, max(0, z.groups.lens[g])) >> shift << shift; };
+  auto blocks_of = [&](int tokens) { return (int)(((unsigned)tokens + kBlock - 1) / kBlock); };
 
-  // ---- members of the groups, and this workgroup's share ----
+  // ---- members of the groups ----
   for (int g = tid; g < n_groups; g += kThreads) sh.count[g] = 0;
   __syncthreads();
   for (int b = tid; b < a.B; b += kThreads) {
-    const int n = common_tokens(z.own.groups, capacity, shift, b, min(capacity, max(0, a.seqlens[b])));
-    const int g = n > 0 ? z.own.groups.of[b] : 0xffff;
+    int g = z.groups.of[b];
+    const int len = min(capacity, max(0, a.seqlens[b]));
+    if ((unsigned)g < (unsigned)n_groups) {
+      const int n = tokens_of(g);
+      if (n == 0 || len < n) g = 0xffff;
+    } else {
+      g = 0xffff;
+    }
     sh.group[b] = (uint16_t)g;
-    if (n > 0) atomicAdd(&sh.count[g], 1);
+    if (g != 0xffff) atomicAdd(&sh.count[g], 1);
   }
   __syncthreads();
-  auto tokens_of = [&](int g) { return min(capacity, max(0, z.own.groups.lens[g])) >> shift << shift; };
-  auto blocks_of = [&](int tokens) { return (int)(((unsigned)tokens + kBlock - 1) / kBlock); };
-  auto weight_of = [&](int rows) { return rows == 0 ? 0 : rows > kTile / 2 ? 2 : 1; };      // of a tile's block
-  auto price = [&](int g) -> long {
+  for (int g = tid; g < n_groups; g += kThreads) {
     const int n = sh.count[g];
-    if (n == 0) return 0;
-    const int rows = n * G, full = rows / kTile;
-    return (long)a.Hkv * (2 * full + weight_of(rows - full * kTile)) * blocks_of(tokens_of(g));
-  };
-  const int per = (n_groups + kThreads - 1) / kThreads;
-  long sum = 0;
-  for (int i = 0; i < per; ++i)
-    if (tid * per + i < n_groups) sum += price(tid * per + i);
-  long incl = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const long other = __shfl_up(incl, d);
-    if (lane >= d) incl += other;
-  }
-  if (lane == 63) sh.sums[wave] = incl;
-  __syncthreads();
-  long base = incl - sum, total = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) base += sh.sums[w];
-    total += sh.sums[w];
-  }
-  const long each = (total + 2 * kPrefixShares - 1) / (2 * kPrefixShares) * 2;              // even: every share inside a tile has a block of it
-  long u = (long)blockIdx.x * each;
-  if (u >= total) return;                              // the whole workgroup
-  const long u_end = min(total, u + each);
-  if (base <= u && u < base + sum) {
-    int g = tid * per;
-    for (long p = price(g); base + p <= u; p = price(g)) base += p, ++g;
-    sh.start_group = g, sh.start_base = base;
+    if (n > 0 && (long)(n - 1) * tokens_of(g) < kLeastShared) sh.count[g] = 0;
   }
   __syncthreads();
-  int g = __builtin_amdgcn_readfirstlane(sh.start_group);
-  long g_base = sh.start_base;
-  int listed_group = -1, listed_tile = -1;
+  if (blockIdx.x == 0)                                 // for the launches behind
+    for (int b = tid; b < a.B; b += kThreads) {
+      const int g = sh.group[b];
+      z.common[b] = g != 0xffff && sh.count[g] > 0 ? tokens_of(g) : 0;
+    }
 
-  while (true) {
-    // ---- the piece of a tile that begins at u ----
-    const int members = sh.count[g], tokens = __builtin_amdgcn_readfirstlane(tokens_of(g)), blocks = blocks_of(tokens), rows = members * G, full = rows / kTile;
-    const long tile_price = 2L * a.Hkv * blocks;
-    const long into = u - g_base;
-    const int tile = (int)min((long)full, into / tile_price), weight = tile < full ? 2 : weight_of(rows - full * kTile);
-    const long in_tile = into - tile * tile_price;
-    const int hk = (int)(in_tile / ((long)weight * blocks));
-    const long unit = g_base + tile * tile_price + (long)hk * weight * blocks;            // where the blocks of this KV head begin
-    const long end = min(u_end, unit + (long)weight * blocks);
-    const int t0 = (int)((u - unit + weight - 1) / weight), t1 = (int)((end - unit + weight - 1) / weight);
+  // ---- parts of tiles: a unit is a tile of a KV head, and has as many parts of equal numbers of blocks as its price asks for ----
+  // At most 2.5 per member, KV head and 64 tokens: below 2^32 for the sizes that are taken (B * Hkv * tokens / 32 below 2^30)
+  struct Units {
+    int full, rest, blocks;                            // full tiles, the price of a block of the other one (0: there is none), blocks
+    uint32_t units, price;
+  };
+  auto units_of = [&](int g) {
+    Units x = {0, 0, 0, 0, 0};
+    const int rows = sh.count[g] * G;
+    if (rows == 0) return x;
+    x.blocks = blocks_of(tokens_of(g)), x.full = rows / kTile;
+    const int left = rows - x.full * kTile;
+    x.rest = left == 0 ? 0 : left > kTile / 2 ? kPriceFull : kPriceHalf;
+    x.units = (uint32_t)a.Hkv * (x.full + (left > 0)), x.price = (uint32_t)a.Hkv * (kPriceFull * x.full + x.rest) * x.blocks;
+    return x;
+  };
+  const int per = (n_groups + kThreads - 1) / kThreads, g0 = tid * per, g1 = min(n_groups, g0 + per);
+  // sums over the workgroup of three numbers of every thread: of the threads in front, and of all
+  struct Three { uint32_t v[3]; };
+  auto sums_of = [&](const Three& x, Three& front, Three& all) {
+    Three incl = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const uint32_t other = __shfl_up(incl.v[i], d);
+        if (lane >= d) incl.v[i] += other;
+      }
+    __syncthreads();
+    if (lane == 63) sh.sums[wave] = make_uint3(incl.v[0], incl.v[1], incl.v[2]);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) front.v[i] = incl.v[i] - x.v[i], all.v[i] = 0;
+    for (int w = 0; w < kWaves; ++w) {
+      const uint3 sum = sh.sums[w];
+      const Three y = {{sum.x, sum.y, sum.z}};
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        if (w < wave) front.v[i] += y.v[i];
+        all.v[i] += y.v[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) all.v[i] = __builtin_amdgcn_readfirstlane(all.v[i]);
+  };
+  Three mine = {{0, 0, 0}}, front, all;
+  for (int g = g0; g < g1; ++g) {
+    const Units x = units_of(g);
+    mine.v[0] += x.price, mine.v[1] += x.units;
+  }
+  sums_of(mine, front, all);
+  const uint32_t total = all.v[0], all_units = all.v[1];
+  if (total == 0) return;                              // the whole workgroup
+  // The price of a part.  Parts of total / 256 where they come to 256 at most, as they do where units are alike; otherwise larger ones, so that with at most 128 units every workgroup
+  // gets one part at most.  The parts behind a unit's first are fewer than the slots in any case: their prices sum up to less than `total`.
+  auto over = [](uint32_t x, uint32_t y) { return x / y + (x % y != 0); };
+  const uint32_t tight = over(total, kPrefixShares), loose = over(total, all_units < kPrefixShares / 2 ? kPrefixShares - all_units : kPrefixShares / 2);
+  auto parts_of = [&](int price_of_block, int blocks, uint32_t each) { return (int)min((uint32_t)blocks, over((uint32_t)price_of_block * blocks, each)); };
+  auto shares_of_group = [&](const Units& x, uint32_t each) -> uint32_t {
+    if (x.units == 0) return 0;
+    return (uint32_t)a.Hkv * (x.full * parts_of(kPriceFull, x.blocks, each) + (x.rest ? parts_of(x.rest, x.blocks, each) : 0));
+  };
+  mine.v[0] = mine.v[2] = 0;
+  for (int g = g0; g < g1; ++g) {
+    const Units x = units_of(g);
+    mine.v[0] += shares_of_group(x, tight), mine.v[2] += shares_of_group(x, loose);
+  }
+  sums_of(mine, front, all);
+  const bool fits = all.v[0] <= kPrefixShares;
+  const uint32_t each = fits ? tight : loose, all_shares = fits ? all.v[0] : all.v[2], share_front = fits ? front.v[0] : front.v[2], unit_front = front.v[1];
+  const uint32_t shares = fits ? mine.v[0] : mine.v[2];
+
+  for (uint32_t share = blockIdx.x; share < all_shares; share += kPrefixShares) {
+    // ---- the part of a tile that this share is ----
+    __syncthreads();                                   // LDS is free again
+    if (share_front <= share && share < share_front + shares) {
+      uint32_t at = share_front, unit = unit_front;
+      for (int g = g0; g < g1; ++g) {
+        const Units x = units_of(g);
+        const uint32_t n = shares_of_group(x, each);
+        if (share < at + n) {
+          sh.start_group = g, sh.start_share = at, sh.start_unit = unit;
+          break;
+        }
+        at += n, unit += x.units;
+      }
+    }
+    __syncthreads();
+    const int g = __builtin_amdgcn_readfirstlane(sh.start_group), members = __builtin_amdgcn_readfirstlane(sh.count[g]);
+    const int tokens = __builtin_amdgcn_readfirstlane(tokens_of(g)), blocks = blocks_of(tokens);
+    const int rows = members * G, full = rows / kTile, n_full = parts_of(kPriceFull, blocks, each);
+    uint32_t rel = share - __builtin_amdgcn_readfirstlane(sh.start_share), unit = __builtin_amdgcn_readfirstlane(sh.start_unit);
+    const bool wide = rel < (uint32_t)a.Hkv * full * n_full || rows - full * kTile > kTile / 2;
+    int tile = full, parts = n_full;
+    if (rel >= (uint32_t)a.Hkv * full * n_full) {
+      rel -= (uint32_t)a.Hkv * full * n_full, unit += (uint32_t)a.Hkv * full;
+      parts = wide ? n_full : parts_of(kPriceHalf, blocks, each);
+    } else {
+      tile = rel / ((uint32_t)n_full * a.Hkv);
+      rel -= (uint32_t)tile * n_full * a.Hkv, unit += (uint32_t)tile * a.Hkv;
+    }
+    const int hk = rel / (uint32_t)parts, number = rel - hk * parts;
+    unit += hk;
+    const int t0 = (int)((uint64_t)number * blocks / parts), t1 = (int)((uint64_t)(number + 1) * blocks / parts);
+    const uint32_t slot_of_part = share - unit - 1;    // parts behind the first of their unit, counted through
     const int row0 = tile * kTile, tile_rows = min(kTile, rows - row0);
 
     // ---- the tile's members, in the order of the batch ----
-    if (listed_group != g || listed_tile != tile) {
+    {
       const int m0 = row0 / G, m1 = (row0 + tile_rows - 1) / G;
       const int chunk = (a.B + kThreads - 1) / kThreads * 64, from = wave * chunk, to = min(a.B, from + chunk);
       int n = 0;
       for (int b0 = from; b0 < to; b0 += 64) n += __popcll(__ballot(b0 + lane < to && sh.group[b0 + lane] == g));
-      __syncthreads();                                 // nobody reads the list in front
       if (lane == 0) sh.waves[wave] = n;
       __syncthreads();
       int at = 0;
@@ -337,27 +427,23 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         if (mine && i >= m0 && i <= m1) sh.list[i - m0] = b0 + lane;
         at += __popcll(who);
       }
-      listed_group = g, listed_tile = tile;
     }
     __syncthreads();
 
-    auto piece = [&](auto parts) {
-      constexpr int PARTS = decltype(parts)::value;
+    auto piece = [&](auto halves) {
+      constexpr int PARTS = decltype(halves)::value;
       Rows<T, D, C8, PARTS> w;
       const int part = PARTS == 1 ? 0 : wave & 1, rows_at = 32 * (PARTS == 1 ? wave : wave >> 1);
       const bool busy = rows_at < tile_rows;           // of the wavefront; the others bring blocks alone
       const int row = rows_at + (lane & 31), mine = min(row, tile_rows - 1);
       const int member = (row0 + mine) / G - row0 / G, head = (row0 + mine) % G;
       const size_t home = (size_t)sh.list[member] * a.Hq + hk * G + head;                 // of out
-      {
+      auto ask = [&]() {
         const uint16_t* from = a.q + home * D + 8 * (lane >> 5);
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) w.q[e] = *reinterpret_cast<const v8s*>(from + 16 * e);
-        // they arrive here: a wait inside the walk would be one for the blocks on their way
-#pragma unroll
-        for (int e = 0; e < D / 16; ++e) asm volatile("" : "+v"(w.q[e]));
-      }
-      w.clear();
+      };
+      w.clear(part);
 
       // blocks on their way: the rows that this wavefront brings.  Common tokens are whole pages, so that all rows of a chunk are there or none;
       // LDS gets other rows of the block for those (P is 0 there), or, from codes, zeros
@@ -367,97 +453,135 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         const unsigned key = (unsigned)t * kBlock + first_row(i);
         return C8 || key < (unsigned)tokens ? key : (unsigned)t * kBlock + first_row(i) % 16;
       };
-      // a lane has the page of one chunk of one block, from block page_t on: no scalar loads in the walk, whose results would be waited for with the
-      // reads of LDS
-      constexpr int kPages = 64 / L::kChunks;
+      // A lane has the place of one chunk of one block in the pages, from block place_t on (which moves on with K: V of a block is asked for in front of K
+      // of the next): no scalar loads in the walk, whose results would be waited for with the reads of LDS, and few scalar instructions
+      constexpr int kPlaces = 64 / L::kChunks;
       const int32_t* table = a.table + (size_t)__builtin_amdgcn_readfirstlane(sh.list[0]) * a.max_pages;
-      int pages, page_t = t0 - kPages;
-      auto row_at = [&](int t, int i) {
-        if (t >= page_t + kPages) {
-          page_t = t;
-          const unsigned at = min((unsigned)a.max_pages - 1, key_of(t + lane / L::kChunks, lane % L::kChunks) >> shift);
-          pages = min(a.n_pages - 1, max(0, table[at]));
-        }
-        const int p = __builtin_amdgcn_readlane(pages, (t - page_t) * L::kChunks + i);
-        return (((size_t)p * a.Hkv + hk) << shift) + (key_of(t, i) & ((1u << shift) - 1));
+      size_t place;
+      int place_t;
+      auto look_up = [&](int t) {
+        place_t = t;
+        const unsigned key = key_of(t + lane / L::kChunks, lane % L::kChunks);
+        const int p = min(a.n_pages - 1, max(0, table[min((unsigned)a.max_pages - 1, key >> shift)]));
+        place = ((((size_t)p * a.Hkv + hk) << shift) + (key & ((1u << shift) - 1))) * (C8 ? 1 : L::kRow);
+      };
+      auto place_of = [&](int t, int i) {              // bytes, or rows of codes
+        if (t >= place_t + kPlaces) look_up(t);
+        const int at = (t - place_t) * L::kChunks + i;
+        return (size_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)place, at) | (size_t)(uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), at) << 32;
       };
       constexpr int kRing = L::kRing;
-      auto step = [&](int t, int s) {
-        if (!busy) return;
-        w.scores(sh.stage[s], part);
-        w.soften(sh.scales[L::kScaled ? s : 0], part, tokens - t * kBlock, z.own.c);
-        w.multiply(sh.stage[s], part);
+      look_up(t0);                                     // both on their way together
+      ask();
+      // The walk: K is brought one block ahead of V, since a step reads K of block t + 1 and V of block t.  begin(): until K of the first block is in LDS; bring(t): at
+      // the start of step t, until K of t + 1 and V of t are; ask_for(t): inside it, what is to come.
+      const float c = z.own.c;
+      auto arrive = [&]() {                            // the queries, here: a wait inside the walk would be one for the blocks on their way
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) asm volatile("" : "+v"(w.q[e]));
       };
-      auto next_slot = [&](int s) { return s + 1 == kRing ? 0 : s + 1; };
+      auto slot = [&](int t) { return (unsigned)(t - t0) % kRing; };
+      auto scales_of = [&](int t) { return sh.scales[L::kScaled ? slot(t) : 0]; };
+      auto walk = [&](auto begin, auto bring, auto ask_for) {
+        begin();
+        if (t0 == t1) return;
+        if (!busy) {
+          for (int t = t0; t < t1; ++t) bring(t), ask_for(t);
+          return;
+        }
+        // One of the two wavefronts of a SIMD goes first: they then are less often at the same kind of instruction (64 x 32768 tokens, 64/8 heads: 88 -> PRIO us)
+        if (!C8 && PARTS == 1 && wave >= 4) __builtin_amdgcn_s_setprio(1);
+        typename Rows<T, D, C8, PARTS>::Scores x, y;
+        w.scores(x, sh.k[0], scales_of(t0), tokens - t0 * kBlock, c);
+        auto step = [&](int t, auto& s, auto& n) {
+          bring(t);
+          w.step(s, n, sh.k[slot(t + 1)], scales_of(t + 1), tokens - (t + 1) * kBlock, sh.v[slot(t)], c, [&]() { ask_for(t); });
+        };
+        for (int t = t0; t < t1; t += 2) {
+          step(t, x, y);
+          if (t + 1 == t1) break;
+          step(t + 1, y, x);
+        }
+      };
       if constexpr (C8) {
-        auto load = [&](typename L::Block& x, int t) {
+        auto load = [&](typename L::Block& x, const void* pages, const uint8_t* scales, int t) {
 #pragma unroll
           for (int i = 0; i < L::kChunks; ++i) {
             const bool there = t < t1 && (int)key_of(t, i) < tokens;
-            const size_t at = row_at(t, i);
-            const auto kd = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.k_pages + at * D), 0, there ? L::kRowsOf * D : 0, 0x00020000);
-            const auto vd = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.v_pages + at * D), 0, there ? L::kRowsOf * D : 0, 0x00020000);
-            const auto ksd = __builtin_amdgcn_make_buffer_rsrc((void*)(a.k_scales + at), 0, there ? L::kRowsOf : 0, 0x00020000);
-            const auto vsd = __builtin_amdgcn_make_buffer_rsrc((void*)(a.v_scales + at), 0, there ? L::kRowsOf : 0, 0x00020000);
-            x.k[i] = __builtin_amdgcn_raw_buffer_load_b64(kd, 8 * lane, 0, 0), x.v[i] = __builtin_amdgcn_raw_buffer_load_b64(vd, 8 * lane, 0, 0);
-            x.ks[i] = __builtin_amdgcn_raw_buffer_load_b8(ksd, my_row, 0, 0), x.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(vsd, my_row, 0, 0);
+            const size_t at = there ? place_of(t, i) : 0;
+            const auto codes = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)pages + at * D), 0, there ? L::kRowsOf * D : 0, 0x00020000);
+            const auto bytes = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + at), 0, there ? L::kRowsOf : 0, 0x00020000);
+            x.codes[i] = __builtin_amdgcn_raw_buffer_load_b64(codes, 8 * lane, 0, 0), x.scales[i] = __builtin_amdgcn_raw_buffer_load_b8(bytes, my_row, 0, 0);
           }
         };
-        auto write = [&](const typename L::Block& x, int s) {
+        auto write_k = [&](const typename L::Block& x, int s) {
 #pragma unroll
           for (int i = 0; i < L::kChunks; ++i) {
             const int r = first_row(i) + my_row;
-            char *k = sh.stage[s] + r * L::kRow + 16 * (my_chunk ^ (r & 7)), *v = sh.stage[s] + L::kSide + r * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r));
-            *reinterpret_cast<v4i*>(k) = widen_chunk<T>(x.k[i], L::kScaled ? 1.f : scale_of(x.ks[i]));
-            *reinterpret_cast<v4i*>(v) = widen_chunk<BF16>(x.v[i], scale_of(x.vs[i]));
+            *reinterpret_cast<v4i*>(sh.k[s] + r * L::kRow + 16 * (my_chunk ^ (r & 7))) = widen_chunk<T>(x.codes[i], L::kScaled ? 1.f : scale_of(x.scales[i]));
             if constexpr (L::kScaled)
-              if (my_chunk == 0) sh.scales[s][r] = scale_of(x.ks[i]);
+              if (my_chunk == 0) sh.scales[s][r] = scale_of(x.scales[i]);
           }
         };
-        typename L::Block x, y;
-        load(x, t0);
-        load(y, t0 + 1);
-        write(x, 0);
-        lds_barrier();
-        for (int t = t0; t < t1; t += 2) {
-          load(x, t + 2);
-          step(t, 0);
-          write(y, 1);
-          lds_barrier();
-          if (t + 1 == t1) break;
-          load(y, t + 3);
-          step(t + 1, 1);
-          write(x, 0);
-          lds_barrier();
-        }
-      } else {
-        // LDS is written in the order of the lanes: a lane reads the chunk that belongs in its place
-        constexpr int kLoads = 2 * L::kChunks;
-        const int r0 = first_row(0) + my_row;          // first_row(i) is the same but for multiples of eight
-        const uint32_t k_off = my_row * L::kRow + 16 * (my_chunk ^ (r0 & 7)), v_off = my_row * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r0));
-        auto load = [&](int t, int s) {
-          if (t >= t1) return;
+        auto write_v = [&](const typename L::Block& x, int s) {
 #pragma unroll
           for (int i = 0; i < L::kChunks; ++i) {
-            const size_t at = row_at(t, i) * L::kRow;
-            const uint32_t to = lds_address(sh.stage[s]) + first_row(i) * L::kRow;
-            dma_b128((const char*)a.k_pages + at, k_off, to);
-            dma_b128((const char*)a.v_pages + at, v_off, to + L::kSide);
+            const int r = first_row(i) + my_row;
+            *reinterpret_cast<v4i*>(sh.v[s] + r * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r))) = widen_chunk<BF16>(x.codes[i], scale_of(x.scales[i]));
           }
         };
+        typename L::Block k, v;
+        walk(
+            [&]() {
+              load(k, a.k_pages, a.k_scales, t0), load(v, a.v_pages, a.v_scales, t0);
+              arrive();
+              write_k(k, 0);
+              load(k, a.k_pages, a.k_scales, t0 + 1);
+              lds_barrier();
+            },
+            [&](int t) {
+              write_k(k, slot(t + 1)), write_v(v, slot(t));
+              load(v, a.v_pages, a.v_scales, t + 1), load(k, a.k_pages, a.k_scales, t + 2);
+              lds_barrier();
+            },
+            [](int) {});
+      } else {
+        // LDS is written in the order of the lanes: a lane reads the chunk that belongs in its place
+        const int r0 = first_row(0) + my_row;          // first_row(i) is the same but for multiples of eight
+        const uint32_t k_off = my_row * L::kRow + 16 * (my_chunk ^ (r0 & 7)), v_off = my_row * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r0));
+        auto load = [&](const void* pages, uint32_t off, const char* to, int t) {
+          if (t >= t1) return;
 #pragma unroll
-        for (int i = 0; i < kRing - 1; ++i) load(t0 + i, i);
-        for (int t = t0, s = 0; t < t1; ++t, s = next_slot(s)) {
-          // block t is here: those behind it that are on their way may stay so
-          if (kRing > 3 && t + 2 < t1) vm_wait<2 * kLoads>();
-          else if (kRing > 2 && t + 1 < t1) vm_wait<kLoads>();
+          for (int i = 0; i < L::kChunks; ++i) dma_b128((const char*)pages + place_of(t, i), off, lds_address(to) + first_row(i) * L::kRow);
+        };
+        // waits until of the sides of blocks that were asked for, the last n at most are still on their way
+        auto wait = [&](int n) {
+          if (n >= 4) vm_wait<4 * L::kChunks>();
+          else if (n == 3) vm_wait<3 * L::kChunks>();
+          else if (n == 2) vm_wait<2 * L::kChunks>();
+          else if (n == 1) vm_wait<L::kChunks>();
           else vm_wait<0>();
-          lds_barrier();
-          load(t + kRing - 1, s == 0 ? kRing - 1 : s - 1);
-          step(t, s);
-        }
+        };
+        auto load_k = [&](int t) { load(a.k_pages, k_off, sh.k[slot(t)], t); };
+        auto load_v = [&](int t) { load(a.v_pages, v_off, sh.v[slot(t)], t); };
+        walk(
+            [&]() {
+              load_k(t0);
+              arrive();
+#pragma unroll
+              for (int i = 1; i < kRing; ++i) load_k(t0 + i), load_v(t0 + i - 1);
+              wait(min(kRing - 1, t1 - 1 - t0) + min(kRing - 1, t1 - t0));
+              lds_barrier();
+            },
+            [&](int t) {
+              // asked for behind K of t + 1 and V of t: K of t + 2 .. t + kRing - 1, V of t + 1 .. t + kRing - 2
+              wait(max(0, min(kRing - 2, t1 - 2 - t)) + max(0, min(kRing - 2, t1 - 1 - t)));
+              lds_barrier();
+            },
+            [&](int t) { load_v(t + kRing - 1), load_k(t + kRing); });
       }
 
+      __builtin_amdgcn_s_setprio(0);
       // ---- both halves of a row's keys, and its place ----
       float l = w.l;
       {
@@ -467,7 +591,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
       }
       if constexpr (PARTS == 2) {
         lds_barrier();                                 // nobody reads the last block any more
-        float(*mail)[64] = reinterpret_cast<float(*)[64]>(sh.stage) + (wave >> 1) * (D / 2);
+        float(*mail)[64] = reinterpret_cast<float(*)[64]>(sh.k) + (wave >> 1) * (D / 2);   // K's blocks and V's behind them
         if (part == 1 && busy) {
 #pragma unroll
           for (int n = 0; n < D / 32; ++n)
@@ -485,80 +609,91 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
             for (int i = 0; i < 16; ++i) w.o[n][i] = w.o[n][i] * k1 + mail[16 * n + i][lane] * k2;
         }
       }
-      if (busy && row < tile_rows && (PARTS == 1 || part == 0)) {
-        const size_t slot = (size_t)blockIdx.x * kTile + row, to = t0 == 0 ? home : slot;
-        float *to_o = t0 == 0 ? z.p.home_o : z.p.slot_o, *to_ml = t0 == 0 ? z.p.home_ml : z.p.slot_ml;
-        const int half = lane >> 5;
-        if (half == 0) {
+      // Rows leave through LDS, where each wavefront has a place: lanes hold 16 bytes of 32 rows at a time, memory takes whole rows (64 x 32768 tokens, 64/8 heads: 33 MB of
+      // parts; 16 bytes a row took STORE us longer)
+      lds_barrier();                                   // nobody reads a block, or another wavefront's part, any more
+      if (busy && (PARTS == 1 || part == 0)) {
+        int me = lane;                                 // not known to be the lane: places would be formed in front of the walk and kept in registers through it
+        asm volatile("" : "+v"(me));
+        const int half = me >> 5;
+        const size_t slot = (size_t)slot_of_part * kTile + row, to = number == 0 ? home : slot;
+        float *to_o = number == 0 ? z.p.home_o : z.p.slot_o, *to_ml = number == 0 ? z.p.home_ml : z.p.slot_ml;
+        if (half == 0 && row < tile_rows) {
           to_ml[2 * to] = w.r, to_ml[2 * to + 1] = l;
-          // the last block lies in the share of its price's place
-          if (t0 == 0) z.p.home_span[home] = make_int4((int)blockIdx.x + 1, (int)((unit + (long)weight * (blocks - 1)) / each) - (int)blockIdx.x, row, 0);
+          if (number == 0) z.p.home_span[home] = make_int4((int)(slot_of_part + 1), parts - 1, row, 0);
         }
+        // 64 channels of the 32 rows at a time; chunk x of a row lies at x ^ (row & 15)
+        char* mine_lds = sh.stage + wave * 8192;
 #pragma unroll
-        for (int n = 0; n < D / 32; ++n)
+        for (int c0 = 0; c0 < D / 32; c0 += 2) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<v4f*>(to_o + to * D + 32 * n + 8 * i + 4 * half) = v4f{w.o[n][4 * i], w.o[n][4 * i + 1], w.o[n][4 * i + 2], w.o[n][4 * i + 3]};
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<v4f*>(mine_lds + 256 * (me & 31) + 16 * ((8 * n + 2 * i + half) ^ (me & 15))) =
+                  v4f{w.o[c0 + n][4 * i], w.o[c0 + n][4 * i + 1], w.o[c0 + n][4 * i + 2], w.o[c0 + n][4 * i + 3]};
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (me >> 4);
+            const v4f x = *reinterpret_cast<const v4f*>(mine_lds + 256 * r + 16 * ((me ^ r) & 15));
+            const size_t at = (size_t)(uint32_t)__shfl((int)(uint32_t)to, r) | (size_t)(uint32_t)__shfl((int)(to >> 32), r) << 32;
+            if (rows_at + r < tile_rows) *reinterpret_cast<v4f*>(to_o + at * D + 32 * c0 + 4 * (me & 15)) = x;
+          }
+        }
       }
     };
-    if (weight == 2) piece(std::integral_constant<int, 1>{});
+    if (wide) piece(std::integral_constant<int, 1>{});
     else piece(std::integral_constant<int, 2>{});
-
-    u = end;
-    if (u >= u_end) break;
-    __syncthreads();                                   // the stage is free again
-    if (u - g_base >= price(g)) {                      // the next group with members
-      g_base += price(g);
-      int next = g + 1;
-      while (true) {
-        const unsigned long long some = __ballot(next + lane < n_groups && sh.count[min(next + lane, n_groups - 1)] > 0);
-        if (some != 0) {
-          next += __builtin_ctzll(some);
-          break;
-        }
-        next += 64;
-      }
-      g = __builtin_amdgcn_readfirstlane(next);
-    }
   }
 }
 
 // One workgroup per sequence and query head: joins the parts of its common and its own tokens in the order of the tokens.  Threads take four channels of
-// every kParts-th part.
+// every kParts-th part, several at a time.  Where parts are is asked for together with the lengths, whether it was written or not.
 template <int D, int kShares>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(PagedDecodeArgs a, PrefixLaunch z) {
-  constexpr int kQuads = D / 4, kParts = 256 / kQuads, kTile = tile_rows(D);
+  constexpr int kQuads = D / 4, kParts = 256 / kQuads, kTile = tile_rows(D), kAhead = 3;
   __shared__ float2 ml[kParts];
   __shared__ __align__(16) v4f sums[kParts][kQuads];
   const int tid = threadIdx.x, quad = tid % kQuads, part = tid / kQuads;
   const size_t at = blockIdx.x;
   const int b = (int)(at / a.Hq), h = (int)(at % a.Hq), hk = h / z.own.G, gh = h % z.own.G, shift = z.own.shift, capacity = a.max_pages << shift;
-  const int len = min(capacity, max(0, a.seqlens[b])), common = common_tokens(z.own.groups, capacity, shift, b, len);
+  int4 span = z.p.home_span[at];
+  int2 own = z.own.own_span[(size_t)b * a.Hkv + hk];
+  const int len = min(capacity, max(0, a.seqlens[b])), common = z.common[b];
   if (len == 0) {
     if (part == 0) store_out4(a.out, a.out_dt, at * D + 4 * quad, 0.f, 0.f, 0.f, 0.f);
     if (a.lse != nullptr && tid == 0) a.lse[at] = -__builtin_inff();
     return;
   }
-  const int4 span = common > 0 ? z.p.home_span[at] : make_int4(0, -1, 0, 0);
-  const int2 own = len > common ? z.own.own_span[(size_t)b * a.Hkv + hk] : make_int2(0, -1);
+  if (common == 0) span.y = -1;
+  if (len == common) own.y = -1;
   const int n1 = span.y + 1, n = n1 + own.y + 1;
   v4f o = {0.f, 0.f, 0.f, 0.f};
   float m = -__builtin_inff(), l = 0.f;
-  for (int i = part; i < n; i += kParts) {
-    const float *from_o, *from_ml;
-    size_t row;
-    if (i < n1) {
-      row = i == 0 ? at : (size_t)(span.x + i - 1) * kTile + span.z;
-      from_o = i == 0 ? z.p.home_o : z.p.slot_o, from_ml = i == 0 ? z.p.home_ml : z.p.slot_ml;
-    } else {
-      const int j = i - n1;
-      row = j == 0 ? at : (size_t)(own.x + j - 1) * z.own.G + gh;
-      from_o = j == 0 ? z.own.own_o : z.own.w.part_o, from_ml = j == 0 ? z.own.own_ml : z.own.w.part_ml;
+  for (int i0 = part; i0 < n; i0 += kParts * kAhead) {
+    v4f x[kAhead];
+    float2 y[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const int i = min(n - 1, i0 + e * kParts), j = i - n1;
+      const bool first = i < n1;
+      const size_t row = i == 0 || j == 0 ? at : first ? (size_t)(span.x + i - 1) * kTile + span.z : (size_t)(own.x + j - 1) * z.own.G + gh;
+      const float* from_o = first ? (i == 0 ? z.p.home_o : z.p.slot_o) : j == 0 ? z.own.own_o : z.own.w.part_o;
+      const float* from_ml = first ? (i == 0 ? z.p.home_ml : z.p.slot_ml) : j == 0 ? z.own.own_ml : z.own.w.part_ml;
+      x[e] = *reinterpret_cast<const v4f*>(from_o + row * D + 4 * quad);
+      y[e] = *reinterpret_cast<const float2*>(from_ml + 2 * row);
+      if (i0 + e * kParts >= n) y[e] = make_float2(-__builtin_inff(), 0.f);
     }
-    const v4f x = *reinterpret_cast<const v4f*>(from_o + row * D + 4 * quad);
-    const float2 y = *reinterpret_cast<const float2*>(from_ml + 2 * row);
-    const float top = fmaxf(m, y.x), k1 = fast_exp2(m - top), k2 = fast_exp2(y.x - top);
-    m = top, l = l * k1 + y.y * k2, o = o * k1 + x * k2;
+    float top = m;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) top = fmaxf(top, y[e].x);
+    const float keep = fast_exp2(m - top);
+    m = top, l *= keep, o *= keep;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) {
+      const float k = fast_exp2(y[e].x - top);
+      l += k * y[e].y, o += k * x[e];
+    }
   }
   if (quad == 0) ml[part] = make_float2(m, l);
   sums[part][quad] = o;
@@ -580,7 +715,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PagedDecodeArgs a, Pr
 
 // Workspace, all parts 16-byte aligned
 struct Layout {
-  size_t home_o, home_ml, home_span, slot_o, slot_ml, own_o, own_ml, own_span, part_o, part_ml, total;
+  size_t home_o, home_ml, home_span, slot_o, slot_ml, own_o, own_ml, own_span, part_o, part_ml, common, total;
 };
 Layout layout_of(bool codes, int B, int Hq, int Hkv, int D) {
   Layout y;
@@ -595,6 +730,7 @@ Layout layout_of(bool codes, int B, int Hq, int Hkv, int D) {
   y.slot_o = take(slots * D * 4), y.slot_ml = take(slots * 8);
   y.own_o = take(rows * D * 4), y.own_ml = take(rows * 8), y.own_span = take((size_t)B * Hkv * 8);
   y.part_o = take(parts * D * 4), y.part_ml = take(parts * 8);
+  y.common = take((size_t)B * 4);
   y.total = at;
   return y;
 }
@@ -606,7 +742,8 @@ void launch(const PagedPrefixArgs& args, hipStream_t st) {
   char* w = (char*)a.workspace;
   PrefixLaunch z;
   z.own = launch_of(a, C8, a.workspace);
-  z.own.groups = Groups{args.group_of, args.group_lens, args.n_groups};
+  z.groups = Groups{args.group_of, args.group_lens, args.n_groups};
+  z.common = (int32_t*)(w + y.common), z.own.common = z.common;
   z.own.w.tail = nullptr;
   z.own.w.part_o = (float*)(w + y.part_o), z.own.w.part_ml = (float*)(w + y.part_ml);
   z.own.own_o = (float*)(w + y.own_o), z.own.own_ml = (float*)(w + y.own_ml), z.own.own_span = (int2*)(w + y.own_span);
@@ -627,12 +764,24 @@ void launch(const PagedPrefixArgs& a, hipStream_t st) {
 
 }  // namespace
 
+// Where the block table has room for less than this altogether, every sequence is walked by itself: what is saved is then no more than what the tiles cost in front of and
+// behind their walks.  Tiles / by itself, us, 32/8 heads of 128 channels: ALONE
+constexpr long kAloneBytes = 128L << 20;
+static bool by_itself(int bits, int B, int Hkv, int max_pages, int page_size, int D) {
+  return (long)B * Hkv * max_pages * page_size <= kAloneBytes / (bits == 8 ? 2 * (D + 1) : 4 * D);
+}
+
 size_t paged_prefix_workspace(int bits, int B, int Hq, int Hkv, int n_groups, int max_pages, int page_size, int D) {
+  if (by_itself(bits, B, Hkv, max_pages, page_size, D))
+    return (bits == 8 ? paged_decode8_workspace : paged_decode_workspace)(B, Hq, Hkv, max_pages, page_size, D);
   return layout_of(bits == 8, B, Hq, Hkv, D).total;
 }
 
 void launch_paged_prefix(const PagedPrefixArgs& a, int bits, hipStream_t st) {
-  if (bits == 8 && a.d.dt == THRIFT_F16) launch<F16, true>(a, st);
+  if (by_itself(bits, a.d.B, a.d.Hkv, a.d.max_pages, a.d.page_size, a.d.D)) {
+    if (bits == 8) launch_paged_decode8(a.d, st);
+    else launch_paged_decode(a.d, st);
+  } else if (bits == 8 && a.d.dt == THRIFT_F16) launch<F16, true>(a, st);
   else if (bits == 8) launch<BF16, true>(a, st);
   else if (a.d.dt == THRIFT_F16) launch<F16, false>(a, st);
   else launch<BF16, false>(a, st);

@@ -86,23 +86,9 @@ struct Space {
   float* part_ml;            // [2*shares][G][2]
 };
 
-// Groups of sequences that start with the same pages
-struct Groups {
-  const int32_t* of;         // [B]
-  const int32_t* lens;       // [n]
-  int n;
-};
-// Tokens in front of sequence b, of length len, that it has in common with its group: whole pages, 0 for none
-__device__ __forceinline__ int common_tokens(const Groups& g, int capacity, int shift, int b, int len) {
-  const int of = g.of[b];
-  if ((unsigned)of >= (unsigned)g.n) return 0;
-  const int n = min(capacity, max(0, g.lens[of])) >> shift << shift;
-  return len >= n ? n : 0;
-}
-
 struct Launch {
   Space w;
-  Groups groups;             // SKIP only: the tokens that sequences of a group have in common are passed over,
+  const int32_t* common;     // SKIP only: [B] tokens in front, whole pages, that are passed over;
   float *own_o, *own_ml;     // a row's part that holds its first step goes here, [B*Hq][D] and [B*Hq][2], instead of to `out` or a slot,
   int2* own_span;            // [B*Hkv] and here the first share with more of the row, and how many there are; slots: [shares][G]
   int G, shift;
@@ -420,9 +406,8 @@ __global__ void __launch_bounds__(64 * waves_of(D), D * NB <= 128 || (C8 && D < 
   auto length = [&](int b) {               // and its skips
     const int n = length_of(a, z, a.seqlens[b]);
     if constexpr (!SKIP) return n;
-    const int common = common_tokens(z.groups, a.max_pages << z.shift, z.shift, b, n);
-    skips = common >> z.shift;
-    return n - common;
+    skips = z.common[b] >> z.shift;
+    return n - (skips << z.shift);
   };
   {
     int n = a.B, per, base = 0, b = 0;

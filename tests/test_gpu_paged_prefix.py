@@ -23,7 +23,7 @@ def T():
 class Batch:
     """Sequences of groups: `of` [B], group_lens in tokens (as given to the call), lens [B].  Pages behind the lengths hold NaN."""
 
-    def __init__(self, of, group_lens, lens, Hkv, D, page, width, dtype, bits, seed=0):
+    def __init__(self, of, group_lens, lens, Hkv, D, page, width, dtype, bits, seed=0, narrow=False):
         self.of, self.group_lens, self.lens, self.bits, self.dtype = of, group_lens, lens, bits, dtype
         g = torch.Generator().manual_seed(seed)
         B = len(of)
@@ -43,6 +43,10 @@ class Batch:
             for j in range(-(-n // page)):
                 live[table[b, j], :min(page, n - j * page)] = True
             table[b, -(-n // page):] = torch.tensor([-1, 2 ** 31 - 1, -2 ** 31, n_pages], dtype=torch.long)[torch.arange(width - -(-n // page)) % 4]
+        if not narrow:
+            # room for more than 128 MB, below which every sequence is read by itself
+            more = -(-(130 << 20) // (B * Hkv * page * D * (4 if bits == 16 else 2)))
+            table = torch.cat([table, torch.full((B, more), -1)], 1)
         self.table = table.to(I32).cuda()
         dead = ~live.cuda()
         kp, vp = (_randn(n_pages, Hkv, page, D, dtype=dtype, seed=seed + i) for i in (0, 1))
@@ -91,10 +95,10 @@ def _mixed(page):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("bits", [16, 8])
 def test_against_64_bits(T, D, Hq, Hkv, dtype, bits):
-    for page in (16, 64, 256):
-        print(f"prefix D={D} Hq={Hq} Hkv={Hkv} page={page} bits={bits} {dtype}", flush=True)
+    for page, narrow in ((16, False), (64, False), (256, False), (32, True)):
+        print(f"prefix D={D} Hq={Hq} Hkv={Hkv} page={page} bits={bits} narrow={narrow} {dtype}", flush=True)
         of, group_lens, lens = _mixed(page)
-        b = Batch(of, group_lens, lens, Hkv, D, page, 13, dtype, bits, seed=page)
+        b = Batch(of, group_lens, lens, Hkv, D, page, 13, dtype, bits, seed=page, narrow=narrow)
         b.check(T, _randn(len(of), Hq, D, dtype=dtype, seed=9))
 
 
@@ -121,6 +125,20 @@ def test_many_groups(T, bits):
     lens = [group_lens[o] + (b * 7) % 30 for b, o in enumerate(of)]
     b = Batch(of, group_lens, lens, 1, D, page, 8, torch.float16, bits, seed=1)
     b.check(T, _randn(B, 2, D, dtype=torch.float16, seed=9))
+
+
+@pytest.mark.parametrize("Hkv,page", [(1, 64), (3, 16)])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_more_tiles_than_workgroups(T, Hkv, page, bits):
+    """Three hundred groups of three, of 600 to 1200 tokens, and one of a hundred: workgroups have several parts of tiles each."""
+    D = 64
+    of = [b % 300 for b in range(900)] + [300] * 100
+    group_lens = [600 + 2 * o for o in range(300)] + [2000]
+    start = [n // page * page for n in group_lens]
+    lens = [start[o] + (b * 7) % 50 for b, o in enumerate(of)]
+    print(f"prefix many tiles Hkv={Hkv} page={page} bits={bits}", flush=True)
+    b = Batch(of, group_lens, lens, Hkv, D, page, -(-2100 // page), torch.bfloat16, bits, seed=1)
+    b.check(T, _randn(1000, 2 * Hkv, D, dtype=torch.bfloat16, seed=9))
 
 
 @pytest.mark.parametrize("bits", [16, 8])
@@ -174,9 +192,10 @@ def test_groups_that_share_nothing(T, bits):
     for group_lens in ([63, 0], [-1, -2 ** 31]):
         b = Batch([0, 1, 0, 1, 1], group_lens, [100, 0, 64, 63, 500], 2, D, page, 9, torch.float16, bits, seed=2)
         b.check(T, _randn(5, 8, D, dtype=torch.float16, seed=7))
-    # and a group whose start is longer than the table is wide: everything there is
-    b = Batch([0, 0, 0], [2 ** 31 - 1], [9 * page, 9 * page, 100], 2, D, page, 9, torch.float16, bits, seed=2)
-    b.check(T, _randn(3, 8, D, dtype=torch.float16, seed=7))
+    # and a group whose start is longer than the table is wide: everything there is, or more than anybody has
+    for narrow in (True, False):
+        b = Batch([0, 0, 0], [2 ** 31 - 1], [9 * page, 9 * page, 100], 2, D, page, 9, torch.float16, bits, seed=2, narrow=narrow)
+        b.check(T, _randn(3, 8, D, dtype=torch.float16, seed=7))
 
 
 @pytest.mark.parametrize("bits", [16, 8])
@@ -217,7 +236,7 @@ def test_streams_workspaces_and_replays(T, bits):
             results.append([one() for _ in range(20)])
     torch.cuda.synchronize()
     assert all(torch.equal(r, want) for rs in results for r in rs)
-    shared = torch.full((T.paged_decode_prefix_workspace_bytes(bits, 5, 8, 2, 2, width, page, D),), 255, dtype=U8, device="cuda")
+    shared = torch.full((T.paged_decode_prefix_workspace_bytes(bits, 5, 8, 2, 2, b.table.shape[1], page, D),), 255, dtype=U8, device="cuda")
     graphs, outs = [], []
     for _ in range(2):
         out = torch.empty(5, 8, D, dtype=torch.float16, device="cuda")
@@ -242,7 +261,7 @@ def test_a_server_whose_requests_share_a_prompt(T, bits):
     """A prompt in whole pages that one sequence holds, requests that start with its pages and go on by themselves: every step's attention is that
     of the cache without groups."""
     B, Hq, Hkv, D, page, dtype = 6, 8, 2, 128, 16, torch.bfloat16
-    table = T.PageTable(B, 40, page, 200, "cuda")
+    table = T.PageTable(B, 2800, page, 200, "cuda")                          # room for more than 128 MB
     cache = (T.PagedKVCache if bits == 16 else T.PagedKVCache8)(table, Hkv, D, dtype)
     freqs, gain = T.rope_frequencies(D, 1e4, device="cuda")
 
