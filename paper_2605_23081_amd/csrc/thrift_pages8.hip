@@ -183,6 +183,23 @@ __global__ void __launch_bounds__(kHeadThreads) paged_append8_items_kernel(Paged
   }
 }
 
+// A workgroup takes as few tokens as still give every thread a head, mostly one, and goes over its heads two or three times.  The kernel is bound by
+// memory, but with 88 registers five wavefronts fit on a SIMD, and workgroups of eight tokens, which turn more heads per formed angle, came to 1.6 rounds
+// of the chip with an idle end (eight / one, us): 72 / 60 for 8192 tokens of 64/8 heads (319 MB, 5.3 TB/s), 147 / 130 for 32768 of 32/8, 13.8 / 11.5 for 8192 of
+// 16/2 heads of 64 channels, 7.2 / 7.8 for 1024 of 32/8.  Reading past the caches takes 57 for the first, but 21 instead of 18 where the heads, 50 MB, were just written.
+HeadShape shape_of(const PagedAppendArgs& a) {
+  const int total = a.Hq + 2 * a.Hkv;
+  HeadShape z = head_shape(a.T, total, a.D, a.rot);
+  int tokens = 1;
+  while (tokens < z.tokens && 2 * z.items * tokens * total <= kHeadThreads) tokens *= 2;
+  z.tokens = tokens;
+  z.lanes = kHeadThreads / (z.items * tokens);
+  if (z.lanes > total) z.lanes = total;
+  const long groups = ((long)a.T + tokens - 1) / tokens, most = (total + z.lanes - 1) / z.lanes, wanted = (2048 + groups - 1) / groups;
+  z.splits = (int)(wanted < most ? wanted : most);
+  return z;
+}
+
 template <typename T>
 void launch_append8(const PagedAppend8Args& args, hipStream_t st) {
   const PagedAppendArgs& a = args.in;
@@ -192,7 +209,7 @@ void launch_append8(const PagedAppend8Args& args, hipStream_t st) {
     paged_append8_kernel<T><<<dim3((unsigned)a.T), dim3(kRowThreads), 0, st>>>(args);
     return;
   }
-  const HeadShape z = head_shape(a.T, a.Hq + 2 * a.Hkv, a.D, a.rot);
+  const HeadShape z = shape_of(a);
   const dim3 grid((unsigned)((a.T + z.tokens - 1) / z.tokens * z.splits)), block(kHeadThreads);
   const bool stream = fills_lines(a.D, a.rot, a.layout);
 #define THRIFT_APPEND8(L_)                                                                    \
