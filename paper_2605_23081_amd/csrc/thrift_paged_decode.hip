@@ -9,6 +9,8 @@ namespace {
 // more, that is less than the search for a share and the second launch.  Shares / rows, us, 32/8 heads of 128 channels: 10.3 / 6.3 for 1 x 256,
 // 10.7 / 5.7 for 16 x 50-100, 12.8 / 10.7 for 16 x 250-500, 54.3 / 54.6 for 256 x 125-500; beyond: 10.3 / 12.5 for 1 x 1000, 15.2 / 17.8 for
 // 16 x 500-1000.  64 channels: 14.0 / 11.5 for 64 x 125-500; 256 channels: 12.5 / 16.2 for 4 x 250-500, 16/16 heads.
+// From codes the same rule, though their rows are half the bytes, since a row's time is then the conversion's: 9.2 / 6.8 for 1 x 256, 9.8 / 5.7 for 16 x 50-100,
+// 12.2 / 11.2 for 16 x 250-500, 20.9 / 18.7 for 64 x 125-250 of 16/16 heads; beyond: 9.6 / 13.4 for 1 x 1000, 15.1 / 17.4 for 16 x 500-1000.
 // With more than four rows per CU the shares are as fast (33.8 / 33.7 for 256 x 63-250) or faster (160 / 226 for 4096 x 15-60).
 constexpr long kRowBytes = 256 << 10, kRowMost = 4 * kCus;
 bool by_rows(int B, int Hq, int Hkv, int max_pages, int page_size, int D) {

@@ -8,11 +8,15 @@
 // tiles and walks blocks of 64 keys:
 //   S = K Q^T      64 keys x 32 rows;  r: a reference of the row, P = 2^(S c - r) <= 2^15
 //   O^T += V^T P^T channels x 32 rows; a lane's part of S is its operand P, without passing through LDS or other lanes
-// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come by LDS DMA, three blocks ahead.  With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
-//   8-bit pages come through registers, two blocks ahead, and are converted on their way to LDS, once for all wavefronts: values and, for bf16 queries, keys times their scales, which bf16
-// holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
-//   P is rounded to 16 bits once, unlike in the walk of own tokens: two pieces would be half as many matrix instructions again, which
-// bound this kernel for large groups.  Sums are those of the unrounded P.
+// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come by LDS DMA into a ring of four blocks (256 channels: two).
+// With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
+//   8-bit pages come through registers and are converted on their way to a ring of two blocks, once for all wavefronts: values and, for bf16 queries, keys
+// times their scales, which bf16 holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
+//   P is rounded to 16 bits once, unlike in the walk of own tokens: two pieces would be half as many matrix instructions again.
+//   What bounds it: for large groups instructions.  64 x 32768 tokens of 64/8 heads are 69 GFLOP, 34 us at the 2.0 PFLOP/s that matrix instructions reach on all
+// CUs; a score's exponential, sum, rounding and maximum next to them cost as much again (a vector instruction beside matrix instructions takes 0.9 ns of a
+// SIMD), so that the walk takes 65, finding the tile's rows and the first blocks 11, the other two launches 30.  One sequence's keys are 134 MB.  For small
+// groups the three launches do.
 //   The reference is the row's largest score so far where that has grown by more than fp16 (or 8 binades, bf16) would hold, so that O is rarely
 // multiplied; for fp16 it lies 7 binades lower, which keeps P normal down to 2^-21 of the largest.  Scores from 2^20 on are rounded before r is
 // taken off, as in the walk: a fused difference would be off by binades.
@@ -27,7 +31,9 @@ namespace {
 
 constexpr int kBlock = 64;                             // keys
 constexpr int kPrefixShares = kCus;
-constexpr int kPriceFull = 3, kPriceHalf = 2;          // of a block for a tile of rows, and for half a one at most
+// What a block costs for a tile of rows, and for half a one at most, where two wavefronts share its keys.  2.2 and 1.5 us from codes, 96 x 16384 tokens: the last
+// part ends after 46 us, with 2 : 1 after 53
+constexpr int kPriceFull = 3, kPriceHalf = 2;
 // Wavefronts of a workgroup.  256 channels: four, with all registers that two have otherwise.
 constexpr int prefix_waves(int D) { return D == 256 ? 4 : 8; }
 constexpr int tile_rows(int D) { return 32 * prefix_waves(D); }
@@ -304,7 +310,8 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
     }
 
   // ---- parts of tiles: a unit is a tile of a KV head, and has as many parts of equal numbers of blocks as its price asks for ----
-  // At most 2.5 per member, KV head and 64 tokens: below 2^32 for the sizes that are taken (B * Hkv * tokens / 32 below 2^30)
+  // At most one per member, KV head and block, and a group has two members at least; with pages of 16 tokens a block may have no more.  Four per member, KV head
+  // and 64 tokens are below 2^32 for the sizes that are taken (B * Hkv * tokens / 32 below 2^30)
   struct Units {
     int full, rest, blocks;                            // full tiles, the price of a block of the other one (0: there is none), blocks
     uint32_t units, price;
@@ -489,7 +496,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
           for (int t = t0; t < t1; ++t) bring(t), ask_for(t);
           return;
         }
-        // One of the two wavefronts of a SIMD goes first: they then are less often at the same kind of instruction (64 x 32768 tokens, 64/8 heads: 88 -> PRIO us)
+        // One of the two wavefronts of a SIMD goes first: they then are less often at the same kind of instruction (64 x 32768 tokens, 64/8 heads: the walk 68 -> 65 us)
         if (!C8 && PARTS == 1 && wave >= 4) __builtin_amdgcn_s_setprio(1);
         typename Rows<T, D, C8, PARTS>::Scores x, y;
         w.scores(x, sh.k[0], scales_of(t0), tokens - t0 * kBlock, c);
@@ -609,8 +616,8 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
             for (int i = 0; i < 16; ++i) w.o[n][i] = w.o[n][i] * k1 + mail[16 * n + i][lane] * k2;
         }
       }
-      // Rows leave through LDS, where each wavefront has a place: lanes hold 16 bytes of 32 rows at a time, memory takes whole rows (64 x 32768 tokens, 64/8 heads: 33 MB of
-      // parts; 16 bytes a row took STORE us longer)
+      // Rows leave through LDS, where each wavefront has a place: lanes hold 16 bytes of 32 rows at a time, memory takes whole rows (2.4 us of
+      // 87 for the 33 MB of parts of 64 x 32768 tokens, 64/8 heads)
       lds_barrier();                                   // nobody reads a block, or another wavefront's part, any more
       if (busy && (PARTS == 1 || part == 0)) {
         int me = lane;                                 // not known to be the lane: places would be formed in front of the walk and kept in registers through it
@@ -765,7 +772,9 @@ void launch(const PagedPrefixArgs& a, hipStream_t st) {
 }  // namespace
 
 // Where the block table has room for less than this altogether, every sequence is walked by itself: what is saved is then no more than what the tiles cost in front of and
-// behind their walks.  Tiles / by itself, us, 32/8 heads of 128 channels: ALONE
+// behind their walks.  Tiles / by itself, us, 32/8 heads of 128 channels where not said: 21.4 / 16.0 for 6 x 2000 tokens (room for 52 MB), 19.7 / 14.2 for 8 x 500 of
+// 16/16 (40), 29.1 / 27.0 for 4 x 8192 (138), 23.9 / 26.4 for 16 x 2000 (139), 20.9 / 27.0 for 32 x 500 of 16/16 (159), 29.6 / 88.7 for 16 x 8192; from codes
+// 31.1 / 14.7 for 6 x 2000.
 constexpr long kAloneBytes = 128L << 20;
 static bool by_itself(int bits, int B, int Hkv, int max_pages, int page_size, int D) {
   return (long)B * Hkv * max_pages * page_size <= kAloneBytes / (bits == 8 ? 2 * (D + 1) : 4 * D);

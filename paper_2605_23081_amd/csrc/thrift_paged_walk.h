@@ -41,7 +41,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 // One workgroup per CU: its four wavefronts have 64 KiB on their way, 16 MiB on the chip.  More of them ask for more than the memory takes at a
 // time, and what waits in front of it is served unevenly (one / two / three per CU: 1220 / 1225 / 1265 us for 16 x 131072 tokens of 32/8 heads,
 // 130 / 132 / 150 for 8 x 16384-32768 of 64/8).
-// Codes are half the bytes: two workgroups per CU have as much on their way.
+// Codes are half the bytes: two workgroups per CU have as much on their way (one / two / three: 62 / 60 / 61 us for 64 x 64-4096 tokens of 16/16 heads).
 constexpr int shares_of(bool codes) { return codes ? 2 * kCus : kCus; }
 
 // scalar loads: the lengths and the table do not change during the launch
