@@ -6,7 +6,7 @@
 //
 // Common tokens.  A tile is at most kTile rows of one group and KV head, a wavefront has 32 of them in the columns of 32 x 32 matrix
 // tiles and walks blocks of 64 keys:
-//   S = K Q^T      64 keys x 32 rows;  r: a reference of the row, P = 2^(S c - r) <= 2^15
+//   S = K Q^T      64 keys x 32 rows;  r: a reference of the row, P = 2^(S c - r)
 //   O^T += V^T P^T channels x 32 rows; a lane's part of S is its operand P, without passing through LDS or other lanes
 // K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come by LDS DMA into a ring of four blocks (256 channels: two).
 // With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
@@ -17,9 +17,9 @@
 // CUs; a score's exponential, sum, rounding and maximum next to them cost as much again (a vector instruction beside matrix instructions takes 0.9 ns of a
 // SIMD), so that the walk takes 65, finding the tile's rows and the first blocks 11, the other two launches 30.  One sequence's keys are 134 MB.  For small
 // groups the three launches do.
-//   The reference is the row's largest score so far where that has grown by more than fp16 (or 8 binades, bf16) would hold, so that O is rarely
-// multiplied; for fp16 it lies 7 binades lower, which keeps P normal down to 2^-21 of the largest.  Scores from 2^20 on are rounded before r is
-// taken off, as in the walk: a fused difference would be off by binades.
+//   The reference is raised where the row's largest score so far has passed it by as much as P may hold (fp16: 2^15, bf16: 1, so that sums of values near the
+// end of its range stay finite), and then lies some binades from that score, so that O is rarely multiplied: 7 below for fp16, which keeps P normal down to
+// 2^-21 of the largest, 8 above for bf16.  Scores from 2^20 on are rounded before r is taken off, as in the walk: a fused difference would be off by binades.
 //   Tiles are cut into parts of equal numbers of blocks on the GPU, so that there is one for every CU: a tile's first part is written to its rows' places, the
 // others to slots.
 #include "thrift_paged_walk.h"
@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t pack16(float x, float y) {
 
 template <typename T> struct Reference;                // how far below the largest score the reference lies, and how far one may pass it
 template <> struct Reference<F16> { static constexpr float kBelow = 7.f, kMost = 15.f; };
-template <> struct Reference<BF16> { static constexpr float kBelow = 0.f, kMost = 8.f; };
+template <> struct Reference<BF16> { static constexpr float kBelow = -8.f, kMost = 0.f; };
 
 constexpr int kMaxSeqs = kMapMaxSeqs, kMaxGroups = kMapMaxSeqs;
 // A group whose common tokens, but for one member's, are fewer than this together is left alone: a part of a tile costs as much in front of and behind its walk as
@@ -239,6 +239,8 @@ struct Rows {
       const float x = fast_exp2(__builtin_fmaf(s[t][e], f, -off)), y = fast_exp2(__builtin_fmaf(s[t][e + 1], f, -off));
       sums[e & 2] += x, sums[(e & 2) + 1] += y;
       p[t][e >> 3][(e & 7) >> 1] = (int)pack16<P>(x, y);
+      // here and not behind the branch on `valid`, to where the compiler takes them otherwise, away from the products
+      asm volatile("" : "+v"(p[t][e >> 3][(e & 7) >> 1]), "+v"(sums[e & 2]), "+v"(sums[(e & 2) + 1]));
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) operand[i] = key(i);

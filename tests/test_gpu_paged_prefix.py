@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests.paged8_util import cache8, prefix64, values64
-from tests.paged_util import check_rounded
+from tests.paged_util import check_rounded, tokens
 from tests.test_gpu_paged import DTYPES, I32, _ints, _randn
 
 pytestmark = pytest.mark.gpu
@@ -284,3 +284,136 @@ def test_a_server_whose_requests_share_a_prompt(T, bits):
         # probabilities of common tokens rounded once, half a step of bf16 of values of at most 6
         assert float((got - want).abs().max()) <= 2.0 ** -8 * 6 and float((lse - wl).abs().max()) <= 2e-5
         assert not torch.equal(got, torch.zeros_like(got))
+
+
+def _with_keys(b, rows):
+    """The batch with every key of token j of its pages replaced by rows(sequence, tokens) in all channels; what is behind the lengths stays NaN."""
+    page = b.values[0].shape[2]
+    k = b.pages[0].clone() if b.bits == 16 else torch.zeros(b.values[0].shape, dtype=b.dtype, device="cuda")
+    for i, n in enumerate(b.lens):
+        held = b.table[i, :-(-n // page)].long()
+        place = torch.arange(len(held) * page, device="cuda")
+        new = rows(i, place).to(b.dtype).view(-1, 1, page, 1).expand(-1, k.shape[1], -1, k.shape[3])
+        k[held] = torch.where((place < n).view(-1, 1, page, 1), new, k[held])
+    if b.bits == 16:
+        b.pages, b.values = (k, b.pages[1]), (k, b.values[1])
+        return b
+    codes = cache8(k, k)[:2]
+    dead = b.pages[1] == 255
+    codes[0][dead], codes[1][dead] = 0x7f, 255
+    b.pages, b.values = (*codes, *b.pages[2:]), (values64(*codes), b.values[1])
+    return b
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("a", [896.0, 1024.0, 2048.0, 4096.0, 28672.0])
+def test_scores_past_24_bits(T, bits, dtype, sign, a):
+    """Scores from 2^23 to 2^33 (in powers of two): keys with the largest one, among the common tokens or a sequence's own, share the weight."""
+    lens, D, Hkv, common = [690, 640, 665, 700], 128, 2, 640
+    b = Batch([0] * 4, [common], lens, Hkv, D, 16, 44, dtype, bits, seed=12)
+    shared = [0, 63, 64, 130, 511, 639]
+    winners = [shared + [641, 689], shared, shared + [664], shared + list(range(640, 680))]
+    low, high = (a / 2, a) if sign > 0 else (-a, -a / 2)
+    _with_keys(b, lambda i, place: torch.where(torch.isin(place, torch.tensor(winners[i], device="cuda")), high, low))
+    q = torch.full((4, 2 * Hkv, D), a, dtype=dtype, device="cuda")
+    out, lse = b.call(T, q, out_dtype=torch.float32, return_lse=True)
+    v = b.values[1]
+    want = torch.stack([tokens(v, b.table[i], n).double()[:, winners[i]].mean(1) for i, n in enumerate(lens)])
+    # the scores are fp32 numbers (a^2 has few bits), so that P is 1 or 0 in either type; at most 46 values are added and parts joined, each partial
+    # sum off by half a step of at most 64 times the largest: 66 U of it
+    top = v[~torch.isnan(v)].double().abs().max()
+    assert bool(((out.view(4, Hkv, 2, D).double() - want.unsqueeze(2)).abs() <= 66 * 2.0 ** -24 * top).all())
+    n = torch.tensor([len(w) for w in winners], dtype=torch.float64, device="cuda")
+    exact = D * a * high / math.sqrt(D) + n.log()
+    assert bool(((lse.double() - exact.unsqueeze(1)).abs() <= 8 * 2.0 ** -24 * exact.abs().unsqueeze(1)).all())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dead", [64, 100, 640])
+def test_scores_of_minus_infinity_weigh_nothing(T, bits, dead):
+    """Keys whose product with the query overflows downwards: the first block of the common tokens, more than it, all of them."""
+    lens, D, Hkv, common = [690, 641, 665, 700], 128, 2, 640
+    b = Batch([0] * 4, [common], lens, Hkv, D, 16, 44, torch.bfloat16, bits, seed=12)
+    _with_keys(b, lambda i, place: torch.where(place < dead, -3e37, (place % 13).float() / 64))
+    q = torch.ones(4, 2 * Hkv, D, dtype=torch.bfloat16, device="cuda")
+    out, lse = b.call(T, q, out_dtype=torch.float32, return_lse=True)
+    for i, n in enumerate(lens):
+        k, v = (tokens(p, b.table[i], n)[:, dead:].double() for p in b.values)
+        s = k.sum(-1) / math.sqrt(D)
+        p = torch.softmax(s, -1)
+        want = (p.unsqueeze(-1) * v).sum(1)
+        # the common tokens' probabilities are rounded to bf16 (2^-8 of each), beside them fp32 sums
+        bound = (2.0 ** -8 + 2.0 ** -14) * (p.unsqueeze(-1) * v.abs()).sum(1) + 2.0 ** -14 * v.abs().amax(1)
+        assert bool(((out[i].view(Hkv, 2, D).double() - want.unsqueeze(1)).abs() <= bound.unsqueeze(1)).all())
+        assert bool(((lse[i].view(Hkv, 2).double() - torch.logsumexp(s, -1).unsqueeze(1)).abs() <= 2.0 ** -14).all())
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_the_largest_values(T, bits):
+    """Values near the end of bfloat16's range, scores that rise a little: a mean of them is one of them, whatever the sums are scaled by in between."""
+    lens, D = [690, 640, 665, 700], 128
+    b = Batch([0] * 4, [640], lens, 2, D, 16, 44, torch.bfloat16, bits, seed=12)
+    _with_keys(b, lambda i, place: torch.floor(place.float() / 100) / 8)
+    if bits == 16:
+        v = b.pages[1]
+        live = ~torch.isnan(v)
+        v[live] = torch.where(v[live] > 0, 1.0, -1.0).to(torch.bfloat16) * 2.0 ** 120
+        b.values = (b.values[0], v)
+    else:
+        codes, scales = (x.clone() for x in b.pages[2:])
+        live = scales != 255
+        scales[live] = 247                                                   # 2^120, codes of 1 and -1
+        codes[live] = (codes[live] & 128) | 0x38
+        b.pages = (*b.pages[:2], codes, scales)
+        b.values = (b.values[0], values64(codes, scales))
+    b.check(T, torch.full((4, 4, D), 0.5, dtype=torch.bfloat16, device="cuda"))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_bad_common_entries_are_clamped(T, dtype, bits):
+    """In common pages and in a sequence's own: the result of the table with its entries clamped to the pages, bit for bit."""
+    b = Batch([0] * 4, [640], [690, 640, 665, 700], 2, 128, 16, 44, dtype, bits, seed=2)
+    pages = [torch.nan_to_num(p, 0.5) if p.dtype == dtype else torch.where(p == 255, 127, p) if p.dim() == 3 else torch.where(p == 0x7f, 0, p) for p in b.pages]
+    n, q = pages[0].shape[0], _randn(4, 8, 128, dtype=dtype, seed=9)
+    for entry, j in ((-1, 0), (n, 7), (-2 ** 31, 21), (2 ** 31 - 1, 39)):
+        b.table[:, j] = entry
+    b.table[0, 41], b.table[3, 43] = -9, n + 3
+    f = T.thrift_paged_decode_prefix if bits == 16 else T.thrift_paged_decode_prefix8
+    got, want = (f(q, *pages, t, _ints(b.lens), _ints(b.of), _ints(b.group_lens), out_dtype=torch.float32, return_lse=True) for t in (b.table, b.table.clamp(0, n - 1)))
+    assert all(torch.equal(x, y) and bool(torch.isfinite(x).all()) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_offsets_past_32_bits(T, bits):
+    """Common pages whose elements lie past 2^31 and whose bytes lie past 2^32."""
+    Hkv, page, D, dtype = 8, 128, 128, torch.bfloat16
+    n_pages = (2 ** 31 + 2 ** 29) // (Hkv * page * D) * (1 if bits == 16 else 2)
+    names = [n_pages - 1, n_pages - 3, 0, n_pages * 4 // 5, 5, n_pages - 2, n_pages - 7]
+    far = torch.tensor(names, device="cuda")
+    some = [_randn(7, Hkv, page, D, dtype=dtype, seed=i) for i in (0, 1)]
+    some = some if bits == 16 else cache8(*some)
+    pages = [torch.empty(n_pages, *p.shape[1:], dtype=p.dtype, device="cuda") for p in some]
+    for p, x in zip(pages, some):
+        p[far] = x
+    few, full = torch.tensor([[0, 1, 2, 3, 4], [0, 1, 2, 3, 5], [0, 1, 2, 3, 6]], dtype=I32, device="cuda"), torch.full((3, 230), -1, dtype=I32, device="cuda")      # room for more than 128 MB
+    full[:, :5] = far[few.long()].to(I32)
+    lens, of, group_lens = _ints([512 + 100, 512, 512 + 128]), _ints([0, 0, 0]), _ints([512])
+    q = _randn(3, 4 * Hkv, D, dtype=dtype, seed=5)
+    f = T.thrift_paged_decode_prefix if bits == 16 else T.thrift_paged_decode_prefix8
+    got = f(q, *pages, full, lens, of, group_lens, out_dtype=torch.float32)
+    del pages
+    few = torch.cat([few, torch.full((3, 225), -1, dtype=I32, device="cuda")], 1)
+    assert torch.equal(got, f(q, *some, few, lens, of, group_lens, out_dtype=torch.float32))
+
+
+def test_the_largest_batch(T):
+    """4096 sequences of one group, and one more is refused."""
+    B, page, D = 4096, 16, 64
+    b = Batch([0] * B, [80], [80 + i % 3 for i in range(B)], 1, D, page, 6, torch.float16, 16, seed=3)
+    q = _randn(B, 1, D, dtype=torch.float16, seed=5)
+    b.check(T, q)
+    with pytest.raises(Exception):
+        T.thrift_paged_decode_prefix(torch.cat([q, q[:1]]), *b.pages, torch.cat([b.table, b.table[:1]]), _ints(b.lens + [80]), _ints([0] * (B + 1)), _ints([80]))
