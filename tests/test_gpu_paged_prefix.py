@@ -417,3 +417,26 @@ def test_the_largest_batch(T):
     b.check(T, q)
     with pytest.raises(Exception):
         T.thrift_paged_decode_prefix(torch.cat([q, q[:1]]), *b.pages, torch.cat([b.table, b.table[:1]]), _ints(b.lens + [80]), _ints([0] * (B + 1)), _ints([80]))
+
+
+def test_the_steps_that_the_readme_shows(T):
+    import os
+    readme = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    code = readme.split("```python\n")[2].split("```")[0]
+    B, Hq, Hkv, D, page, pages, dtype = 4, 8, 2, 128, 16, 40, torch.bfloat16
+    for kind in (T.PagedKVCache, T.PagedKVCache8):
+        table = T.PageTable(B, 2800, page, 100, "cuda")                      # room for more than 128 MB
+        cache = kind(table, Hkv, D, dtype)
+        freqs, gain = T.rope_frequencies(D, 1e4, device="cuda")
+        prompt = _randn(pages * page, 2 * Hkv, D, dtype=dtype)
+        cache.append(prompt[:, :Hkv], prompt[:, Hkv:], table.map(_ints([pages * page, 0, 0, 0]), pages * page), prompt[:, :Hkv].repeat(1, Hq // Hkv, 1), freqs, "half", gain)
+        names = dict(torch=torch, B=B, pages=pages, page_size=page, table=table, cache=cache, freqs=freqs, gain=gain, rows=7, new_lens=_ints([1, 3, 2, 1]),
+                     q=_randn(7, Hq, D, dtype=dtype, seed=1), k=_randn(7, Hkv, D, dtype=dtype, seed=2), v=_randn(7, Hkv, D, dtype=dtype, seed=3), ended=_ints([0, 1, 0, 0]))
+        code_to, code_end = code.split("table.block_table[ended")
+        exec(code_to, names)
+        want = cache.decode(names["q"][names["last"]], out_dtype=torch.float32)
+        # probabilities of common tokens rounded once, half a step of bf16 of values of at most 6, and the output rounded
+        assert float((names["out"].float() - want).abs().max()) <= 2.0 ** -8 * (6 + float(want.abs().max()))
+        assert table.free_count.tolist() == [100 - pages - 4]
+        exec("table.block_table[ended" + code_end, names)
+        assert table.free_count.tolist() == [100 - pages - 3] and table.seqlens.tolist() == [pages * page + 1, 0, pages * page + 2, pages * page + 1]
