@@ -8,14 +8,14 @@
 // tiles and walks blocks of 64 keys:
 //   S = K Q^T      64 keys x 32 rows;  r: a reference of the row, P = 2^(S c - r)
 //   O^T += V^T P^T channels x 32 rows; a lane's part of S is its operand P, without passing through LDS or other lanes
-// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come by LDS DMA into a ring of four blocks (256 channels: two).
+// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come by LDS DMA into a ring of four blocks, two at a time (256 channels: a ring of two).
 // With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
 //   8-bit pages come through registers and are converted on their way to a ring of two blocks, once for all wavefronts: values and, for bf16 queries, keys
 // times their scales, which bf16 holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
 //   P is rounded to 16 bits once, unlike in the walk of own tokens: two pieces would be half as many matrix instructions again.
 //   What bounds it: for large groups instructions.  64 x 32768 tokens of 64/8 heads are 69 GFLOP, 34 us at the 2.0 PFLOP/s that matrix instructions reach on all
 // CUs; a score's exponential, sum, rounding and maximum next to them cost as much again (a vector instruction beside matrix instructions takes 0.9 ns of a
-// SIMD), so that the walk takes 65, finding the tile's rows and the first blocks 11, the other two launches 30.  One sequence's keys are 134 MB.  For small
+// SIMD), so that the walk takes 62, finding the tile's rows and the first blocks 11, the other two launches 30.  One sequence's keys are 134 MB.  For small
 // groups the three launches do.
 //   The reference is raised where the row's largest score so far has passed it by as much as P may hold (fp16: 2^15, bf16: 1, so that sums of values near the
 // end of its range stay finite), and then lies some binades from that score, so that O is rarely multiplied: 7 below for fp16, which keeps P normal down to
@@ -573,21 +573,41 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         };
         auto load_k = [&](int t) { load(a.k_pages, k_off, sh.k[slot(t)], t); };
         auto load_v = [&](int t) { load(a.v_pages, v_off, sh.v[slot(t)], t); };
-        walk(
-            [&]() {
-              load_k(t0);
-              arrive();
-#pragma unroll
-              for (int i = 1; i < kRing; ++i) load_k(t0 + i), load_v(t0 + i - 1);
-              wait(min(kRing - 1, t1 - 1 - t0) + min(kRing - 1, t1 - t0));
-              lds_barrier();
-            },
-            [&](int t) {
-              // asked for behind K of t + 1 and V of t: K of t + 2 .. t + kRing - 1, V of t + 1 .. t + kRing - 2
-              wait(max(0, min(kRing - 2, t1 - 2 - t)) + max(0, min(kRing - 2, t1 - 1 - t)));
-              lds_barrier();
-            },
-            [&](int t) { load_v(t + kRing - 1), load_k(t + kRing); });
+        if constexpr (kRing == 4) {
+          // Two blocks at a time: a wait and a barrier for every second step, with the next two blocks on their way for a step and a half (64 x 32768 tokens, 64/8 heads: 116 us
+          // in all with one for every step, now 113).  Two steps read K of t + 1 and t + 2 and V of t and t + 1; the places of all before are free
+          walk(
+              [&]() {
+                load_k(t0);
+                arrive();
+                load_v(t0), load_k(t0 + 1), load_v(t0 + 1), load_k(t0 + 2);
+                wait(min(2, t1 - 1 - t0) + min(2, t1 - t0));
+                lds_barrier();
+              },
+              [&](int t) {
+                if ((t - t0) & 1) return;
+                wait(0);
+                lds_barrier();
+              },
+              [&](int t) {
+                if ((t - t0) & 1) return;
+                load_v(t + 2), load_k(t + 3), load_v(t + 3), load_k(t + 4);
+              });
+        } else {
+          walk(
+              [&]() {
+                load_k(t0);
+                arrive();
+                load_k(t0 + 1), load_v(t0);
+                wait(min(1, t1 - 1 - t0) + min(1, t1 - t0));
+                lds_barrier();
+              },
+              [&](int t) {
+                wait(0);
+                lds_barrier();
+              },
+              [&](int t) { load_v(t + 1), load_k(t + 2); });
+        }
       }
 
       __builtin_amdgcn_s_setprio(0);
@@ -619,7 +639,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         }
       }
       // Rows leave through LDS, where each wavefront has a place: lanes hold 16 bytes of 32 rows at a time, memory takes whole rows (2.4 us of
-      // 87 for the 33 MB of parts of 64 x 32768 tokens, 64/8 heads)
+      // 84 for the 33 MB of parts of 64 x 32768 tokens, 64/8 heads)
       lds_barrier();                                   // nobody reads a block, or another wavefront's part, any more
       if (busy && (PARTS == 1 || part == 0)) {
         int me = lane;                                 // not known to be the lane: places would be formed in front of the walk and kept in registers through it
