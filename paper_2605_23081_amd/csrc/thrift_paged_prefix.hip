@@ -8,10 +8,9 @@
 // tiles and walks blocks of 64 keys:
 //   S = K Q^T      64 keys x 32 rows;  r: a reference of the row, P = 2^(S c - r)
 //   O^T += V^T P^T channels x 32 rows; a lane's part of S is its operand P, without passing through LDS or other lanes
-// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They come by LDS DMA into a ring of four blocks, two at a time (256 channels: a ring of two).
+// K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They lie in a ring of four blocks, with a barrier for every second one (256 channels: a ring of two), where LDS DMA brings them.
 // With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
-//   8-bit pages come through registers and are converted on their way to a ring of two blocks, once for all wavefronts: values and, for bf16 queries, keys
-// times their scales, which bf16 holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
+//   8-bit pages come through registers and are converted on their way, once for all wavefronts: values and, for bf16 queries, keys times their scales, which bf16 holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
 //   P is rounded to 16 bits once, unlike in the walk of own tokens: two pieces would be half as many matrix instructions again.
 //   What bounds it: for large groups instructions.  64 x 32768 tokens of 64/8 heads are 69 GFLOP, 34 us at the 2.0 PFLOP/s that matrix instructions reach on all
 // CUs; a score's exponential, sum, rounding and maximum next to them cost as much again (a vector instruction beside matrix instructions takes 0.9 ns of a
@@ -81,7 +80,7 @@ struct Tiles {
   static constexpr int kWaves = prefix_waves(D), kThreads = 64 * kWaves, kTile = tile_rows(D);
   static constexpr int kRow = 2 * D;                                        // bytes of a row in LDS
   static constexpr int kSide = kBlock * kRow;                               // bytes of a block of K or V
-  static constexpr int kRing = C8 || D == 256 ? 2 : 4;                      // blocks of K, and of V, in LDS
+  static constexpr int kRing = D == 256 ? 2 : 4;                      // blocks of K, and of V, in LDS
   static constexpr int kChunks = kBlock * D / 8 / kThreads;                 // 16-byte chunks of K, and of V, of a thread
   static constexpr int kRowsOf = 512 / D;                                   // rows of a wavefront's chunk
   static_assert(kChunks * kWaves * kRowsOf == kBlock, "");
@@ -540,20 +539,42 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
           }
         };
         typename L::Block k, v;
-        walk(
-            [&]() {
-              load(k, a.k_pages, a.k_scales, t0), load(v, a.v_pages, a.v_scales, t0);
-              arrive();
-              write_k(k, 0);
-              load(k, a.k_pages, a.k_scales, t0 + 1);
-              lds_barrier();
-            },
-            [&](int t) {
-              write_k(k, slot(t + 1)), write_v(v, slot(t));
-              load(v, a.v_pages, a.v_scales, t + 1), load(k, a.k_pages, a.k_scales, t + 2);
-              lds_barrier();
-            },
-            [](int) {});
+        auto load_k = [&](typename L::Block& x, int t) { load(x, a.k_pages, a.k_scales, t); };
+        auto load_v = [&](typename L::Block& x, int t) { load(x, a.v_pages, a.v_scales, t); };
+        if constexpr (kRing == 4) {
+          // As below, a barrier for every second step (96 x 16384 tokens of 32/8 heads: 73.0 us in all with one for every step, now 72, and fewer spills); a step
+          // writes K of t + 3 and V of t + 2
+          walk(
+              [&]() {
+                typename L::Block k1, v1, k2;
+                load_k(k, t0), load_v(v, t0), load_k(k1, t0 + 1), load_v(v1, t0 + 1), load_k(k2, t0 + 2);
+                arrive();
+                write_k(k, 0), write_v(v, 0), write_k(k1, 1), write_v(v1, 1), write_k(k2, 2);
+                load_v(v, t0 + 2), load_k(k, t0 + 3);
+                lds_barrier();
+              },
+              [&](int t) {
+                if (((t - t0) & 1) == 0) lds_barrier();      // the first of them: K of t0 is read, whose place K of t0 + 4 gets in the next step
+                write_v(v, slot(t + 2)), write_k(k, slot(t + 3));
+                load_v(v, t + 3), load_k(k, t + 4);
+              },
+              [](int) {});
+        } else {
+          walk(
+              [&]() {
+                load_k(k, t0), load_v(v, t0);
+                arrive();
+                write_k(k, 0);
+                load_k(k, t0 + 1);
+                lds_barrier();
+              },
+              [&](int t) {
+                write_k(k, slot(t + 1)), write_v(v, slot(t));
+                load_v(v, t + 1), load_k(k, t + 2);
+                lds_barrier();
+              },
+              [](int) {});
+        }
       } else {
         // LDS is written in the order of the lanes: a lane reads the chunk that belongs in its place
         const int r0 = first_row(0) + my_row;          // first_row(i) is the same but for multiples of eight
