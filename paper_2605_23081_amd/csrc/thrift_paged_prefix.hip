@@ -10,12 +10,13 @@
 //   O^T += V^T P^T channels x 32 rows; a lane's part of S is its operand P, without passing through LDS or other lanes
 // K and V of a block lie in LDS for all wavefronts, V is transposed by the reads.  They lie in a ring of four blocks, with a barrier for every second one (256 channels: a ring of two), where LDS DMA brings them.
 // With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
-//   8-bit pages come through registers and are converted on their way, once for all wavefronts: values and, for bf16 queries, keys times their scales, which bf16 holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
+//   8-bit pages come through registers and are converted on their way, once for all wavefronts: values and, for bf16 queries, keys times their scales,
+// which bf16 holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
 //   P is rounded to 16 bits once, unlike in the walk of own tokens: two pieces would be half as many matrix instructions again.
 //   What bounds it: for large groups instructions.  64 x 32768 tokens of 64/8 heads are 69 GFLOP, 34 us at the 2.0 PFLOP/s that matrix instructions reach on all
 // CUs; a score's exponential, sum, rounding and maximum next to them cost as much again (a vector instruction beside matrix instructions takes 0.9 ns of a
-// SIMD), so that the walk takes 62, finding the tile's rows and the first blocks 11, the other two launches 30.  One sequence's keys are 134 MB.  For small
-// groups the three launches do.
+// SIMD), so that the walk takes 58, what is in front of it and behind 22, the other two launches 30.  The common keys and values are
+// 134 MB, read from memory once, by both tiles of a KV head.  For small groups the three launches do.
 //   The reference is raised where the row's largest score so far has passed it by as much as P may hold (fp16: 2^15, bf16: 1, so that sums of values near the
 // end of its range stay finite), and then lies some binades from that score, so that O is rarely multiplied: 7 below for fp16, which keeps P normal down to
 // 2^-21 of the largest, 8 above for bf16.  Scores from 2^20 on are rounded before r is taken off, as in the walk: a fused difference would be off by binades.

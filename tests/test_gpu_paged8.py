@@ -75,6 +75,13 @@ def test_append_against_64_bits(T, T_, Hq, Hkv, D, rot, page, layout, dtype):
     assert all(bool((p[rest] == 0xab).all()) for p in rows)
 
 
+@pytest.mark.parametrize("T_,Hq,Hkv,D,rot,page", [(2100, 1, 1, 16, 16, 16), (5000, 2, 1, 32, 16, 32), (4097, 1, 2, 64, 64, 64), (1500, 8, 2, 128, 128, 16), (9001, 3, 1, 16, 0, 16), (2049, 4, 4, 256, 128, 16)])
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_append_of_many_tokens(T, T_, Hq, Hkv, D, rot, page, layout):
+    """Workgroups of one token and, where its heads are few, of several."""
+    test_append_against_64_bits(T, T_, Hq, Hkv, D, rot, page, layout, DTYPES[T_ % 2])
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("D", [128, 96])
 def test_the_largest_the_smallest_and_no_numbers(T, dtype, D):
