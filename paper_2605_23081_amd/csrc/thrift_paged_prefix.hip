@@ -491,6 +491,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
       };
       auto slot = [&](int t) { return (unsigned)(t - t0) % kRing; };
       auto scales_of = [&](int t) { return sh.scales[L::kScaled ? slot(t) : 0]; };
+      auto keys_from = [&](int t) { return (int)((unsigned)tokens - (unsigned)t * kBlock); };         // 31 bits are passed behind the last block
       auto walk = [&](auto begin, auto bring, auto ask_for) {
         begin();
         if (t0 == t1) return;
@@ -501,10 +502,10 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         // One of the two wavefronts of a SIMD goes first: they then are less often at the same kind of instruction (64 x 32768 tokens, 64/8 heads: the walk 68 -> 65 us)
         if (!C8 && PARTS == 1 && wave >= 4) __builtin_amdgcn_s_setprio(1);
         typename Rows<T, D, C8, PARTS>::Scores x, y;
-        w.scores(x, sh.k[0], scales_of(t0), tokens - t0 * kBlock, c);
+        w.scores(x, sh.k[0], scales_of(t0), keys_from(t0), c);
         auto step = [&](int t, auto& s, auto& n) {
           bring(t);
-          w.step(s, n, sh.k[slot(t + 1)], scales_of(t + 1), tokens - (t + 1) * kBlock, sh.v[slot(t)], c, [&]() { ask_for(t); });
+          w.step(s, n, sh.k[slot(t + 1)], scales_of(t + 1), keys_from(t + 1), sh.v[slot(t)], c, [&]() { ask_for(t); });
         };
         for (int t = t0; t < t1; t += 2) {
           step(t, x, y);

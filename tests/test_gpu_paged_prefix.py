@@ -440,3 +440,26 @@ def test_the_steps_that_the_readme_shows(T):
         assert table.free_count.tolist() == [100 - pages - 4]
         exec("table.block_table[ended" + code_end, names)
         assert table.free_count.tolist() == [100 - pages - 3] and table.seqlens.tolist() == [pages * page + 1, 0, pages * page + 2, pages * page + 1]
+
+
+@pytest.mark.parametrize("dtype,lens,start", [(torch.bfloat16, [2 ** 31 - 16, 2 ** 31 - 1], 2 ** 31 - 1), (torch.float16, [2 ** 31 - 16 - 15, 2 ** 30 + 77], 2 ** 30)])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_the_longest_block_table(T, dtype, lens, start, bits):
+    """A table of 2^31 - 16 tokens that names four pages over and over, all of it common or half; blocks that end past 2^31."""
+    D, page, width = 64, 16, 2 ** 27 - 1
+    kp = _randn(4, 1, page, D, dtype=dtype)
+    vp = torch.randint(-4, 5, (4, 1, page, D), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(dtype)
+    pages = (kp, vp) if bits == 16 else cache8(kp, vp)
+    table = torch.arange(width, dtype=I32, device="cuda").remainder_(4).expand(2, width).contiguous()
+    print(f"longest prefix {dtype} {lens} {start} {bits}", flush=True)
+    f = T.thrift_paged_decode_prefix if bits == 16 else T.thrift_paged_decode_prefix8
+    # queries of 0 weigh all keys alike: P is a power of two, and sums of 2^23 values, whose means over 64 tokens are below 2, are exact
+    assert float(vp.view(64, D).float().mean(0).abs().max()) < 2
+    out, lse = f(torch.zeros(2, 1, D, dtype=dtype, device="cuda"), *pages, table, _ints(lens), _ints([0, 0]), _ints([start]), out_dtype=torch.float32, return_lse=True)
+    for b, n in enumerate(min(n, width * page) for n in lens):
+        count = torch.tensor([n // 64 + (j < n % 64) for j in range(64)], dtype=torch.float64, device="cuda")
+        want = (count.unsqueeze(1) * vp.view(64, D).double()).sum(0) / n
+        # the parts of 256 tiles, and those of 4 wavefronts and 512 shares of the own tokens: 772 additions each in the sums of values (half a step of at
+        # most 4 n) and of weights
+        assert bool(((out[b, 0].double() - want).abs() <= 4 * (2 * 772 + 4) * 2.0 ** -24).all())
+        assert abs(float(lse[b, 0]) - math.log(n)) <= (772 + 4 * math.log(n)) * 2.0 ** -24
