@@ -561,6 +561,23 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
                 load_v(v, t + 3), load_k(k, t + 4);
               },
               [](int) {});
+        } else if constexpr (L::kScaled) {
+          // One side at a time: K of t + 2 is written inside step t, where K of t is read, and the registers then take V of t + 1.  256 channels, 64 x 32768 tokens of 64/8 heads:
+          // 371 us instead of 563 with fp16 queries, which spill more registers in the walk, but 345 instead of 310 with bf16
+          walk(
+              [&]() {
+                typename L::Block k1;
+                load_k(k, t0), load_k(k1, t0 + 1), load_v(v, t0);
+                arrive();
+                write_k(k, 0), write_k(k1, 1), write_v(v, 0);
+                load_k(k, t0 + 2);
+                lds_barrier();
+              },
+              [&](int t) {
+                if (t != t0) write_v(k, slot(t)), load_k(k, t + 2);
+                lds_barrier();
+              },
+              [&](int t) { write_k(k, slot(t + 2)), load_v(k, t + 1); });
         } else {
           walk(
               [&]() {
