@@ -463,3 +463,47 @@ def test_the_longest_block_table(T, dtype, lens, start, bits):
         # most 4 n) and of weights
         assert bool(((out[b, 0].double() - want).abs() <= 4 * (2 * 772 + 4) * 2.0 ** -24).all())
         assert abs(float(lse[b, 0]) - math.log(n)) <= (772 + 4 * math.log(n)) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_a_captured_step_replayed(T, bits):
+    """Append with the queries rotated in place, attention with and without common starts, and rows read back in one graph; replayed with other tokens, slots,
+    lengths and groups, each replay against the same calls made one by one on another cache."""
+    B, Hq, Hkv, D, page, width, dtype = 5, 8, 2, 128, 16, 2800, torch.float16
+    n_pages = 300
+    shapes = [(n_pages, Hkv, page, D)] * 2 if bits == 16 else [(n_pages, Hkv, page, D), (n_pages, Hkv, page)] * 2
+    caches = [[torch.zeros(s, dtype=dtype if bits == 16 else U8, device="cuda") for s in shapes] for _ in range(2)]
+    append, decode, prefix, read = (T.thrift_paged_append, T.thrift_paged_decode, T.thrift_paged_decode_prefix, T.thrift_paged_read) if bits == 16 else \
+        (T.thrift_paged_append8, T.thrift_paged_decode8, T.thrift_paged_decode_prefix8, T.thrift_paged_read8)
+    table = torch.full((B, width), -1, dtype=I32)
+    table[:, :40] = torch.arange(40)
+    table[:, 40:80] = 40 + torch.arange(B * 40).view(B, 40)
+    table = table.cuda()
+    lens, of, group_lens, slots, positions = _ints([1] * B), _ints([0] * B), _ints([640]), _ints([-1] * 80), _ints([0] * 80)
+    q, k, v = (torch.zeros(80, h, D, dtype=dtype, device="cuda") for h in (Hq, Hkv, Hkv))
+    freqs, gain = T.rope_frequencies(D, 1e4, device="cuda")
+    more = {} if bits == 16 else dict(dtype=dtype)
+
+    def step(cache, q):
+        append(k, v, slots, *cache, q=q, q_out=q, positions=positions, freqs=freqs, gain=gain)
+        return [q, decode(q[:B], *cache, table, lens), *prefix(q[:B], *cache, table, lens, of, group_lens, return_lse=True), *read(*cache, table, lens, 48, first=positions[:B], **more)]
+
+    step(caches[0], q), step(caches[1], q.clone())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step(caches[0], q)
+    names = torch.arange(n_pages * page)
+    for i, (n, groups, start) in enumerate((([690, 641, 700, 640, 655], [0] * 5, 640), ([700, 0, 1, 640, 1200], [0, 0, 0, 0, -1], 320), ([1280] * 5, [0, 0, 0, -1, -1], 500), ([3] * 5, [0] * 5, 640))):
+        g = torch.Generator().manual_seed(i)
+        q.copy_(_randn(80, Hq, D, dtype=dtype, seed=3 * i)), k.copy_(_randn(80, Hkv, D, dtype=dtype, seed=3 * i + 1)), v.copy_(_randn(80, Hkv, D, dtype=dtype, seed=3 * i + 2))
+        slots.copy_(names[torch.randperm(240 * page, generator=g)[:80]].to(I32).cuda()), positions.copy_(torch.randint(0, 5000, (80,), generator=g).to(I32).cuda())
+        slots[7::9] = -1
+        lens.copy_(_ints(n)), of.copy_(_ints(groups)), group_lens.copy_(_ints([start]))
+        want = [x.clone() for x in step(caches[1], q.clone())]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for j, (x, y) in enumerate(zip(outs, want)):
+            assert torch.equal(x, y), (i, j)
+        assert all(torch.equal(x, y) for x, y in zip(*caches))
