@@ -121,7 +121,7 @@ class _General:
     def decode(*_):
         return None
 
-    append = attention = rope = page_map = paged_append = paged_decode = paged_append8 = paged_decode8 = paged_decode_prefix = paged_decode_prefix8 = decode
+    append = attention = rope = page_map = paged_append = paged_decode = paged_append8 = paged_decode8 = paged_decode_prefix = paged_decode_prefix8 = paged_read = paged_read8 = decode
 
 
 def _native():
@@ -732,6 +732,9 @@ def _paged_read(name: str, pages, block_table, seqlens, N: int, dtype, first, k_
 def thrift_paged_read(k_pages, v_pages, block_table, seqlens, N: int, first: Optional[torch.Tensor] = None,
                       k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Tokens first[b] .. first[b] + N - 1 (default: from 0) of every sequence as rows (k, v) [B,Hkv,N,D]; 0 past the lengths."""
+    r = (_call or _native()).paged_read(k_pages, v_pages, block_table, seqlens, N, first, k_out, v_out, *_here_now())
+    if r is not None:
+        return _result(r, "thrift_paged_read")
     _pages(k_pages, v_pages)
     return _paged_read("thrift_paged_read", (k_pages, v_pages), block_table, seqlens, N, k_pages.dtype, first, k_out, v_out)
 
@@ -740,6 +743,9 @@ def thrift_paged_read8(k_codes, k_scales, v_codes, v_scales, block_table, seqlen
                        first: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
                        v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """thrift_paged_read of the 8-bit cache, in dtype."""
+    r = (_call or _native()).paged_read8(k_codes, k_scales, v_codes, v_scales, block_table, seqlens, N, first, k_out, v_out, _DT.get(dtype, F32), *_here_now())
+    if r is not None:
+        return _result(r, "thrift_paged_read8")
     _pages8(k_codes, k_scales, v_codes, v_scales)
     assert dtype in (torch.float16, torch.bfloat16), dtype
     return _paged_read("thrift_paged_read8", (k_codes, k_scales, v_codes, v_scales), block_table, seqlens, N, dtype, first, k_out, v_out, _DT[dtype])

@@ -426,6 +426,53 @@ PyObject* paged_decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return both;
 }
 
+// paged_read(k_pages, v_pages, block_table, seqlens, n, first, k_out, v_out, device, stream): (k, v)
+// CODES: k_codes, k_scales, v_codes, v_scales for the pages, and the type of the rows (a thrift_dtype) behind v_out
+template <bool CODES>
+PyObject* paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  constexpr int kPages = CODES ? 4 : 2;
+  const Tensor *p[4] = {}, *table, *lens, *first, *given[2];
+  int N, device, code = 0;
+  void* stream;
+  thrift_dtype dt;
+  if (n != kPages + 8 + (CODES ? 1 : 0)) Py_RETURN_NONE;
+  PyObject* const* b = a + kPages;         // behind the pages
+  PyObject* const* c = b + 6 + (CODES ? 1 : 0);                  // device, stream
+  if (!integer(c[0], &device) || !(CODES ? pages8(a, device, p) && integer(b[6], &code) : pages(a[0], a[1], device, &p[0], &p[1], &dt)) ||
+      !plain(b[0], device, &table) || !plain(b[1], device, &lens) || !integer(b[2], &N) || !plain_or_none(b[3], device, &first) ||
+      !plain_or_none(b[4], device, &given[0]) || !plain_or_none(b[5], device, &given[1]) || !stream_of(c[1], &stream) || table->dim() != 2)
+    Py_RETURN_NONE;
+  if (CODES) {
+    if (code != THRIFT_F16 && code != THRIFT_BF16) Py_RETURN_NONE;
+    dt = (thrift_dtype)code;
+  }
+  const int64_t B = table->size(0), width = table->size(1), Hkv = p[0]->size(1), D = p[0]->size(3);
+  const at::ScalarType type = dt == THRIFT_F16 ? at::kHalf : at::kBFloat16;
+  if (N < 1 || B < 1 || B > 0x7fffffff || width > 0x7fffffff || !is(*table, at::kInt, {B, width}) || !is(*lens, at::kInt, {B}) ||
+      (first && !is(*first, at::kInt, {B})))
+    Py_RETURN_NONE;
+  for (const Tensor* t : given)
+    if (t && !is(*t, type, {B, Hkv, N, D})) Py_RETURN_NONE;
+  Tensor out[2];
+  for (int i = 0; i < 2; ++i) out[i] = given[i] ? *given[i] : at::empty({B, Hkv, N, D}, table->options().dtype(type));
+  thrift_status r;
+  {
+    const Unlocked unlocked;
+    const int32_t *t = ptr_as<int32_t>(table), *f = ptr_as<int32_t>(first), *l = ptr_as<int32_t>(lens);
+    const int n_pages = (int)p[0]->size(0), page = (int)p[0]->size(2), nb = (int)B, h = (int)Hkv, m = (int)width, d = (int)D;
+    if constexpr (CODES)
+      r = thrift_paged_read8(ptr_as<uint8_t>(p[0]), ptr_as<uint8_t>(p[1]), ptr_as<uint8_t>(p[2]), ptr_as<uint8_t>(p[3]), n_pages, t, m, f, l, nb, h, N, d, page,
+                             out[0].data_ptr(), out[1].data_ptr(), dt, stream);
+    else
+      r = thrift_paged_read(ptr(p[0]), ptr(p[1]), n_pages, t, m, f, l, nb, h, N, d, page, out[0].data_ptr(), out[1].data_ptr(), stream);
+  }
+  if (r != THRIFT_OK) return PyLong_FromLong((long)r);
+  PyObject* both = PyTuple_New(2);
+  if (both == nullptr) return nullptr;
+  for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, THPVariable_Wrap(out[i]));
+  return both;
+}
+
 // A tensor whose sizes or storage cannot be asked for (a fake one, one under a transform) throws: not a plain argument.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
@@ -449,6 +496,8 @@ PyMethodDef methods[] = {
     {"paged_decode8", (PyCFunction)(void (*)(void))guarded<paged_decode<true, false>>, METH_FASTCALL, nullptr},
     {"paged_decode_prefix", (PyCFunction)(void (*)(void))guarded<paged_decode<false, true>>, METH_FASTCALL, nullptr},
     {"paged_decode_prefix8", (PyCFunction)(void (*)(void))guarded<paged_decode<true, true>>, METH_FASTCALL, nullptr},
+    {"paged_read", (PyCFunction)(void (*)(void))guarded<paged_read<false>>, METH_FASTCALL, nullptr},
+    {"paged_read8", (PyCFunction)(void (*)(void))guarded<paged_read<true>>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

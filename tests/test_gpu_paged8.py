@@ -441,3 +441,28 @@ def test_the_module_leaves_other_arguments_to_the_general_path(T):
         wide = torch.zeros(3, 100, dtype=I32, device="cuda")
         assert one(table=wide, ws=torch.empty(16, dtype=U8, device="cuda")) == 5
     assert all(f() is None for f in (m.paged_append8, m.paged_decode8, m.paged_decode_prefix, m.paged_decode_prefix8))
+
+
+def test_the_module_leaves_other_reads_to_the_general_path(T, monkeypatch):
+    m = T._native()
+    table, lens = _ints([[0, 1], [2, 3], [3, 0]]), _ints([20, 3, 0])
+    p8, p16 = _pages8(4, 2, 16, 128, 0x38), [_randn(4, 2, 16, 128, dtype=torch.bfloat16, seed=i) for i in (1, 2)]
+    out = torch.zeros(3, 2, 24, 128, dtype=torch.bfloat16, device="cuda")
+    for f, pages in ((m.paged_read, p16), (m.paged_read8, p8)):
+        last = dict(dt=T.BF16) if len(pages) == 4 else {}
+        one = lambda **kw: f(*{**dict({f"p{i}": x for i, x in enumerate(pages)}, table=table, lens=lens, n=24, first=None, ko=None, vo=None, **last, device=0, stream=0), **kw}.values())
+        k, v = one()
+        assert k.shape == v.shape == out.shape and one(ko=out)[0].data_ptr() == out.data_ptr()
+        for bad in (dict(device=1), dict(table=table[:2]), dict(table=lens), dict(lens=lens.long()), dict(n=0), dict(n=-3), dict(n=2 ** 40), dict(n=24.0), dict(first=lens[:2]), dict(ko=out[:2]),
+                    dict(vo=out.float()), dict(ko=out.half()), dict(vo=out.transpose(0, 1)), dict(p0=pages[0][:, :1]), dict(p1=pages[1].cpu()), dict(n=2 ** 31 - 1, table=table.expand(3, 2)[:0]),
+                    *([dict(dt=T.F32), dict(dt=7), dict(p1=pages[0])] if last else [dict(p0=pages[0].float())])):
+            assert one(**bad) is None, bad
+        assert f() is None
+    assert m.paged_read(*p16, table, lens, 1 << 22, None, out, out, 0, 0) is None
+    with pytest.raises(T.ThriftError):
+        T.thrift_paged_read(torch.zeros(4, 2, 20, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(4, 2, 20, 128, dtype=torch.bfloat16, device="cuda"), table, lens, 24)
+    calls = lambda: [*T.thrift_paged_read(*p16, table, lens, 24, first=_ints([0, 2, -5])), *T.thrift_paged_read8(*p8, table, lens, 7, torch.float16),
+                     *T.thrift_paged_read8(*p8, table, lens, 24, k_out=out.clone())]
+    want = calls()
+    monkeypatch.setattr(T, "_call", T._General)
+    assert all(torch.equal(x, y) for x, y in zip(calls(), want))
