@@ -462,8 +462,9 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         const unsigned key = (unsigned)t * kBlock + first_row(i);
         return C8 || key < (unsigned)tokens ? key : (unsigned)t * kBlock + first_row(i) % 16;
       };
-      // A lane has the place of one chunk of one block in the pages, from block place_t on (which moves on with K: V of a block is asked for in front of K
-      // of the next): no scalar loads in the walk, whose results would be waited for with the reads of LDS, and few scalar instructions
+      // A lane has the place of one chunk of one block in the pages, from block place_t on: no scalar loads in the walk, whose results would be waited for with the
+      // reads of LDS, and few scalar instructions.  The window moves on with K of a block t and then begins at t - 1: the forms ask for V of t - 1 in front of K of t, or
+      // behind it where a side at a time is on its way, and never for an earlier block
       constexpr int kPlaces = 64 / L::kChunks;
       const int32_t* table = a.table + (size_t)__builtin_amdgcn_readfirstlane(sh.list[0]) * a.max_pages;
       size_t place;
@@ -475,7 +476,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         place = ((((size_t)p * a.Hkv + hk) << shift) + (key & ((1u << shift) - 1))) * (C8 ? 1 : L::kRow);
       };
       auto place_of = [&](int t, int i) {              // bytes, or rows of codes
-        if (t >= place_t + kPlaces) look_up(t);
+        if (t >= place_t + kPlaces) look_up(t - 1);
         const int at = (t - place_t) * L::kChunks + i;
         return (size_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)place, at) | (size_t)(uint32_t)__builtin_amdgcn_readlane((int)(place >> 32), at) << 32;
       };

@@ -1,0 +1,62 @@
+"""Attention over common starts whose tiles are cut into long parts, every page a different one, against 64 bits."""
+import math
+
+import pytest
+import torch
+
+from tests.paged8_util import cache8, prefix64, values64
+from tests.paged_util import check_rounded
+from tests.test_gpu_paged import DTYPES, I32, _ints, _randn
+from tests.test_gpu_paged_prefix import T  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+SHARES = 256                              # parts that all tiles are cut into
+HKV = 64                                  # KV heads: with one tile each, a part has a quarter of a head's blocks
+
+
+def _problem(D, G, blocks, dtype, bits, members=3):
+    """Sequences of one group of 64 KV heads.  Where a head is one tile, its blocks of 64 tokens come in four parts of `blocks` each (the last one lacks a page);
+    where it is two, in two parts and one, or more."""
+    page = 16
+    start = 64 * blocks * SHARES // HKV - page                                # the last block lacks a page
+    shared = start // page
+    own = [0, 1, 40] + [page] * (members - 3)
+    lens = [start + n for n in own]
+    g = torch.Generator().manual_seed(D + blocks)
+    n_pages = shared + 3 * members + 1
+    names = torch.randperm(n_pages, generator=g)
+    # room for more than 128 MB, below which every sequence is read by itself
+    table = torch.full((members, shared + 3 + (130 << 20) // (members * HKV * page * D * 2)), -1, dtype=I32)
+    table[:, :shared] = names[:shared]
+    for b in range(members):
+        table[b, shared:shared + 3] = names[shared + 3 * b:shared + 3 * b + 3]
+    kp, vp = (_randn(n_pages, HKV, page, D, dtype=dtype, seed=i) for i in (0, 1))
+    # queries of which some hundred tokens have most of the weight: a block of other tokens in the place of one is seen in most rows
+    q = (_randn(members, HKV * G, D, dtype=torch.float32, seed=9) * 2.5).to(dtype)
+    if bits == 16:
+        pages, values = (kp, vp), (kp, vp)
+    else:
+        vp.mul_((2 * _randn(n_pages, HKV, page, 1, dtype=dtype, seed=6)).exp())
+        pages = cache8(kp, vp)
+        values = values64(*pages[:2]), values64(*pages[2:])
+    return q, pages, values, table.cuda(), lens, start
+
+
+# 4 x 3 rows of a tile: wavefronts take half a block's keys each; 32 x 5: whole blocks (256 channels: one tile of 128 rows with whole blocks, one of 32 with halves)
+@pytest.mark.parametrize("D,blocks", [(D, n) for D in (64, 128, 256) for n in (9, 17, 33, 65)] + [(64, 129)])
+@pytest.mark.parametrize("G,members", [(4, 3), (32, 5)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [16, 8])
+def test_long_parts(T, D, blocks, G, members, dtype, bits):  # noqa: F811
+    print(f"prefix parts D={D} blocks={blocks} G={G} members={members} bits={bits} {dtype}", flush=True)
+    q, pages, values, table, lens, start = _problem(D, G, blocks, dtype, bits, members)
+    f = T.thrift_paged_decode_prefix if bits == 16 else T.thrift_paged_decode_prefix8
+    got, lse = f(q, *pages, table, _ints(lens), _ints([0] * members), _ints([start]), out_dtype=torch.float32, return_lse=True)
+    # some KV heads in 64 bits: the first, the last and two between
+    heads = [0, 21, 42, HKV - 1]
+    rows = [h * G + i for h in heads for i in range(G)]
+    few = [p[:, heads].contiguous() for p in values]
+    want, wl, eo, el = prefix64(q[:, rows].contiguous(), *few, table, lens, [start] * members, 1 / math.sqrt(D), dtype if bits == 16 else torch.bfloat16)
+    check_rounded(got[:, rows], want, eo)
+    assert bool(((lse[:, rows].double() - wl).abs() <= el).all())
