@@ -111,6 +111,13 @@ struct Tiles {
   };
 };
 
+// The lane's number, formed where it stands
+__device__ __forceinline__ int lane_here() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+  return x;
+}
+
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
 // One tile's rows in a wavefront: 32 of them.
@@ -184,11 +191,13 @@ struct Rows {
         }
     }
     if (valid < kBlock) {
+      // The lane's number is asked for here, and the rest are constants: keys of registers, or what they start from, would be formed in front of the walk and kept through it
+      const int there = valid - 32 * part - 4 * (lane_here() >> 5);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (32 * (part + t) + 8 * (i >> 2) + 4 * half + (i & 3) >= valid) n[t][i] = -__builtin_inff();
+          if (32 * t + 8 * (i >> 2) + (i & 3) >= there) n[t][i] = -__builtin_inff();
     }
   }
 
@@ -525,21 +534,23 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
             x.codes[i] = __builtin_amdgcn_raw_buffer_load_b64(codes, 8 * lane, 0, 0), x.scales[i] = __builtin_amdgcn_raw_buffer_load_b8(bytes, my_row, 0, 0);
           }
         };
+        // rows of a thread's chunks are the same but for multiples of eight, and so are their places in a row
+        constexpr int kApart = kWaves * L::kRowsOf;
+        static_assert(L::kChunks == 1 || kApart % 8 == 0, "");
+        const int r0 = first_row(0) + my_row;
+        const uint32_t k_off = r0 * L::kRow + 16 * (my_chunk ^ (r0 & 7)), v_off = r0 * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r0));
         auto write_k = [&](const typename L::Block& x, int s) {
 #pragma unroll
           for (int i = 0; i < L::kChunks; ++i) {
-            const int r = first_row(i) + my_row;
-            *reinterpret_cast<v4i*>(sh.k[s] + r * L::kRow + 16 * (my_chunk ^ (r & 7))) = widen_chunk<T>(x.codes[i], L::kScaled ? 1.f : scale_of(x.scales[i]));
+            *reinterpret_cast<v4i*>(sh.k[s] + k_off + i * kApart * L::kRow) = widen_chunk<T>(x.codes[i], L::kScaled ? 1.f : scale_of(x.scales[i]));
             if constexpr (L::kScaled)
-              if (my_chunk == 0) sh.scales[s][r] = scale_of(x.scales[i]);
+              if (my_chunk == 0) sh.scales[s][r0 + i * kApart] = scale_of(x.scales[i]);
           }
         };
         auto write_v = [&](const typename L::Block& x, int s) {
 #pragma unroll
-          for (int i = 0; i < L::kChunks; ++i) {
-            const int r = first_row(i) + my_row;
-            *reinterpret_cast<v4i*>(sh.v[s] + r * L::kRow + ((16u * my_chunk) ^ Rows<T, D, C8, 1>::v_swizzle(r))) = widen_chunk<BF16>(x.codes[i], scale_of(x.scales[i]));
-          }
+          for (int i = 0; i < L::kChunks; ++i)
+            *reinterpret_cast<v4i*>(sh.v[s] + v_off + i * kApart * L::kRow) = widen_chunk<BF16>(x.codes[i], scale_of(x.scales[i]));
         };
         typename L::Block k, v;
         auto load_k = [&](typename L::Block& x, int t) { load(x, a.k_pages, a.k_scales, t); };
@@ -564,7 +575,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
               [](int) {});
         } else if constexpr (L::kScaled) {
           // One side at a time: K of t + 2 is written inside step t, where K of t is read, and the registers then take V of t + 1.  256 channels, 64 x 32768 tokens of 64/8 heads:
-          // 371 us instead of 563 with fp16 queries, which spill more registers in the walk, but 345 instead of 310 with bf16
+          // 318 us instead of 334 with fp16 queries, which spill registers with both sides on their way, but 321 instead of 305 with bf16
           walk(
               [&]() {
                 typename L::Block k1;

@@ -123,8 +123,8 @@ struct Walk {
   static constexpr int kRun = C8 ? VC : VC < 8 ? VC : 8;         // neighbouring channels of a lane
   static constexpr int NR = NB * (VC * 4 + 2);                   // registers of a state
   // the next row's queries are on their way during a step; 32 heads of 256 channels have no registers for that: with it they
-  // take 161 us for 64 x 2048-4096 tokens of 64/2 heads, without it 83-90.  They are still short of 26 registers per lane, some of which are
-  // reloaded inside the walk; no other form uses scratch memory.
+  // take 161 us for 64 x 2048-4096 tokens of 64/2 heads, without it 83-90.  They are still short of 26 registers per lane (of 20
+  // behind common starts), some of which are reloaded inside the walk; no other form uses scratch memory.
   static constexpr bool kQueryAhead = NB * D < 512;
   static constexpr int kStream = 2;        // non-temporal: keys and values are read once
   int lane, col, grp;
