@@ -551,9 +551,8 @@ size_t thrift_paged_decode_prefix_workspace(int bits, int B, int Hq, int Hkv, in
 
 /*
  * Attention of one new token per sequence where sequences start with the same pages: thrift_paged_decode, with the keys and values of a common
- * start read once for all of its sequences.  The result is that of thrift_paged_decode but for the order of its fp32 sums, and for the
- * probabilities of the common tokens, which are rounded to 16 bits (dt's; bf16 over the 8-bit cache) for the product with the values.  Over the 8-bit cache,
- * common values past bf16's largest number, 3.39e38, count as infinite, and so do common keys for bf16 queries.
+ * start read once for all of its sequences.  The result is that of thrift_paged_decode but for the order of its fp32 sums.  Over the
+ * 8-bit cache, common values past bf16's largest number, 3.39e38, count as infinite, and so do common keys for bf16 queries.
  *   group_of [B] int32: the group of each sequence, any order; a number outside 0 .. n_groups - 1: none
  *   group_lens [n_groups] int32: tokens in front that the sequences of a group have in the same pages, rounded down to whole pages, at most
  *     max_pages * page_size.  They are read through the block table of one of them.  A sequence shorter than that, or of no group, is read

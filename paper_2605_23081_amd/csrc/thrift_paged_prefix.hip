@@ -12,11 +12,11 @@
 // With at most half a tile of rows, wavefronts take half a block's keys each, two to a row.
 //   8-bit pages come through registers and are converted on their way, once for all wavefronts: values and, for bf16 queries, keys times their scales,
 // which bf16 holds exactly; for fp16 queries keys without, and the scales, in LDS too, are factors of the scores.
-//   P is rounded to 16 bits once, unlike in the walk of own tokens: two pieces would be half as many matrix instructions again.
-//   What bounds it: for large groups instructions.  64 x 32768 tokens of 64/8 heads are 69 GFLOP, 34 us at the 2.0 PFLOP/s that matrix instructions reach on all
-// CUs; a score's exponential, sum, rounding and maximum next to them cost as much again (a vector instruction beside matrix instructions takes 0.9 ns of a
-// SIMD), so that the walk takes 58, what is in front of it and behind 22, the other two launches 30.  The common keys and values are
-// 134 MB, read from memory once, by both tiles of a KV head.  For small groups the three launches do.
+//   P is two 16-bit pieces, high and low, for two products, as in the walk of own tokens: what a result holds does not depend on which tokens are common.  Rounded once, results were
+// off by 1.1e-3 of their norm (bf16; 1.5e-4 fp16) and 64 x 32768 tokens of 64/8 heads took 107 us instead of 134.  The pieces take the registers of their scores.
+//   What bounds it: for large groups instructions.  64 x 32768 tokens of 64/8 heads are 103 GFLOP with the second piece, 52 us at the 2.0 PFLOP/s that matrix instructions reach on all
+// CUs; a score's exponential, sum, two roundings and maximum next to them cost as much again (a vector instruction beside matrix instructions takes 0.9 ns of a
+// SIMD).  The common keys and values are 134 MB, read from memory once, by both tiles of a KV head.  For small groups the three launches do.
 //   The reference is raised where the row's largest score so far has passed it by as much as P may hold (fp16: 2^15, bf16: 1, so that sums of values near the
 // end of its range stay finite), and then lies some binades from that score, so that O is rarely multiplied: 7 below for fp16, which keeps P normal down to
 // 2^-21 of the largest, 8 above for bf16.  Scores from 2^20 on are rounded before r is taken off, as in the walk: a fused difference would be off by binades.
@@ -31,8 +31,8 @@ namespace {
 
 constexpr int kBlock = 64;                             // keys
 constexpr int kPrefixShares = kCus;
-// What a block costs for a tile of rows, and for half a one at most, where two wavefronts share its keys.  2.2 and 1.5 us from codes, 96 x 16384 tokens: the last
-// part ends after 46 us, with 2 : 1 after 53
+// What a block costs for a tile of rows, and for half a one at most, where two wavefronts share its keys.  From codes, 96 x 16384 tokens: 79.5 us in all, with 2 : 1
+// 83, with 5 : 3 79
 constexpr int kPriceFull = 3, kPriceHalf = 2;
 // Wavefronts of a workgroup.  256 channels: four, with all registers that two have otherwise.
 constexpr int prefix_waves(int D) { return D == 256 ? 4 : 8; }
@@ -240,16 +240,18 @@ struct Rows {
     };
     const KeyReader key = keys_in(k);
     v8s operand[kAhead + 1];
-    v4i p[NT][2];
+    v4i p[NT][2], low[NT][2];
     float sums[4] = {0.f, 0.f, 0.f, 0.f};
     // elements 2 i and 2 i + 1 of the lane's P
     auto pair = [&](int i) {
       const int t = i >> 3, e = 2 * i & 15;
       const float x = fast_exp2(__builtin_fmaf(s[t][e], f, -off)), y = fast_exp2(__builtin_fmaf(s[t][e + 1], f, -off));
       sums[e & 2] += x, sums[(e & 2) + 1] += y;
-      p[t][e >> 3][(e & 7) >> 1] = (int)pack16<P>(x, y);
+      const uint32_t high = pack16<P>(x, y);
+      p[t][e >> 3][(e & 7) >> 1] = (int)high;
+      low[t][e >> 3][(e & 7) >> 1] = (int)pack16<P>(x - P::to_float((uint16_t)high), y - P::to_float((uint16_t)(high >> 16)));
       // here and not behind the branch on `valid`, to where the compiler takes them otherwise, away from the products
-      asm volatile("" : "+v"(p[t][e >> 3][(e & 7) >> 1]), "+v"(sums[e & 2]), "+v"(sums[(e & 2) + 1]));
+      asm volatile("" : "+v"(p[t][e >> 3][(e & 7) >> 1]), "+v"(low[t][e >> 3][(e & 7) >> 1]), "+v"(sums[e & 2]), "+v"(sums[(e & 2) + 1]));
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) operand[i] = key(i);
@@ -270,7 +272,9 @@ struct Rows {
 #pragma unroll
     for (int i = 0; i < kValues; ++i) {
       const int tu = i / (D / 32), tile = i % (D / 32), at = i % (kAhead + 1);
-      o[tile] = P::mfma(__builtin_shufflevector(value[at][0], value[at][1], 0, 1, 2, 3, 4, 5, 6, 7), __builtin_bit_cast(v8s, p[tu >> 1][tu & 1]), o[tile]);
+      const v8s channels = __builtin_shufflevector(value[at][0], value[at][1], 0, 1, 2, 3, 4, 5, 6, 7);
+      o[tile] = P::mfma(channels, __builtin_bit_cast(v8s, p[tu >> 1][tu & 1]), o[tile]);
+      o[tile] = P::mfma(channels, __builtin_bit_cast(v8s, low[tu >> 1][tu & 1]), o[tile]);
       if (i + kAhead < kValues) read_value(i + kAhead);
 #pragma unroll
       for (int x = 16 * NT * i / kValues; x < 16 * NT * (i + 1) / kValues; ++x) most = fmaxf(most, n[x >> 4][x & 15]);
@@ -509,8 +513,6 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
           for (int t = t0; t < t1; ++t) bring(t), ask_for(t);
           return;
         }
-        // One of the two wavefronts of a SIMD goes first: they then are less often at the same kind of instruction (64 x 32768 tokens, 64/8 heads: the walk 68 -> 65 us)
-        if (!C8 && PARTS == 1 && wave >= 4) __builtin_amdgcn_s_setprio(1);
         typename Rows<T, D, C8, PARTS>::Scores x, y;
         w.scores(x, sh.k[0], scales_of(t0), keys_from(t0), c);
         auto step = [&](int t, auto& s, auto& n) {
@@ -556,7 +558,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         auto load_k = [&](typename L::Block& x, int t) { load(x, a.k_pages, a.k_scales, t); };
         auto load_v = [&](typename L::Block& x, int t) { load(x, a.v_pages, a.v_scales, t); };
         if constexpr (kRing == 4) {
-          // As below, a barrier for every second step (96 x 16384 tokens of 32/8 heads: 73.0 us in all with one for every step, now 72, and fewer spills); a step
+          // As below, a barrier for every second step (96 x 16384 tokens of 32/8 heads: 82.5 us in all with one for every step, now 79.5); a step
           // writes K of t + 3 and V of t + 2
           walk(
               [&]() {
@@ -575,7 +577,7 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
               [](int) {});
         } else if constexpr (L::kScaled) {
           // One side at a time: K of t + 2 is written inside step t, where K of t is read, and the registers then take V of t + 1.  256 channels, 64 x 32768 tokens of 64/8 heads:
-          // 318 us instead of 334 with fp16 queries, which spill registers with both sides on their way, but 321 instead of 305 with bf16
+          // 350 us instead of 380 with fp16 queries, which spill registers with both sides on their way, but 352 instead of 335 with bf16
           walk(
               [&]() {
                 typename L::Block k1;
@@ -626,8 +628,8 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         auto load_k = [&](int t) { load(a.k_pages, k_off, sh.k[slot(t)], t); };
         auto load_v = [&](int t) { load(a.v_pages, v_off, sh.v[slot(t)], t); };
         if constexpr (kRing == 4) {
-          // Two blocks at a time: a wait and a barrier for every second step, with the next two blocks on their way for a step and a half (64 x 32768 tokens, 64/8 heads: 116 us
-          // in all with one for every step, now 113).  Two steps read K of t + 1 and t + 2 and V of t and t + 1; the places of all before are free
+          // Two blocks at a time: a wait and a barrier for every second step, with the next two blocks on their way for a step and a half (64 x 32768 tokens, 64/8 heads: 138 us
+          // in all with one for every step, now 135).  Two steps read K of t + 1 and t + 2 and V of t and t + 1; the places of all before are free
           walk(
               [&]() {
                 load_k(t0);
@@ -662,7 +664,6 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
         }
       }
 
-      __builtin_amdgcn_s_setprio(0);
       // ---- both halves of a row's keys, and its place ----
       float l = w.l;
       {
@@ -690,8 +691,8 @@ __global__ void __launch_bounds__(64 * prefix_waves(D)) prefix_kernel(PagedDecod
             for (int i = 0; i < 16; ++i) w.o[n][i] = w.o[n][i] * k1 + mail[16 * n + i][lane] * k2;
         }
       }
-      // Rows leave through LDS, where each wavefront has a place: lanes hold 16 bytes of 32 rows at a time, memory takes whole rows (2.4 us of
-      // 84 for the 33 MB of parts of 64 x 32768 tokens, 64/8 heads)
+      // Rows leave through LDS, where each wavefront has a place: lanes hold 16 bytes of 32 rows at a time, memory takes whole rows (2.4 us for
+      // the 33 MB of parts of 64 x 32768 tokens, 64/8 heads)
       lds_barrier();                                   // nobody reads a block, or another wavefront's part, any more
       if (busy && (PARTS == 1 || part == 0)) {
         int me = lane;                                 // not known to be the lane: places would be formed in front of the walk and kept in registers through it

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests.paged8_util import cache8, prefix64, values64
-from tests.paged_util import check_rounded
+from tests.paged_util import attention64, check_rounded
 from tests.test_gpu_paged import DTYPES, I32, _ints, _randn
 from tests.test_gpu_paged_prefix import T  # noqa: F401
 
@@ -60,3 +60,35 @@ def test_long_parts(T, D, blocks, G, members, dtype, bits):  # noqa: F811
     want, wl, eo, el = prefix64(q[:, rows].contiguous(), *few, table, lens, [start] * members, 1 / math.sqrt(D), dtype if bits == 16 else torch.bfloat16)
     check_rounded(got[:, rows], want, eo)
     assert bool(((lse[:, rows].double() - wl).abs() <= el).all())
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("Hq,Hkv", [(16, 4), (128, 4)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [16, 8])
+def test_probabilities_of_common_tokens_hold_two_pieces(T, D, Hq, Hkv, dtype, bits):  # noqa: F811
+    """Exact scores of which a few tokens have the weight: fp32 results are as near to 64 bits over common tokens as over a sequence's own."""
+    page, start, members, scale = 16, 256, 5, 0.25
+    lens = [start, start + 1, start + 7, start + 16, start + 40]
+    shared = start // page
+    n_pages = shared + 3 * members + 1
+    g = torch.Generator(device="cuda").manual_seed(D + Hq)
+    # products and their sums are whole numbers
+    k = torch.randint(-1, 2, (n_pages, Hkv, page, D), generator=g, device="cuda").to(dtype)
+    q = (2 * torch.randint(-1, 2, (members, Hq, D), generator=g, device="cuda")).to(dtype)
+    v = torch.randn(n_pages, Hkv, page, D, generator=g, device="cuda").to(dtype)
+    pages = (k, v) if bits == 16 else cache8(k, v)
+    values = (k, v) if bits == 16 else (values64(*pages[:2]), values64(*pages[2:]))
+    table = torch.full((members, shared + 3 + (130 << 20) // (members * Hkv * page * D * 2)), -1, dtype=I32, device="cuda")
+    table[:, :shared] = torch.arange(shared)
+    table[:, shared:shared + 3] = shared + torch.arange(3 * members).view(members, 3)
+    f = T.thrift_paged_decode_prefix if bits == 16 else T.thrift_paged_decode_prefix8
+    got, lse = f(q, *pages, table, _ints(lens), _ints([0] * members), _ints([start]), softmax_scale=scale, out_dtype=torch.float32, return_lse=True)
+    want, wl, _, _ = attention64(q, *values, table, lens, scale)
+    weights = torch.stack([attention64(q[b:b + 1], values[0], values[1].abs(), table[b:b + 1], [n], scale)[0][0] for b, n in enumerate(lens)])
+    # Of a weight: 2^-16 by its two pieces; the factor of the scores (rounded once, U of at most 64 binades that matter) and the difference to the reference
+    # (the same), 8 U for the exponential and the joins, all of it twice, in the weight and in their sum; and a sum over at most 296 tokens, of weights and of values.
+    U = 2.0 ** -24
+    rel = 2.0 ** -16 + (2 * (64 + 64 + 8) + 2 * 296) * U
+    assert bool(((got.double() - want).abs() <= rel * weights).all())
+    assert bool(((lse.double() - wl).abs() <= (2 * (64 + 64 + 8) + 296 + wl.abs()) * U).all())
