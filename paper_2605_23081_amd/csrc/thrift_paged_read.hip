@@ -131,7 +131,7 @@ void launch(const PagedReadArgs& a, hipStream_t st) {
   z.chunks = a.D / 8;
   z.rows = kItems / z.chunks;
   if (z.rows > a.N) z.rows = a.N;
-  z.parts = (a.N + z.rows - 1) / z.rows;
+  z.parts = (int)(((long)a.N + z.rows - 1) / z.rows);
   z.magic = z.chunks == 1 ? 0u : (uint32_t)((0x100000000ull + z.chunks - 1) / z.chunks);
   const long groups = (long)a.B * a.Hkv * z.parts;          // at most B * Hkv * N
   z.groups = (uint32_t)groups;

@@ -66,3 +66,15 @@ def test_more_heads_than_a_launch_has_workgroups(T, bits):  # noqa: F811
         rows = pages[names[:, 0].long(), :, first.long()]
         rows[first >= lens] = 0
         assert torch.equal(got[:, :, 0], rows)
+
+
+def test_the_longest_rows(T):  # noqa: F811
+    """2^31 - 1 tokens of one head, of which the sequence has all but the last 255."""
+    D, page, N = 8, 256, 2 ** 31 - 1
+    width = 2 ** 23 - 1                                                      # 2^31 - 256 tokens
+    names = torch.randint(0, 7, (1, width), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda", dtype=I32)
+    kp, vp = (_randn(7, 1, page, D, dtype=DT, seed=i) for i in (0, 1))
+    k, v = T.thrift_paged_read(kp, vp, names, _ints([2 ** 31 - 1]), N)
+    for got, pages in ((k, kp), (v, vp)):
+        _same_rows(got[0, 0, :width * page], pages[:, 0], names[0], 1 << 24)
+        assert not bool(got[0, 0, width * page:].any())
