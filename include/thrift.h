@@ -482,7 +482,7 @@ size_t thrift_paged_decode_workspace(int B, int Hq, int Hkv, int max_pages, int 
  *     of Hkv, at most 32 heads per KV head; B * Hq below 2^23, n_pages * page_size and max_pages * page_size below 2^31,
  *     B * Hkv * max_pages * page_size below 2^35
  *   seqlens [B]: cached tokens, clamped to 0 .. max_pages * page_size.  What pages hold past the length reaches no result, whatever
- *     it is.  A sequence of length 0 gives zeros.  Within the length, values are finite (an infinite one gives NaN in its channel)
+ *     it is.  A sequence of length 0 gives zeros.  Within the length, values are finite (an infinite one gives NaN or infinity in its channel)
  *     and so is the sum of `len` of them in fp32 (bf16 reaches past that from 2^128 / len on).  A key whose score is -inf weighs nothing; a row of such
  *     keys alone gives NaN.
  *   block_table entries within the length must name pages; others give unspecified numbers but are never followed outside

@@ -92,3 +92,33 @@ def test_probabilities_of_common_tokens_hold_two_pieces(T, D, Hq, Hkv, dtype, bi
     rel = 2.0 ** -16 + (2 * (64 + 64 + 8) + 2 * 296) * U
     assert bool(((got.double() - want).abs() <= rel * weights).all())
     assert bool(((lse.double() - wl).abs() <= (2 * (64 + 64 + 8) + 296 + wl.abs()) * U).all())
+
+
+@pytest.mark.parametrize("members,G", [(2, 1), (5, 32)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bits", [16, 8])
+def test_the_longest_start_with_a_few_tokens_that_count(T, members, G, dtype, bits):  # noqa: F811
+    """2^31 - 16 common tokens in four pages over and over, and five pages at odd places whose scores are far above all others: keys and values there have to be
+    each other's."""
+    D, page, width = 64, 16, 2 ** 27 - 1
+    places = [3, 12345, 2 ** 26 - 1, 2 ** 26 + 4097, width - 1]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    kp, vp = (torch.randn(9, 1, page, D, generator=g, device="cuda") for _ in range(2))
+    q = torch.randn(members, G, D, generator=g, device="cuda") * 0.25
+    q[:, :, 0] = 16.0                                                        # channel 0: 16 * 32 / 8 = 64 above the rest, which has a few units
+    kp[:, :, :, 0] = 0.0
+    kp[4:, :, :, 0] = 32.0
+    kp, vp, q = kp.to(dtype), vp.to(dtype), q.to(dtype)
+    pages = (kp, vp) if bits == 16 else cache8(kp, vp)
+    kv, vv = (kp, vp) if bits == 16 else (values64(*pages[:2]), values64(*pages[2:]))
+    table = torch.arange(width, dtype=I32, device="cuda").remainder_(4)
+    table[torch.tensor(places, device="cuda")] = torch.arange(4, 9, dtype=I32, device="cuda")
+    table = table.expand(members, width).contiguous()
+    print(f"longest start with a few tokens {members} {G} {bits} {dtype}", flush=True)
+    f = T.thrift_paged_decode_prefix if bits == 16 else T.thrift_paged_decode_prefix8
+    got, lse = f(q, *pages, table, _ints([2 ** 31 - 1] * members), _ints([0] * members), _ints([2 ** 31 - 1]), out_dtype=torch.float32, return_lse=True)
+    # the 80 tokens alone: 2^31 others of a score that is at least 50 lower weigh 2^31 e^-50 < 2^-41
+    few = torch.arange(4, 9, dtype=I32, device="cuda").expand(members, 5)
+    want, wl, eo, el = attention64(q, kv, vv, few, [80] * members, 1 / math.sqrt(D))
+    assert bool(((got.double() - want).abs() <= eo + 2.0 ** -30 * vv.double().abs().max()).all())
+    assert bool(((lse.double() - wl).abs() <= el + 2.0 ** -30).all())
