@@ -184,9 +184,9 @@ __global__ void __launch_bounds__(kHeadThreads) paged_append8_items_kernel(Paged
 }
 
 // A workgroup takes as few tokens as still give every thread a head, mostly one, and goes over its heads two or three times.  The kernel is bound by
-// memory, but with 88 registers five wavefronts fit on a SIMD, and workgroups of eight tokens, which turn more heads per formed angle, came to 1.6 rounds
-// of the chip with an idle end (eight / one, us): 72 / 60 for 8192 tokens of 64/8 heads (319 MB, 5.3 TB/s), 147 / 130 for 32768 of 32/8, 13.8 / 11.5 for 8192 of
-// 16/2 heads of 64 channels, 7.2 / 7.8 for 1024 of 32/8.  Reading past the caches takes 57 for the first, but 21 instead of 18 where the heads, 50 MB, were just written.
+// memory; workgroups of eight tokens turn more heads per formed angle, but are a fraction of the number (eight / one, us): 72 / 60 for 8192 tokens of 64/8 heads
+// (319 MB, 5.3 TB/s), 147 / 130 for 32768 of 32/8, 13.8 / 11.5 for 8192 of 16/2 heads of 64 channels, 7.2 / 7.8 for 1024 of 32/8.  72 registers, seven wavefronts per SIMD (fp16
+// in the interleaved layout: 88 and five).  Reading past the caches takes 57 for the first, but 21 instead of 18 where the heads, 50 MB, were just written.
 HeadShape shape_of(const PagedAppendArgs& a) {
   const int total = a.Hq + 2 * a.Hkv;
   HeadShape z = head_shape(a.T, total, a.D, a.rot);
